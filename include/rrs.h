@@ -93,8 +93,9 @@ enum {
   RRS_ERR_ARCH = -7,       /* the current device is not gfx950 */
   RRS_ERR_HIP = -8,        /* a HIP runtime call or launch failed */
   RRS_ERR_FLAGS = -9,      /* unknown or unsupported flag bits (_ex functions) */
-  RRS_ERR_PRECONDITION = -10, /* RRS_DEBUG only: an input is not finite, or perm /
-                                 block_order is not a permutation */
+  RRS_ERR_PRECONDITION = -10, /* RRS_DEBUG only: an input is not finite, perm /
+                                 block_order is not a permutation, or an index of the
+                                 key/value cache's calls is out of range */
   RRS_ERR_TIMEOUT = -11       /* RRS_DEBUG only: a bounded wait between workgroups ran
                                  out (the affected outputs were written as NaN) */
 };
@@ -544,6 +545,150 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
                                       int N, int K, int group_size, int flags, void* Y,
                                       void* workspace, size_t workspace_bytes, void* scratch,
                                       size_t scratch_bytes, void* stream);
+
+/*
+ * ------------------------------------------------------------------------
+ * Paged key/value cache: what stands between the fused QKV projection and the
+ * output projection when tokens are decoded (the paper's A4W4KV16 and A4W4KV4
+ * settings, Section 4.1: the cache in 16 bits, or in 4 bits with one scale per
+ * group of channels, round to nearest). Positions are rotated into queries and
+ * keys and both caches are written in one pass (rrs_rope_kv_append), one new
+ * token per sequence attends to its cache (rrs_paged_attention), and a cache
+ * that has grown past its bound gives up the tokens that received least
+ * attention (rrs_kv_evict).
+ *
+ * Cache. Tokens live in pages of page_size slots; sequence b's slot t is slot
+ * t % page_size of page table[b * max_pages + t / page_size]. Per layer:
+ *  - k, v: pages x kv_heads x page_size rows of head_dim values, row-major, so that one
+ *    head's page is one contiguous run. RRS_KV_F16: float16. RRS_KV_INT4: head_dim / 2
+ *    bytes of packed codes (two's complement in [-7, 7], low nibble = even channel,
+ *    as everywhere in this library).
+ *  - k_scale, v_scale (RRS_KV_INT4; else NULL): pages x kv_heads x page_size float16,
+ *    one per row: s = fp16(max |x| / 7), q = clamp(rint(x / s), -7, 7) of the
+ *    float16 values x (codes 0 where s = 0); the row stands for q s. The scale is rounded
+ *    before it divides, so codes and scale are exact functions of x.
+ *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
+ *    read. No page belongs to two rows of the table in a call that writes the cache.
+ * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,
+ * sequences, max_pages, pages >= 1; sequences * kv_heads < 2^23; max_pages * page_size
+ * < 2^31. The struct is read on the host during the call only.
+ *
+ * The calls below follow the conventions at the top of this file; wrong sizes are
+ * RRS_ERR_SHAPE, an unknown format or flag RRS_ERR_FLAGS. Every device array is 16-byte
+ * aligned. Indices in device memory are bounded by the kernels: a page outside [0, pages)
+ * is not written and reads as page 0, lengths are cut to [0, max_length]; with RRS_DEBUG
+ * such an index is RRS_ERR_PRECONDITION. Values in slots at or past a
+ * sequence's length are never used, whatever they hold.
+ * ------------------------------------------------------------------------
+ */
+enum { RRS_KV_F16 = 0, RRS_KV_INT4 = 1 };
+
+typedef struct rrs_kv_cache {
+  void* k;
+  void* v;
+  void* k_scale;        /* NULL for RRS_KV_F16 */
+  void* v_scale;        /* NULL for RRS_KV_F16 */
+  const int32_t* table; /* sequences x max_pages */
+  int32_t format;       /* RRS_KV_F16 or RRS_KV_INT4 */
+  int32_t pages;        /* pages of k and v */
+  int32_t kv_heads;
+  int32_t page_size;
+  int32_t head_dim;
+  int32_t sequences;
+  int32_t max_pages;    /* table entries per sequence */
+} rrs_kv_cache;
+
+/* Pairs (2 j, 2 j + 1) instead of (j, j + rotary_dim / 2). */
+enum { RRS_ROPE_INTERLEAVED = 1 };
+
+/*
+ * Rotary positions and cache append in one pass over the QKV projection's output.
+ *   qkv       in : M rows of (heads + 2 kv_heads) head_dim float16 (queries, keys,
+ *                  values), row m at m * row_stride elements; row_stride a multiple of 8,
+ *                  at least the row.
+ *   positions in : M x axes int32 (1 <= axes <= 4): a token's position on every axis (one
+ *                  for text; time, height and width for images and video).
+ *   sections  in : HOST array of `axes` ints >= 0 with sum rotary_dim / 2: the first
+ *                  sections[0] frequencies turn with axis 0, the next sections[1] with
+ *                  axis 1, and so on.
+ *   rope      in : rope_rows x rotary_dim float32: row p holds the cosines, then the
+ *                  sines, of position p at the rotary_dim / 2 frequencies. A position
+ *                  outside [0, rope_rows) takes the nearest row.
+ *   rotary_dim   : a multiple of 16, 16 <= rotary_dim <= head_dim; further channels pass
+ *                  through. Pair (x, y) becomes (x c - y s, y c + x s), in float32,
+ *                  rounded to float16 once.
+ *   seq, slot in : M int32: where token m's key and value go. seq outside
+ *                  [0, sequences) or slot outside [0, max_pages * page_size): the token
+ *                  is not stored (padding). No two tokens share a place.
+ *   Q        out : M x heads x head_dim float16, the rotated queries.
+ *   weights, slot_pos: NULL, or the arrays of rrs_kv_evict (sequences x kv_heads x
+ *                  max_pages * page_size): a stored token's entries become 0 and its
+ *                  position on axis 0.
+ */
+rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int heads,
+                              const int32_t* positions, int axes, const int32_t* sections,
+                              const float* rope, int rope_rows, int rotary_dim, int flags,
+                              const rrs_kv_cache* cache, const int32_t* seq, const int32_t* slot,
+                              void* Q, float* weights, int32_t* slot_pos, void* stream);
+
+/*
+ * Attention of one new token per sequence over its cache (the token's own key and value
+ * appended before):
+ *   out[b, h] = sum_t p_t v_t,  p = softmax over t < lengths[b] of scale q_bh . k_t.
+ *   Q        in : sequences x heads x head_dim float16; heads a multiple of kv_heads, query
+ *                 head h reads KV head h / (heads / kv_heads).
+ *   lengths  in : sequences int32; max_length >= every length, 1 <= max_length <=
+ *                 max_pages * page_size (it sizes the launch and the workspace).
+ *   mask     in : NULL, or sequences x (max_pages * page_size) bytes; slots with 0 take no
+ *                 part.
+ *   weights     : NULL, or sequences x kv_heads x (max_pages * page_size) float32, in
+ *                 place: slot t < lengths[b] gains the sum of p_t over the KV head's query
+ *                 heads.
+ *   out     out : sequences x heads x head_dim float16; zeros where no slot takes part.
+ *   lse     out : NULL, or sequences x heads float32, log sum_t exp(scale q . k_t)
+ *                 (-inf where no slot takes part), with which outputs over parts of
+ *                 a context are joined.
+ *   workspace   : at least rrs_paged_attention_workspace_bytes; contents ignored.
+ * Logits, softmax and sums in float32. Results do not depend on the other sequences of the
+ * batch's values, and repeat bit for bit for the same shapes and max_length.
+ */
+size_t rrs_paged_attention_workspace_bytes(const rrs_kv_cache* cache, int heads, int max_length,
+                                           int with_weights);
+rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cache,
+                               const int32_t* lengths, int max_length, float scale,
+                               const uint8_t* mask, float* weights, void* out, float* lse,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction by accumulated attention weight. For every sequence and KV head, of the slots
+ * below n = lengths[b] the first `budget` are kept in this order: protected slots
+ * (slot_pos >= keep_from[b]), then larger weight, then lower slot (a NaN weight counts as
+ * less than every number). Kept slots below budget stay where they are; the evicted ones
+ * among them take, in increasing order, the kept slots at or above budget. Keys carry their
+ * positions, so the order of slots means nothing to attention. Nothing moves where
+ * n <= budget.
+ *   weights, slot_pos      in : sequences x kv_heads x (max_pages * page_size) float32 / int32.
+ *   keep_from              in : sequences int32.
+ *   budget                    : 1 <= budget <= max_pages * page_size.
+ *   kept                  out : sequences x kv_heads x budget int32: the slot that slot
+ *                               j's token came from; -1 from min(n, budget) on.
+ *   new_lengths           out : sequences int32, min(n, budget).
+ *   weights_out, pos_out  out : as weights and slot_pos, of the moved slots; 0 and -1 from
+ *                               new_lengths[b] on. They must not overlap the inputs.
+ * k, v and the scales are moved in place. Pages past the new length are the caller's to reuse.
+ */
+rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int max_length,
+                        const float* weights, const int32_t* slot_pos, const int32_t* keep_from,
+                        int budget, int32_t* kept, int32_t* new_lengths, float* weights_out,
+                        int32_t* pos_out, void* stream);
+
+/*
+ * The cached values as float16: K and V, each sequences x kv_heads x max_length x
+ * head_dim, zeros from a sequence's length on (for the attention of a prompt's tokens, and
+ * to look at what an INT4 cache stands for: fp16(q s)).
+ */
+rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int max_length, void* K,
+                       void* V, void* stream);
 
 #ifdef __cplusplus
 }

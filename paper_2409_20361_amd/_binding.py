@@ -14,6 +14,7 @@ _lib: Optional[ctypes.CDLL] = None
 _vp = ctypes.c_void_p
 _i = ctypes.c_int
 _sz = ctypes.c_size_t
+_f = ctypes.c_float
 
 _SIGNATURES = {
     "rrs_status_string": (ctypes.c_char_p, [ctypes.c_int32]),
@@ -63,6 +64,13 @@ _SIGNATURES = {
                                             _vp, _sz, _vp]),
     "rrs_linear_reorder_scratch": (ctypes.c_int32, [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp,
                                                     _sz, _vp, _sz, _vp]),
+    "rrs_rope_kv_append": (ctypes.c_int32, [_vp, ctypes.c_int64, _i, _i, _vp, _i, _vp, _vp, _i,
+                                            _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "rrs_paged_attention_workspace_bytes": (_sz, [_vp, _i, _i, _i]),
+    "rrs_paged_attention": (ctypes.c_int32, [_vp, _i, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _vp,
+                                             _sz, _vp]),
+    "rrs_kv_evict": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    "rrs_kv_read": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp]),
 }
 
 # Channels per block of the runtime reorder (include/rrs.h, RRS_REORDER_BLOCK).

@@ -11,38 +11,17 @@
 #include <vector>
 
 #include "rrs.h"
+#include "rrs_check.h"
 #include "rrs_internal.h"
 
-namespace {
+using rrs::check_device;
+using rrs::debug_check_finite_f16;
+using rrs::debug_enabled;
+using rrs::debug_fetch;
+using rrs::from_hip;
+using rrs::is_aligned;
 
-constexpr int kVersion = 602;  // 0.6.2: GEMM on scratch memory
-constexpr int kMaxDevices = 64;
-
-bool is_aligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-bool valid_k(int K) { return K >= 512 && K <= 16384 && (K & (K - 1)) == 0; }
-bool valid_m(int M) { return M >= 1; }
-bool valid_n(int N) { return N >= 1 && (N % 16) == 0; }
-bool valid_group(int K, int g) {
-  return (g == 64 || g == 128 || g == 256 || g == 512) && K % g == 0;
-}
-bool valid_flags(int flags, int allowed) { return (flags & ~allowed) == 0; }
-// Every _ex function accepts RRS_WEIGHT_TILED, so that one flags value can
-// serve all calls of a layer; only the calls that read or write Wq use it.
-constexpr int kQuantFlags = RRS_SKIP_ROTATION | RRS_SKIP_SMOOTHING;
-constexpr int kAllFlags = kQuantFlags | RRS_WEIGHT_TILED;
-constexpr int kRotationFlags = RRS_SKIP_ROTATION | RRS_WEIGHT_TILED;
-static_assert(RRS_SKIP_ROTATION == rrs::kSkipRotation && RRS_SKIP_SMOOTHING == rrs::kSkipSmoothing,
-              "public and internal flag values agree");
-
-rrs::WqLayout layout(int flags) { return rrs::WqLayout{(flags & RRS_WEIGHT_TILED) != 0}; }
-
-// Output scale of the GEMM: 2^-8 undoes the 16 x 16 of the unpacked int8
-// operands, 1/K the unnormalized rotation (absent without rotation).
-float out_scale(int K, int flags) {
-  const float s = std::ldexp(1.0f, -8);
-  return (flags & RRS_SKIP_ROTATION) ? s : s / (float)K;
-}
+namespace rrs {
 
 // RRS_DEBUG is read at every call (a getenv, far below a launch's cost), so a
 // process can switch the checks on and off between calls.
@@ -70,6 +49,81 @@ rrs_status debug_fetch(void* host, const void* dev, size_t bytes, void* stream) 
   return RRS_OK;
 }
 
+// Every float16 of the count at `p` is finite (exponent field not all ones).
+rrs_status debug_check_finite_f16(const void* p, size_t count, const char* what, void* stream) {
+  std::vector<uint16_t> h(count);
+  if (rrs_status e = debug_fetch(h.data(), p, count * 2, stream)) return e;
+  for (size_t i = 0; i < count; ++i) {
+    if ((h[i] & 0x7C00u) == 0x7C00u) {
+      std::fprintf(stderr, "[rrs] RRS_DEBUG: %s[%zu] is not finite (bits 0x%04x)\n", what, i,
+                   (unsigned)h[i]);
+      return RRS_ERR_PRECONDITION;
+    }
+  }
+  return RRS_OK;
+}
+
+namespace {
+constexpr int kMaxDevices = 64;
+// 0 = unknown, 1 = gfx950, 2 = other architecture.
+std::atomic<int> g_arch_cache[kMaxDevices];
+
+}  // namespace
+
+rrs_status check_device() {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess) {
+    (void)hipGetLastError();
+    return RRS_ERR_NO_DEVICE;
+  }
+  int cached = (dev >= 0 && dev < kMaxDevices) ? g_arch_cache[dev].load() : 0;
+  if (cached == 0) {  // the first call on this device
+    int count = 0;
+    if (hipGetDeviceCount(&count) != hipSuccess || count <= 0) {
+      (void)hipGetLastError();
+      return RRS_ERR_NO_DEVICE;
+    }
+    hipDeviceProp_t prop;
+    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) {
+      (void)hipGetLastError();
+      return RRS_ERR_HIP;
+    }
+    cached = (std::strncmp(prop.gcnArchName, "gfx950", 6) == 0) ? 1 : 2;
+    if (dev >= 0 && dev < kMaxDevices) g_arch_cache[dev].store(cached);
+  }
+  return cached == 1 ? RRS_OK : RRS_ERR_ARCH;
+}
+
+}  // namespace rrs
+
+namespace {
+
+constexpr int kVersion = 700;  // 0.7.0: the key/value cache operators
+
+bool valid_k(int K) { return K >= 512 && K <= 16384 && (K & (K - 1)) == 0; }
+bool valid_m(int M) { return M >= 1; }
+bool valid_n(int N) { return N >= 1 && (N % 16) == 0; }
+bool valid_group(int K, int g) {
+  return (g == 64 || g == 128 || g == 256 || g == 512) && K % g == 0;
+}
+bool valid_flags(int flags, int allowed) { return (flags & ~allowed) == 0; }
+// Every _ex function accepts RRS_WEIGHT_TILED, so that one flags value can
+// serve all calls of a layer; only the calls that read or write Wq use it.
+constexpr int kQuantFlags = RRS_SKIP_ROTATION | RRS_SKIP_SMOOTHING;
+constexpr int kAllFlags = kQuantFlags | RRS_WEIGHT_TILED;
+constexpr int kRotationFlags = RRS_SKIP_ROTATION | RRS_WEIGHT_TILED;
+static_assert(RRS_SKIP_ROTATION == rrs::kSkipRotation && RRS_SKIP_SMOOTHING == rrs::kSkipSmoothing,
+              "public and internal flag values agree");
+
+rrs::WqLayout layout(int flags) { return rrs::WqLayout{(flags & RRS_WEIGHT_TILED) != 0}; }
+
+// Output scale of the GEMM: 2^-8 undoes the 16 x 16 of the unpacked int8
+// operands, 1/K the unnormalized rotation (absent without rotation).
+float out_scale(int K, int flags) {
+  const float s = std::ldexp(1.0f, -8);
+  return (flags & RRS_SKIP_ROTATION) ? s : s / (float)K;
+}
+
 // `perm` (n entries) holds every value of 0..n-1 exactly once.
 rrs_status debug_check_perm(const int32_t* perm, int n, const char* what, void* stream) {
   if (!perm) return RRS_OK;
@@ -84,20 +138,6 @@ rrs_status debug_check_perm(const int32_t* perm, int n, const char* what, void* 
       return RRS_ERR_PRECONDITION;
     }
     seen[(size_t)v] = 1;
-  }
-  return RRS_OK;
-}
-
-// Every float16 of the count at `p` is finite (exponent field not all ones).
-rrs_status debug_check_finite_f16(const void* p, size_t count, const char* what, void* stream) {
-  std::vector<uint16_t> h(count);
-  if (rrs_status e = debug_fetch(h.data(), p, count * 2, stream)) return e;
-  for (size_t i = 0; i < count; ++i) {
-    if ((h[i] & 0x7C00u) == 0x7C00u) {
-      std::fprintf(stderr, "[rrs] RRS_DEBUG: %s[%zu] is not finite (bits 0x%04x)\n", what, i,
-                   (unsigned)h[i]);
-      return RRS_ERR_PRECONDITION;
-    }
   }
   return RRS_OK;
 }
@@ -154,35 +194,6 @@ rrs_status debug_check_finite_f32(const float* p, size_t count, const char* what
   return RRS_OK;
 }
 
-// 0 = unknown, 1 = gfx950, 2 = other architecture.
-std::atomic<int> g_arch_cache[kMaxDevices];
-
-rrs_status check_device() {
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess) {
-    (void)hipGetLastError();
-    return RRS_ERR_NO_DEVICE;
-  }
-  int cached = (dev >= 0 && dev < kMaxDevices) ? g_arch_cache[dev].load() : 0;
-  if (cached == 0) {  // the first call on this device
-    int count = 0;
-    if (hipGetDeviceCount(&count) != hipSuccess || count <= 0) {
-      (void)hipGetLastError();
-      return RRS_ERR_NO_DEVICE;
-    }
-    hipDeviceProp_t prop;
-    if (hipGetDeviceProperties(&prop, dev) != hipSuccess) {
-      (void)hipGetLastError();
-      return RRS_ERR_HIP;
-    }
-    cached = (std::strncmp(prop.gcnArchName, "gfx950", 6) == 0) ? 1 : 2;
-    if (dev >= 0 && dev < kMaxDevices) g_arch_cache[dev].store(cached);
-  }
-  return cached == 1 ? RRS_OK : RRS_ERR_ARCH;
-}
-
-rrs_status from_hip(hipError_t e) { return e == hipSuccess ? RRS_OK : RRS_ERR_HIP; }
-
 // The GEMM of a call: on the caller's scratch where that helps and is large
 // enough, else without. s == nullptr: per-channel; border: runtime reorder.
 hipError_t run_gemm(const void* Xq, const float* a, const float* s, const void* Wq,
@@ -216,7 +227,7 @@ const char* rrs_status_string(rrs_status s) {
     case RRS_ERR_NULL: return "RRS_ERR_NULL: a required pointer is NULL";
     case RRS_ERR_SHAPE:
       return "RRS_ERR_SHAPE: need M >= 1, N >= 1 with N % 16 == 0, K a power of two in "
-             "[512, 16384]";
+             "[512, 16384]; for the key/value cache the sizes that rrs.h states";
     case RRS_ERR_GROUP: return "RRS_ERR_GROUP: group size must be 64, 128, 256 or 512 and divide K";
     case RRS_ERR_ALIGN: return "RRS_ERR_ALIGN: every pointer must be 16-byte aligned";
     case RRS_ERR_WORKSPACE: return "RRS_ERR_WORKSPACE: workspace smaller than required";
@@ -228,8 +239,8 @@ const char* rrs_status_string(rrs_status s) {
       return "RRS_ERR_TIMEOUT: (RRS_DEBUG) a bounded wait between workgroups ran out; the "
              "affected outputs are NaN";
     case RRS_ERR_PRECONDITION:
-      return "RRS_ERR_PRECONDITION: (RRS_DEBUG) an input is not finite or a permutation is "
-             "not one";
+      return "RRS_ERR_PRECONDITION: (RRS_DEBUG) an input is not finite, a permutation is not "
+             "one, or an index is out of range";
     default: return "RRS_ERR_UNKNOWN";
   }
 }

@@ -1,0 +1,258 @@
+"""paged_attention on the GPU against a plain 64-bit form (bounds: _kv_util.attention)."""
+import math
+
+import pytest
+import torch
+
+import paper_2409_20361_amd as rrs
+from _kv_util import attention, make_cache
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(lengths, heads, hk, D, page, fmt, max_length=None, mask=None, with_weights=False,
+         scale=None, seed=0, spoil=True, sharp=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    B, top = len(lengths), max(max(lengths), 1)
+    cache = make_cache(gen, B, top if max_length is None else max_length, hk, D, page, fmt)
+    Q = (torch.randn((B, heads, D), generator=gen) * sharp).half().cuda()
+    if mask is not None:
+        mask = (torch.rand((B, cache.capacity), generator=gen) < mask).cuda()
+    if spoil:   # whatever lies past a sequence's end or under the mask is not used
+        dead = torch.arange(cache.capacity).cuda() >= torch.tensor(lengths).cuda()[:, None]
+        if mask is not None:
+            dead = dead | ~mask
+        b, t = dead.nonzero(as_tuple=True)
+        where = (cache.table[b, t // page].long(), slice(None), t % page)
+        if fmt == "f16":
+            cache.k[where], cache.v[where] = float("nan"), float("inf")
+        else:
+            cache.k_scale[where], cache.v_scale[where] = float("inf"), float("nan")
+    w = torch.rand((B, hk, cache.capacity), generator=gen).cuda() if with_weights else None
+    w0 = w.clone() if with_weights else None
+    n = torch.tensor(lengths, dtype=torch.int32).cuda()
+    out, lse = rrs.paged_attention(Q, cache, n, max_length=max_length or top, scale=scale,
+                                   mask=mask, weights=w, return_lse=True)
+    ref = attention(Q, cache, lengths, scale if scale is not None else D ** -0.5, mask)
+    for b, r in enumerate(ref):
+        label = f"sequence {b}, length {lengths[b]}"
+        if r is None:
+            assert not out[b].any(), label
+            assert (lse[b] == -math.inf).all(), label
+            if with_weights:
+                assert torch.equal(w[b], w0[b]), label
+            continue
+        err = (out[b].double().cpu() - r["o"]).abs()
+        assert (err <= r["tol"]).all(), (label, float((err - r["tol"]).max()))
+        assert ((lse[b].double().cpu() - r["lse"]).abs() <= r["lse_tol"]).all(), label
+        if with_weights:
+            m = lengths[b]
+            gain = w[b].double().cpu() - w0[b].double().cpu()
+            bound = r["w_tol"] + 2.0 ** -24 * (w0[b, :, :m].double().cpu() + r["w"])
+            assert ((gain[:, :m] - r["w"]).abs() <= bound).all(), label
+            assert torch.equal(w[b, :, m:], w0[b, :, m:]), label
+            assert torch.equal(w[b, :, :m][:, ~r["live"]], w0[b, :, :m][:, ~r["live"]]), label
+    return out, lse, w
+
+
+EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 100, 127, 128, 129, 255, 256, 257, 300]
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("D,page", [(64, 16), (128, 32), (128, 64), (256, 128), (256, 16)])
+def test_lengths(D, page, fmt):
+    _run(EDGES, 8, 2, D, page, fmt)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("heads,hk", [(1, 1), (4, 4), (3, 1), (8, 1), (15, 1), (16, 1), (17, 1),
+                                      (40, 1), (32, 2), (14, 2), (66, 2), (5, 5)])
+def test_heads(heads, hk, fmt):
+    _run([70, 1, 333, 0], heads, hk, 128, 16, fmt, with_weights=True)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("weights", [False, True])
+@pytest.mark.parametrize("D,heads,hk,lengths", [
+    (128, 4, 2, [1500, 2048, 1]), (128, 8, 1, [4097, 3]), (64, 6, 2, [9000]), (256, 4, 1, [5001]),
+    (128, 1, 1, [20011]), (64, 33, 1, [6000, 5999]),
+])
+def test_split_and_joined(D, heads, hk, lengths, weights, fmt):
+    _run(lengths, heads, hk, D, 64, fmt, with_weights=weights, seed=4)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("share", [0.0, 0.02, 0.5, 1.0])
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_mask(D, share, fmt):
+    _run([1, 16, 90, 700, 2500], 6, 2, D, 16, fmt, mask=share, with_weights=True, seed=5)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+def test_sharp_and_flat(fmt):
+    """Logits in the hundreds (one slot takes all), and all of them equal."""
+    _run([513, 64, 2000], 8, 2, 128, 32, fmt, sharp=40.0, with_weights=True, seed=6)
+    _run([513, 64, 2000], 8, 2, 128, 32, fmt, scale=0.0, with_weights=True, seed=6)
+    _run([513, 64, 2000], 8, 2, 128, 32, fmt, scale=-0.3, seed=6)
+
+
+def test_int4_scales_far_apart():
+    """Value rows whose scales differ by 2^20 and rows of zeros."""
+    gen = torch.Generator().manual_seed(8)
+    cache = make_cache(gen, 2, 700, 2, 128, 16, "int4")
+    e = torch.randint(-18, 3, cache.v_scale.shape, generator=gen)
+    cache.v_scale.copy_(torch.pow(2.0, e.double()).half())
+    cache.v_scale[torch.rand(e.shape, generator=gen).cuda() < 0.2] = 0
+    cache.v_scale[cache.table[1].long()] *= 2.0 ** -6
+    Q = torch.randn((2, 8, 128), generator=gen).half().cuda()
+    lengths = [700, 433]
+    out = rrs.paged_attention(Q, cache, torch.tensor(lengths, dtype=torch.int32).cuda(), 700)
+    for b, r in enumerate(attention(Q, cache, lengths, 128 ** -0.5)):
+        assert ((out[b].double().cpu() - r["o"]).abs() <= r["tol"]).all()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+def test_max_length_above_the_lengths(fmt):
+    """A generous bound changes nothing but the launch; lengths above the bound are cut."""
+    lengths = [40, 0, 1000]
+    _run(lengths, 4, 2, 128, 16, fmt, max_length=50000, with_weights=True)
+    gen = torch.Generator().manual_seed(2)
+    cache = make_cache(gen, 2, 96, 1, 64, 16, fmt)
+    Q = torch.randn((2, 2, 64), generator=gen).half().cuda()
+    cut = rrs.paged_attention(Q, cache, torch.tensor([90, -5], dtype=torch.int32).cuda(), 50)
+    r = attention(Q, cache, [50, 0], 64 ** -0.5)
+    assert ((cut[0].double().cpu() - r[0]["o"]).abs() <= r[0]["tol"]).all() and not cut[1].any()
+
+
+def test_pages_that_do_not_exist_read_as_page_0():
+    gen = torch.Generator().manual_seed(9)
+    cache = make_cache(gen, 1, 48, 1, 128, 16, "f16")
+    Q = torch.randn((1, 4, 128), generator=gen).half().cuda()
+    n = torch.tensor([48], dtype=torch.int32).cuda()
+    cache.table[0, 1] = 0
+    want = rrs.paged_attention(Q, cache, n, 48)
+    for bad in (-1, cache.k.shape[0], 2 ** 31 - 1):
+        cache.table[0, 1] = bad
+        assert torch.equal(rrs.paged_attention(Q, cache, n, 48), want)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+def test_offsets_past_32_bits(fmt):
+    """Pages whose rows begin past 2^32 bytes: a small table into a large pool."""
+    D, hk, page = 128, 32, 64
+    per_page = hk * page * (2 * D if fmt == "f16" else D // 2)
+    pages = (5 << 30) // per_page
+    dtype = torch.float16 if fmt == "f16" else torch.uint8
+    pool = [torch.zeros((pages, hk, page, D if fmt == "f16" else D // 2), dtype=dtype,
+                        device="cuda") for _ in range(2)]
+    scales = [torch.zeros((pages, hk, page), dtype=torch.float16, device="cuda")
+              if fmt == "int4" else None for _ in range(2)]
+    table = torch.tensor([[pages - 1, 0, pages - 2]], dtype=torch.int32, device="cuda")
+    big = rrs.KVCache(pool[0], pool[1], table, *scales)
+    gen = torch.Generator().manual_seed(10)
+    small = make_cache(gen, 1, 3 * page, hk, D, page, fmt, extra_pages=0)
+    for b, s in zip(big, small):
+        if b is not None and b.dim() > 2:
+            b[table[0].long()] = s[small.table[0].long()]
+    Q = torch.randn((1, hk, D), generator=gen).half().cuda()
+    n = torch.tensor([170], dtype=torch.int32).cuda()
+    assert torch.equal(rrs.paged_attention(Q, big, n, 192), rrs.paged_attention(Q, small, n, 192))
+    for x, y in zip(rrs.kv_read(big, n, 192), rrs.kv_read(small, n, 192)):
+        assert torch.equal(x, y)
+    # appended and evicted rows there, too
+    qkv = torch.randn((1, 3 * hk * D), generator=gen).half().cuda()
+    one = lambda v: torch.tensor([v], dtype=torch.int32).cuda()  # noqa: E731
+    w = torch.rand((1, hk, 192), generator=gen).cuda()
+    pos = torch.arange(192, dtype=torch.int32).cuda().expand(1, hk, 192).contiguous()
+    for c in (big, small):
+        rrs.rope_kv_append(qkv, one(5)[:, None], rrs.rope_table(9, D), c, one(0), one(170), hk)
+        rrs.kv_evict(c, one(171), w, pos, one(160), 60, 192)
+    for x, y in zip(rrs.kv_read(big, one(60), 192), rrs.kv_read(small, one(60), 192)):
+        assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+def test_streams_repeats_and_graph(fmt):
+    """The same bits on another stream, again, and from a graph replayed between other work."""
+    gen = torch.Generator().manual_seed(11)
+    lengths = torch.tensor([3000, 77, 0, 1], dtype=torch.int32).cuda()
+    cache = make_cache(gen, 4, 3000, 2, 128, 64, fmt)
+    Q = torch.randn((4, 8, 128), generator=gen).half().cuda()
+    w = torch.zeros((4, 2, cache.capacity), device="cuda")
+    ws = torch.empty(rrs.paged_attention_workspace_bytes(cache, 8, 3000, True),
+                     dtype=torch.uint8, device="cuda")
+
+    def call(out=None):
+        return rrs.paged_attention(Q, cache, lengths, 3000, weights=w, workspace=ws, out=out)
+    want = call()
+    first = w.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        w.zero_()
+        got = call()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(w, first)
+    out = torch.empty_like(Q)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out)
+    for i in range(4):
+        w.zero_()
+        out.fill_(float("nan"))
+        Q2 = torch.randn((4, 8, 128), generator=gen).half().cuda()
+        Q.copy_(Q2)
+        graph.replay()
+        torch.cuda.synchronize()
+        a, aw = out.clone(), w.clone()
+        w.zero_()
+        assert torch.equal(call(), a) and torch.equal(w, aw)
+        ws.random_()
+
+
+def test_lse_joins_parts():
+    """Two parts of one context, joined with their lse, are the whole."""
+    gen = torch.Generator().manual_seed(12)
+    cache = make_cache(gen, 1, 640, 2, 128, 64, "f16")
+    Q = torch.randn((1, 6, 128), generator=gen).half().cuda()
+    n = lambda v: torch.tensor([v], dtype=torch.int32).cuda()  # noqa: E731
+    whole, lse = rrs.paged_attention(Q, cache, n(640), 640, return_lse=True)
+    a, la = rrs.paged_attention(Q, cache, n(256), 640, return_lse=True)
+    rest = cache._replace(table=cache.table[:, 4:].contiguous())
+    b, lb = rrs.paged_attention(Q, rest, n(384), 384, return_lse=True)
+    top = torch.logaddexp(la, lb)
+    joined = a.float() * (la - top).exp()[..., None] + b.float() * (lb - top).exp()[..., None]
+    # three float16 outputs of size <= 1 (their own rounding and the weights', 2^-10 each)
+    assert (joined - whole.float()).abs().max() <= 3 * 2.0 ** -10
+    assert (top - lse).abs().max() <= 1e-4
+
+
+def test_refusals():
+    gen = torch.Generator().manual_seed(13)
+    cache = make_cache(gen, 2, 64, 2, 128, 16, "f16")
+    Q = torch.randn((2, 4, 128), generator=gen).half().cuda()
+    n = torch.tensor([5, 6], dtype=torch.int32).cuda()
+    call = rrs.paged_attention
+    with pytest.raises(rrs.RRSError, match="SHAPE"):
+        call(Q[:, :3].contiguous(), cache, n, 64)
+    with pytest.raises(rrs.RRSError, match="SHAPE"):
+        call(Q, cache, n, 0)
+    with pytest.raises(rrs.RRSError, match="SHAPE"):
+        call(Q, cache, n, 65)
+    with pytest.raises(ValueError):
+        call(Q[:1], cache, n, 64)
+    with pytest.raises(TypeError):
+        call(Q.float(), cache, n, 64)
+    with pytest.raises(TypeError):
+        call(Q, cache, n.long(), 64)
+    with pytest.raises(ValueError):
+        call(Q.transpose(0, 1).contiguous().transpose(0, 1), cache, n, 64)
+    with pytest.raises(TypeError):
+        call(Q, cache, n, 64, mask=torch.ones((2, 64), dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        call(Q, cache, n, 64, weights=torch.ones((2, 2, 63), device="cuda"))
+    need = rrs.paged_attention_workspace_bytes(cache, 4, 64, True)
+    assert need > 0
+    with pytest.raises(rrs.RRSError, match="WORKSPACE"):
+        call(Q, cache, n, 64, weights=torch.ones((2, 2, 64), device="cuda"),
+             workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    assert rrs.paged_attention_workspace_bytes(cache, 3, 64) == 0
