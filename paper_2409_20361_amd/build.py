@@ -28,8 +28,10 @@ SOURCES = ["rrs_api.cpp", "rrs_gemm_route.cpp", "rrs_quant.hip", "rrs_weight.hip
 # rrs_gemm_stream_gather.hip: keep MFMA results in VGPRs (the per-block
 #   rescale reads every accumulator; in AGPRs each read is an extra copy).
 # rrs_gemm_fp6.hip: the same (every partial is read by the rescale).
+# rrs_attention.hip: the same (logits are read by the softmax, sums rescaled).
 EXTRA = {"rrs_gemm_stream_gather.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "rrs_gemm_fp6.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "rrs_gemm_fp6.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "rrs_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in any kernel.
 # -ffp-contract=off: every rounding in the rotation and scale chain is an

@@ -11,17 +11,17 @@
 //                  (ds_read_b64_tr). The slots that a quarter of the wave reads are those whose p it holds,
 //                  so P goes from the first product's result into the second's operand without leaving the lane.
 // All of it is streaming: HBM bounds it (4 D bytes and 4 D flops per slot and query head), so
-// loads for the next tile are issued before the current one is computed.
+// loads for the next tile are issued before the current one is done with.
 //
-// The slots of a sequence are cut into chunks, one workgroup each; its four waves
-// take the chunk's tiles in turn and are joined in LDS, chunks of one sequence by a second kernel
-// in chunk order (so results repeat bit for bit). That kernel also turns the logits, kept
+// The slots of a sequence are cut into pieces, one workgroup each; its four waves
+// take the piece's tiles in turn and are joined in LDS, pieces of one sequence by a second kernel
+// in their order (so results repeat bit for bit). That kernel also turns the logits, kept
 // in the workspace when they are asked for, into attention weights.
 //
 // INT4. Codes become float16 exactly (an exponent is or-ed on, an offset taken off). A key's scale
-// multiplies its logit; a value's scale multiplies its p before p is rounded to float16.
-// So that this product neither overflows nor loses bits to subnormals, m is the maximum
-// of S + e, 2^e >= scale: p scale <= 1 and p <= 2^24.
+// multiplies its logit; a value's scale multiplies its p before p is rounded to float16. So that
+// this product neither overflows nor loses bits to subnormals, the scales are in units
+// of a power of two above the largest seen so far, kept like the softmax's maximum.
 //
 // p is rounded to float16 (as the matrix instruction needs it): 2^-11 relative per term, no
 // more than the rounding of the output itself. Everything else is float32.
@@ -32,10 +32,12 @@ namespace rrs {
 namespace {
 
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s;
 typedef __attribute__((address_space(3))) v2i* lds_v2i;
@@ -43,23 +45,125 @@ typedef __attribute__((address_space(3))) v2i* lds_v2i;
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 16;  // query heads per workgroup: columns of the products
+constexpr int kWidest = 256;  // sequences up to which pieces follow the lengths
 constexpr float kLog2e = 1.4426950408889634f;
 
-// Sizes of a launch, and where its pieces lie in the workspace.
+// Sizes of a launch, and where its pieces lie in the workspace. A piece is a run of one sequence's
+// slots, the work of one workgroup per KV head and row block; pieces of all sequences are
+// numbered one after another.
 struct Plan {
   int group;       // query heads per KV head
-  int row_blocks;  // workgroups per KV head and chunk: ceil(group / kRows)
-  int chunk;       // slots per workgroup
-  int chunks;      // of the longest sequence
+  int row_blocks;  // ceil(group / kRows)
+  int step;        // slots that a workgroup takes at a time: pieces are whole numbers of them
+  int target;      // workgroups to aim at; 0: pieces of `steps` steps each, `pieces` per sequence
+  int steps;       // at least so many steps to a piece
+  int pieces;
   int ld_logits;   // row stride of the logits: max_length rounded up to whole blocks of 16
-  float* part;     // sequences x heads x chunks x dim: sums relative to the chunk's m
-  float2* stats;   // sequences x heads x chunks: m (base 2) and the sum of p
+  int2* of_seq;    // sequences: first piece and number of pieces
+  float* part;     // pieces x heads x dim: sums relative to the piece's m
+  float2* stats;   // pieces x heads: m (base 2) and the sum of p
   float* logits;   // sequences x heads x ld_logits, base 2; nullptr: not wanted
 };
 
+// A piece of a sequence: slots [begin, end) of it, number `index` of all pieces, `count` of which
+// are the sequence's.
+struct Piece {
+  int b, n, begin, end, index, count, first;
+};
+
+// Inclusive prefix sums over the wave; the last lane holds the total.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1 lane below in the row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);  // 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);  // 4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);  // 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // rows 0, 2 into 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // the lower half's total
+  return x;
+}
+__device__ __forceinline__ int wave_total(int x) {
+  return __builtin_amdgcn_readlane(wave_prefix(x), 63);
+}
+
+// Which piece `index` is; false past the last. Every wave of every workgroup works this out for
+// itself from the lengths, so that sequences of any lengths are cut into pieces of about the same
+// size without the host knowing them.
+__device__ __forceinline__ bool find_piece(const AttentionArgs& a, const KvView& c,
+                                           const Plan& plan, int index, Piece* out) {
+  const int lane = threadIdx.x & 63;
+  const auto length = [&](int b) { return min(max(a.lengths[b], 0), a.max_length); };
+  const auto all_steps = [&](int n) { return max(1, (n + plan.step - 1) / plan.step); };
+  const auto steps_of = [&](int n) { return min(all_steps(n), 1 << 22); };  // sums fit an int
+  int q = plan.steps, b = -1, first = 0;
+  if (plan.target == 0) {
+    b = index / plan.pieces;
+    first = b * plan.pieces;
+    if (b >= c.sequences) return false;
+  } else if (c.sequences == 1) {
+    const int want = max(plan.target / (c.heads * plan.row_blocks), 1);
+    q = max(q, (all_steps(length(0)) + want - 1) / want);
+    b = 0;
+  } else {
+    const int want = max(plan.target / (c.heads * plan.row_blocks), 1);  // pieces
+    int steps[kWidest / 64] = {};  // of sequences lane, lane + 64, ...
+    int total = 0;
+#pragma unroll
+    for (int i = 0; i < kWidest / 64; ++i)
+      if (64 * i < c.sequences) {
+        if (64 * i + lane < c.sequences) steps[i] = steps_of(length(64 * i + lane));
+        total += steps[i];
+      }
+    q = max(q, (wave_total(total) + want - 1) / want);
+    // Each sequence's last piece is short: larger pieces until they fit the target.
+    for (int round = 0; round < 3; ++round) {
+      int sum = 0;
+#pragma unroll
+      for (int i = 0; i < kWidest / 64; ++i)
+        if (64 * i < c.sequences) sum += (steps[i] + q - 1) / q;
+      sum = wave_total(sum);
+      if (sum <= want || sum <= c.sequences) break;
+      q += max(1, (int)((long long)q * (sum - want) / want));
+    }
+    // The sequence whose pieces contain the index.
+#pragma unroll
+    for (int i = 0; i < kWidest / 64; ++i)
+      if (64 * i < c.sequences && b < 0) {
+        const int mine = (steps[i] + q - 1) / q;
+        const int upto = wave_prefix(mine);
+        const uint64_t past = __ballot(first + upto > index);
+        if (past) {
+          const int l = __builtin_ctzll(past);
+          b = 64 * i + l;
+          first += __builtin_amdgcn_readlane(upto - mine, l);
+        } else {
+          first += __builtin_amdgcn_readlane(upto, 63);
+        }
+      }
+    if (b < 0) return false;
+  }
+  const int n = __builtin_amdgcn_readfirstlane(length(b));
+  const int steps = all_steps(n);
+  const int count = ((c.sequences == 1 ? steps : steps_of(n)) + q - 1) / q;
+  const int i = index - first;
+  if (i >= count) return false;
+  // Even pieces: the first steps % count of them are one step longer.
+  const int base = steps / count, longer = steps % count;
+  const int from = i * base + min(i, longer);
+  const int to = from + base + (i < longer ? 1 : 0);
+  out->b = b;
+  out->n = n;
+  out->begin = __builtin_amdgcn_readfirstlane(from * plan.step);
+  out->end = __builtin_amdgcn_readfirstlane(min(n, to * plan.step));
+  out->index = index;
+  out->count = __builtin_amdgcn_readfirstlane(count);
+  out->first = first;
+  return true;
+}
+
 template <int D, bool kInt4>
 struct Shape {
-  static constexpr int kTile = kInt4 ? 64 : 32;      // slots per wave and step
+  // Slots per wave and step. 16 where 32 rows would not leave registers for a second wave.
+  static constexpr int kTile = kInt4 ? 64 : D == 256 ? 16 : 32;
   static constexpr int kBlocks = kTile / 16;         // of 16 slots
   static constexpr int kRow = kInt4 ? D / 2 : 2 * D; // bytes of a cache row
   static constexpr int kSteps = D / 32;              // mfma steps of a logit
@@ -72,6 +176,7 @@ struct Shape {
   static constexpr int kValues = kTile * kRow;       // bytes of a wave's value tile
   static constexpr int kSums = kRows * kLdO * 4;
   static constexpr int kLds = kValues > kSums ? kValues : kSums;  // per wave
+  static constexpr int kPerSimd = D == 256 ? 2 : 3;  // waves: limits the registers
 
   // Where 16-byte chunk c of slot t's value row lies in the wave's tile. The chunks of a row are
   // permuted by the slot, so that the rows that one transposed read touches lie in
@@ -109,18 +214,48 @@ __device__ __forceinline__ v8h eight_codes(uint32_t w) {
 }
 __device__ __forceinline__ int code_order(int e) { return (e >> 1) + 4 * (e & 1); }
 
-__device__ __forceinline__ v8h mask_halves(v8h x, const bool (&live)[8]) {
-  v4u w = __builtin_bit_cast(v4u, x);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    w[i] &= (live[2 * i] ? 0xFFFFu : 0u) | (live[2 * i + 1] ? 0xFFFF0000u : 0u);
-  return __builtin_bit_cast(v8h, w);
+// The T at byte `at` past an address that is the same for the wave: the address stays in scalar
+// registers and the offset in one vector register (the compiler would else keep a 64-bit
+// vector address for every such load of the loop).
+template <typename T>
+__device__ __forceinline__ T load_at(const void* base, uint32_t at) {
+  typedef const __attribute__((address_space(1))) uint8_t* Global;
+  Global p = (Global)base;
+  asm("" : "+s"(p), "+v"(at));
+  return *(const __attribute__((address_space(1))) T*)(p + at);
 }
 
-// Grid: units (sequence, KV head) x row blocks x chunks. The row blocks of a unit and chunk read
-// the same rows: they are 8 apart, on one XCD, and share its L2.
-template <int D, bool kInt4>
-__global__ void __launch_bounds__(kThreads)
+// Halves of x whose slot takes no part become 0.
+template <typename V>
+__device__ __forceinline__ V mask_halves(V x, const bool* live) {
+  constexpr int kDwords = sizeof(V) / 4;
+  typedef uint32_t W __attribute__((ext_vector_type(kDwords)));
+  W w = __builtin_bit_cast(W, x);
+#pragma unroll
+  for (int i = 0; i < kDwords; ++i)
+    w[i] &= (live[2 * i] ? 0xFFFFu : 0u) | (live[2 * i + 1] ? 0xFFFF0000u : 0u);
+  return __builtin_bit_cast(V, w);
+}
+
+// The largest of x over the four lanes of a column.
+__device__ __forceinline__ float column_max(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  const uint32_t v = __builtin_bit_cast(uint32_t, x);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]),
+               __builtin_bit_cast(float, (uint32_t)b[1]));
+}
+
+// p may grow to 2^kSlack before the sums are rescaled to a new maximum: few tiles then do it,
+// and float16 holds such p with the same relative precision.
+constexpr float kSlack = 8.0f;
+
+// Grid: pieces x KV heads x row blocks. The row blocks of a piece and head read the same rows: they
+// are 8 apart, on one XCD, and share its L2.
+template <int D, bool kInt4, bool kMask>
+__global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask && D == 128)))
     attention_kernel(AttentionArgs a, KvView c, Plan plan) {
   using S = Shape<D, kInt4>;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * S::kLds];
@@ -136,15 +271,13 @@ __global__ void __launch_bounds__(kThreads)
     rb = unit / 8 % plan.row_blocks;
     unit = unit / (8 * plan.row_blocks) * 8 + unit % 8;
   }
-  const int chunk = unit % plan.chunks;
-  unit /= plan.chunks;
-  if (unit >= c.sequences * c.heads) return;  // the last eight may be short
-  const int b = unit / c.heads, hk = unit % c.heads;
-  const int n = min(a.lengths[b], a.max_length);
-  const int begin = chunk * plan.chunk;
-  if (begin >= n && chunk > 0) return;
-  const int end = min(n, begin + plan.chunk);
-  const bool whole = n <= plan.chunk;  // the sequence is this one chunk
+  const int hk = unit % c.heads;
+  Piece piece;
+  if (!find_piece(a, c, plan, unit / c.heads, &piece)) return;
+  const int b = piece.b, n = piece.n, begin = piece.begin, end = piece.end;
+  const bool whole = piece.count == 1;  // the piece is the sequence
+  if (plan.of_seq && threadIdx.x == 0 && hk == 0 && rb == 0 && piece.index == piece.first)
+    plan.of_seq[b] = make_int2(piece.first, piece.count);
 
   // Queries as the second operand: column col, channels as the keys' lanes hold them.
   const int rows = min(plan.group - rb * kRows, kRows);
@@ -162,75 +295,95 @@ __global__ void __launch_bounds__(kThreads)
       q[i] = x;
     }
   }
-  const float scale = a.scale * kLog2e;
+  // Logits are compared unscaled: a negative scale turns the queries around, and of no scale at
+  // all every logit is 0.
+  float scale = a.scale * kLog2e;
+  if (!(scale > 0.0f)) {
+    const _Float16 turn = (_Float16)(scale < 0.0f ? -1.0f : 0.0f);
+#pragma unroll
+    for (int i = 0; i < S::kSteps; ++i) q[i] *= turn;
+    scale = scale < 0.0f ? -scale : 1.0f;
+  }
+  float* logits = nullptr;
+  if (plan.logits && col < rows)
+    logits = plan.logits + ((size_t)b * a.heads + head0 + col) * plan.ld_logits + 4 * quarter;
 
   v4f o[S::kOut] = {};
   float m = -INFINITY, sum = 0.0f;
+  float rounded = 0.0f;  // float16 values: the sum of p as the products take it
+  float vnorm = 0x1p-14f;  // INT4: the power of two that value scales and o are in units of
   uint8_t* tile = lds + wave * S::kLds;
 
+  // Pages: lane i holds page page0 + i of the sequence.
+  const int last = (n - 1) & ~15;  // the last block of 16 slots
+  int page0 = 0, pages = 0;
+  const auto load_pages = [&](int first) {
+    page0 = first;
+    pages = c.page_of(b, min(first + lane, last >> c.log_page));
+  };
   // Loads of one tile: keys as operands, values as contiguous pieces of their rows, scales of the
-  // lane's four slots per block. Rows past the sequence's end read its last row.
+  // lane's four slots per block. Blocks past the sequence's end read its last one. Rows past the
+  // end lie in that block, in a page of the cache; what they hold is dropped below.
   v4u key[S::kBlocks][(S::kKey + 15) / 16];
   v4u val[S::kBlocks][S::kPieces];
-  uint2 ks[S::kBlocks], vs[S::kBlocks];
-  const auto first_row = [&](int t) {  // of the block of 16 slots at t, and rows from there
-    const int p = c.page_of(b, t >> c.log_page);
-    return c.page_row(p, hk) + (t & ((1 << c.log_page) - 1));
-  };
-  const int last = (n - 1) & ~15;
+  v2u ks[S::kBlocks], vs[S::kBlocks];
+  uint32_t mask[S::kBlocks];
+  size_t row[S::kBlocks];  // the blocks' first rows
+  const uint32_t key_at = col * S::kRow + quarter * (kInt4 ? S::kKey : 16);
   const auto load_keys = [&](int t0) {
+    if ((min(t0 + S::kTile - 16, last) >> c.log_page) - page0 >= 64) load_pages(t0 >> c.log_page);
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u) {
       const int t = min(t0 + 16 * u, last);
-      const size_t row = first_row(t);
-      const int slot = min(col, n - 1 - t);
-      const uint8_t* p = c.k + row * S::kRow + slot * S::kRow + quarter * (kInt4 ? S::kKey : 16);
+      const int page = t >> c.log_page;
+      row[u] = c.page_row(__builtin_amdgcn_readlane(pages, page - page0), hk) +
+               (t & ((1 << c.log_page) - 1));
+      const uint8_t* p = c.k + row[u] * S::kRow;
       if constexpr (S::kKey < 16) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p);
-        key[u][0] = v4u{w.x, w.y, 0u, 0u};
+        const v2u w = load_at<v2u>(p, key_at);
+        key[u][0] = v4u{w[0], w[1], 0u, 0u};
       } else {
 #pragma unroll
         for (int i = 0; i < S::kKey / 16; ++i)
-          key[u][i] = *reinterpret_cast<const v4u*>(p + i * (kInt4 ? 16 : 64));
+          key[u][i] = load_at<v4u>(p + i * (kInt4 ? 16 : 64), key_at);
       }
       if constexpr (kInt4) {  // four slots: 8 bytes, inside the page
-        ks[u] = *reinterpret_cast<const uint2*>(c.k_scale + row + 4 * quarter);
-        vs[u] = *reinterpret_cast<const uint2*>(c.v_scale + row + 4 * quarter);
+        ks[u] = load_at<v2u>(c.k_scale + row[u], 8 * quarter);
+        vs[u] = load_at<v2u>(c.v_scale + row[u], 8 * quarter);
       }
+      if constexpr (kMask)  // four slots: aligned, inside the row
+        mask[u] = load_at<uint32_t>(a.mask + (size_t)b * c.capacity() + t, 4 * quarter);
     }
   };
   constexpr int kPerRow = S::kRow / S::kPiece;   // pieces of a row
   constexpr int kRowsPerLoad = 64 / kPerRow;     // rows that the wave loads at a time
-  const auto load_values = [&](int t0) {
+  const uint32_t val_at = lane / kPerRow * S::kRow + lane % kPerRow * S::kPiece;
+  const auto load_values = [&]() {
 #pragma unroll
-    for (int u = 0; u < S::kBlocks; ++u) {
-      const int t = min(t0 + 16 * u, last);
-      const uint8_t* p = c.v + first_row(t) * S::kRow + lane % kPerRow * S::kPiece;
+    for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
       for (int i = 0; i < S::kPieces; ++i) {
-        const int slot = min(i * kRowsPerLoad + lane / kPerRow, n - 1 - t);
+        const uint8_t* p = c.v + (row[u] + i * kRowsPerLoad) * S::kRow;
         if constexpr (S::kPiece < 16) {
-          const uint2 w = *reinterpret_cast<const uint2*>(p + slot * S::kRow);
-          val[u][i] = v4u{w.x, w.y, 0u, 0u};
+          const v2u w = load_at<v2u>(p, val_at);
+          val[u][i] = v4u{w[0], w[1], 0u, 0u};
         } else {
-          val[u][i] = *reinterpret_cast<const v4u*>(p + slot * S::kRow);
+          val[u][i] = load_at<v4u>(p, val_at);
         }
       }
-    }
   };
 
   int t0 = begin + wave * S::kTile;
   if (t0 < end) {
+    load_pages(t0 >> c.log_page);
     load_keys(t0);
-    load_values(t0);
+    load_values();
   }
   for (; t0 < end; t0 += kWaves * S::kTile) {
     const int next = t0 + kWaves * S::kTile;
-    // Logits, base 2.
+    // Logits, without the scale.
     float l[S::kBlocks][4];
-    bool live[S::kBlocks][4];
-    float top = -INFINITY;
-    float vscale[S::kBlocks][4];
+    v4u vscale[(S::kBlocks + 1) / 2];  // INT4: the tile's value scales, two to a dword
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u) {
       v4f s = {};
@@ -243,55 +396,117 @@ __global__ void __launch_bounds__(kThreads)
           k = __builtin_bit_cast(v8h, key[u][i]);
         s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i], s, 0, 0, 0);
       }
-      const int t = t0 + 16 * u + 4 * quarter;
-      uint32_t mask = 0x01010101u;
-      if (a.mask && t < end)  // four slots of one page: aligned, inside the row
-        mask = *reinterpret_cast<const uint32_t*>(a.mask + (size_t)b * c.capacity() + t);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        live[u][r] = t + r < end && ((mask >> (8 * r)) & 255u) != 0;
-        float x = s[r] * scale;
-        float ref = 0.0f;
-        if constexpr (kInt4) {
-          const uint32_t wk = r < 2 ? ks[u].x : ks[u].y, wv = r < 2 ? vs[u].x : vs[u].y;
-          x *= half_to_float((r & 1) ? wk >> 16 : wk & 0xFFFFu);
-          vscale[u][r] = half_to_float((r & 1) ? wv >> 16 : wv & 0xFFFFu);
-          ref = vscale[u][r] > 0.0f ? (float)__builtin_amdgcn_frexp_expf(vscale[u][r]) : -24.0f;
-        }
-        l[u][r] = live[u][r] ? x : -INFINITY;
-        top = fmaxf(top, l[u][r] + ref);
+        if constexpr (kInt4)
+          l[u][r] = __builtin_fmaf(
+              s[r], (float)__builtin_bit_cast(v2h, (uint32_t)ks[u][r / 2])[r & 1], 0.0f);
+        else
+          l[u][r] = s[r];
       }
-      if (plan.logits && t < end && col < rows)
-        *reinterpret_cast<float4*>(plan.logits + ((size_t)b * a.heads + head0 + col) *
-                                                     plan.ld_logits + t) =
-            make_float4(l[u][0], l[u][1], l[u][2], l[u][3]);
+      if constexpr (kInt4) {
+        vscale[u / 2][2 * (u & 1)] = vs[u][0];
+        vscale[u / 2][2 * (u & 1) + 1] = vs[u][1];
+      }
+    }
+    // Slots that take no part: a logit of -inf, a value scale of 0 (whatever was there).
+    bool live[S::kBlocks * 4];
+    if (kMask || t0 + S::kTile > end) {
+#pragma unroll
+      for (int u = 0; u < S::kBlocks; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const bool in = t0 + 16 * u + 4 * quarter + r < end &&
+                          (!kMask || ((mask[u] >> (8 * r)) & 255u) != 0);
+          live[4 * u + r] = in;
+          l[u][r] = in ? l[u][r] : -INFINITY;
+        }
+      if constexpr (kInt4) {
+#pragma unroll
+        for (int u = 0; u < S::kBlocks / 2; ++u)
+          vscale[u] = mask_halves(vscale[u], &live[8 * u]);
+      }
+    }
+    if (logits) {
+#pragma unroll
+      for (int u = 0; u < S::kBlocks; ++u)
+        if (t0 + 16 * u + 4 * quarter < end)
+          *reinterpret_cast<float4*>(logits + t0 + 16 * u) =
+              make_float4(l[u][0] * scale, l[u][1] * scale, l[u][2] * scale, l[u][3] * scale);
     }
     if (next < end) load_keys(next);
 
     // The running maximum of the column, over the quarters too.
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    if (__any(top > m)) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < S::kBlocks; ++u)
+      top = fmaxf(fmaxf(fmaxf(top, l[u][0]), fmaxf(l[u][1], l[u][2])), l[u][3]);
+    top = column_max(top) * scale;
+    if (__any(top > m + kSlack)) {
       const float up = fmaxf(m, top);
       const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
       m = up;
       sum *= shrink;
+      rounded *= shrink;
 #pragma unroll
       for (int j = 0; j < S::kOut; ++j) o[j] *= shrink;
     }
+    if constexpr (kInt4) {
+      // The power of two above the largest value scale so far, at least 2^-14 (its inverse is a
+      // float16 then; a smaller scale's values are below float16's normal range).
+      v2h big = __builtin_bit_cast(v2h, (uint32_t)vscale[0][0]);
+#pragma unroll
+      for (int u = 0; u < S::kBlocks / 2; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          big = __builtin_elementwise_max(big, __builtin_bit_cast(v2h, (uint32_t)vscale[u][i]));
+      const float largest = fmaxf((float)big[0], (float)big[1]);
+      if (__any(largest > vnorm)) {
+        const float all = column_max(largest);  // of the tile: the same in every column
+        const int e = __builtin_amdgcn_frexp_expf(all);
+        const float norm = __builtin_amdgcn_ldexpf(1.0f, min(e, 14));
+        if (norm > vnorm) {
+          const float shrink = vnorm / norm;  // powers of two
+          vnorm = norm;
+#pragma unroll
+          for (int j = 0; j < S::kOut; ++j) o[j] *= shrink;
+        }
+      }
+      const _Float16 inv = (_Float16)(1.0f / vnorm);
+#pragma unroll
+      for (int u = 0; u < S::kBlocks / 2; ++u)
+        vscale[u] = __builtin_bit_cast(
+            v4u, __builtin_bit_cast(v8h, vscale[u]) * v8h{inv, inv, inv, inv, inv, inv, inv, inv});
+    }
     const float base = m == -INFINITY ? 0.0f : m;
-    v8h p[S::kBlocks / 2];
+    _Float16 p[S::kBlocks * 4];
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float x = __builtin_amdgcn_exp2f(l[u][r] - base);
+        float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
         sum += x;
-        if constexpr (kInt4) x = live[u][r] ? x * vscale[u][r] : 0.0f;
-        p[u / 2][4 * (u & 1) + r] = (_Float16)x;
+        if constexpr (kInt4)
+          x *= (float)__builtin_bit_cast(v8h, vscale[u / 2])[4 * (u & 1) + r];
+        p[4 * u + r] = (_Float16)x;
       }
 
-    // Values through LDS; the wave's own tile, so no barrier.
+    if constexpr (!kInt4) {
+#pragma unroll
+      for (int i = 0; i < S::kBlocks * 2; ++i)
+        rounded = __builtin_amdgcn_fdot2(v2h{p[2 * i], p[2 * i + 1]},
+                                         v2h{(_Float16)1.0f, (_Float16)1.0f}, rounded, false);
+    }
+
+    // Values through LDS; the wave's own tile, so no barrier. Rows past the end: 0 times what they
+    // hold might not be 0 (INT4 codes are always finite).
+    if (!kInt4 && t0 + S::kTile > end) {
+#pragma unroll
+      for (int u = 0; u < S::kBlocks; ++u)
+#pragma unroll
+        for (int i = 0; i < S::kPieces; ++i)
+          if (t0 + 16 * u + i * kRowsPerLoad + lane / kPerRow >= end) val[u][i] = v4u{};
+    }
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
@@ -304,7 +519,7 @@ __global__ void __launch_bounds__(kThreads)
         else
           *reinterpret_cast<v4u*>(tile + S::at(t, piece)) = val[u][i];
       }
-    if (next < end) load_values(next);
+    if (next < end) load_values();
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int j = 0; j < S::kOut; ++j) {
@@ -316,100 +531,127 @@ __global__ void __launch_bounds__(kThreads)
         const int t = 32 * (col >> 3) + 16 * (s >> 2) + 4 * quarter + (s & 3);
         const v2i w = __builtin_amdgcn_ds_read_tr4_b64_v2i32(
             (lds_v2i)(tile + S::at(t, j >> 1) + 8 * (j & 1)));
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_codes((uint32_t)w[0]), p[0], o[j], 0,
-                                                      0, 0);
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(eight_codes((uint32_t)w[1]),
-                                                      p[S::kBlocks / 2 - 1], o[j], 0, 0, 0);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              eight_codes((uint32_t)w[h]),
+              v8h{p[8 * h], p[8 * h + 1], p[8 * h + 2], p[8 * h + 3], p[8 * h + 4], p[8 * h + 5],
+                  p[8 * h + 6], p[8 * h + 7]},
+              o[j], 0, 0, 0);
       } else {
         // Lanes 4 r .. 4 r + 3 of a quarter name row r: 16 channels of 4 slots.
-        v4s w[2];
+        v4s w[S::kBlocks];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
+        for (int u = 0; u < S::kBlocks; ++u) {
           const int t = 16 * u + 4 * quarter + (col >> 2);
           w[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
               (lds_v4s)(tile + S::at(t, 2 * j + ((col & 3) >> 1)) + 8 * (col & 1)));
+          if constexpr (kMask) w[u] = mask_halves(w[u], &live[4 * u]);  // 0 times what it holds
         }
-        v8h v = __builtin_bit_cast(
-            v8h, __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7));
-        if (a.mask) {  // 0 times what a masked row holds
-          const bool alive[8] = {live[0][0], live[0][1], live[0][2], live[0][3],
-                                 live[1][0], live[1][1], live[1][2], live[1][3]};
-          v = mask_halves(v, alive);
-        }
-        o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[0], o[j], 0, 0, 0);
+        if constexpr (S::kBlocks == 2)
+          o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              __builtin_bit_cast(v8h,
+                                 __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7)),
+              v8h{p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7]}, o[j], 0, 0, 0);
+        else
+          o[j] = __builtin_amdgcn_mfma_f32_16x16x16f16(
+              __builtin_bit_cast(v4h, w[0]), v4h{p[0], p[1], p[2], p[3]}, o[j], 0, 0, 0);
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
 
-  // The waves' sums meet in LDS.
+  // The waves' sums meet in LDS. o is put in proportion to sum: in units of vnorm (INT4), or from
+  // the sum of the rounded p, so that what rounding did to a weight it also did to the sum
+  // that divides it (one weight that outgrows all others is then exact).
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
+  float unit_o = vnorm;
+  if constexpr (!kInt4) {
+    rounded += __shfl_xor(rounded, 16);
+    rounded += __shfl_xor(rounded, 32);
+    unit_o = rounded > 0.0f ? sum / rounded : 0.0f;
+  }
+  if (quarter == 0) wave_stats[wave][col] = make_float2(m, sum);
+  __syncthreads();
+  float top = -INFINITY, total = 0.0f;  // of the column, over the waves
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_stats[w][col].x);
+  const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w)
+    total += wave_stats[w][col].y * __builtin_amdgcn_exp2f(wave_stats[w][col].x - base);
+  unit_o *= __builtin_amdgcn_exp2f(m - base);
+  if (whole) unit_o = total > 0.0f ? unit_o / total : 0.0f;
   float* mine = reinterpret_cast<float*>(tile);
 #pragma unroll
   for (int j = 0; j < S::kOut; ++j)
-    *reinterpret_cast<v4f*>(mine + col * S::kLdO + 16 * j + 4 * quarter) = o[j];
-  if (quarter == 0) wave_stats[wave][col] = make_float2(m, sum);
+    *reinterpret_cast<v4f*>(mine + col * S::kLdO + 16 * j + 4 * quarter) = o[j] * unit_o;
+  if (threadIdx.x < rows) {
+    const size_t bh = (size_t)b * a.heads + head0 + threadIdx.x;
+    if (whole && a.lse)
+      a.lse[bh] = total > 0.0f ? (top + __builtin_amdgcn_logf(total)) / kLog2e : -INFINITY;
+    if (plan.stats) plan.stats[(size_t)piece.index * a.heads + head0 + threadIdx.x] = make_float2(top, total);
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < rows * D; i += kThreads) {
-    const int r = i / D, d = i % D;
-    float top = wave_stats[0][r].x;
+  for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {
+    const int r = i / (D / 4), d = 4 * (i % (D / 4));
+    v4f acc = {};
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, wave_stats[w][r].x);
-    float acc = 0.0f, total = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float2 st = wave_stats[w][r];
-      const float f = st.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(st.x - top);
-      acc += f * reinterpret_cast<const float*>(lds + w * S::kLds)[r * S::kLdO + d];
-      total += f * st.y;
-    }
+    for (int w = 0; w < kWaves; ++w)
+      acc += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds + w * S::kLds) +
+                                           r * S::kLdO + d);
     const size_t bh = (size_t)b * a.heads + head0 + r;
-    if (whole) {
-      const float x = total > 0.0f ? acc / total : 0.0f;
-      a.out[bh * D + d] = __builtin_bit_cast(uint16_t, (_Float16)x);
-      if (d == 0 && a.lse)
-        a.lse[bh] = total > 0.0f ? (top + __builtin_amdgcn_logf(total)) / kLog2e : -INFINITY;
-    } else {
-      plan.part[(bh * plan.chunks + chunk) * D + d] = acc;
-    }
-    if (d == 0 && plan.stats) plan.stats[bh * plan.chunks + chunk] = make_float2(top, total);
+    if (whole)
+      *reinterpret_cast<v4h*>(a.out + bh * D + d) =
+          v4h{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
+    else
+      *reinterpret_cast<v4f*>(plan.part +
+                              ((size_t)piece.index * a.heads + head0 + r) * D + d) = acc;
   }
 }
 
-// The common maximum of a head's chunks and the sum relative to it.
-__device__ __forceinline__ float2 join_stats(const float2* stats, int chunks) {
+// The common maximum of a head's pieces and the sum relative to it, by a whole wave. stats: the
+// head's first piece; `heads` apart.
+__device__ __forceinline__ float2 join_stats(const float2* stats, int count, int heads) {
+  const int lane = threadIdx.x & 63;
   float top = -INFINITY, total = 0.0f;
-  for (int i = 0; i < chunks; ++i) top = fmaxf(top, stats[i].x);
-  for (int i = 0; i < chunks; ++i)
-    if (stats[i].x > -INFINITY) total += stats[i].y * __builtin_amdgcn_exp2f(stats[i].x - top);
+  for (int i = lane; i < count; i += 64) top = fmaxf(top, stats[(size_t)i * heads].x);
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (top == -INFINITY) return make_float2(top, 0.0f);
+  for (int i = lane; i < count; i += 64) {
+    const float2 st = stats[(size_t)i * heads];
+    total += st.y * __builtin_amdgcn_exp2f(st.x - top);
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
   return make_float2(top, total);
 }
 
-// The first sequences x heads workgroups join the chunks of one head each (those of more than one
-// chunk); the others turn the logits of 1024 slots of a (sequence, KV head) into weights.
+// The first `joins` workgroups join the pieces of one head each (of sequences of more than one
+// piece); the others turn the logits of 1024 slots of a (sequence, KV head) into weights.
 template <int D>
 __global__ void __launch_bounds__(kThreads)
-    attention_join_kernel(AttentionArgs a, KvView c, Plan plan, int weight_blocks) {
-  constexpr int kParts = kThreads / (D / 4);  // chunks read at a time, 4 channels per thread
+    attention_join_kernel(AttentionArgs a, KvView c, Plan plan, int joins, int weight_blocks) {
+  constexpr int kParts = kThreads / (D / 4);  // pieces read at a time, 4 channels per thread
   __shared__ float4 acc_of[kThreads];
   __shared__ float top_of[kThreads], inv_of[kThreads];
-  const int joins = plan.chunks > 1 ? c.sequences * a.heads : 0;
   if ((int)blockIdx.x < joins) {
-    const int bh = blockIdx.x, b = bh / a.heads;
-    const int n = min(a.lengths[b], a.max_length);
-    if (n <= plan.chunk) return;
-    const int chunks = (n - 1) / plan.chunk + 1;
-    const float2* stats = plan.stats + (size_t)bh * plan.chunks;
-    const float2 all = join_stats(stats, chunks);
+    const int bh = blockIdx.x, b = bh / a.heads, h = bh % a.heads;
+    const int2 at = plan.of_seq[b];  // first piece, pieces
+    if (at.y == 1) return;
+    const float2* stats = plan.stats + (size_t)at.x * a.heads + h;
+    const float2 all = join_stats(stats, at.y, a.heads);
     const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
-    const float4* src = reinterpret_cast<const float4*>(plan.part + (size_t)bh * plan.chunks * D);
+    const float4* src = reinterpret_cast<const float4*>(
+        plan.part + ((size_t)at.x * a.heads + h) * D);
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int i = part; i < chunks; i += kParts) {
-      const float m = stats[i].x;
-      if (m == -INFINITY) continue;
-      const float f = __builtin_amdgcn_exp2f(m - all.x);
-      const float4 x = src[(size_t)i * (D / 4) + d4];
+    const float base = all.x == -INFINITY ? 0.0f : all.x;
+#pragma unroll 4
+    for (int i = part; i < at.y; i += kParts) {
+      const float f = __builtin_amdgcn_exp2f(stats[(size_t)i * a.heads].x - base);
+      const float4 x = src[(size_t)i * a.heads * (D / 4) + d4];
       acc.x += f * x.x;
       acc.y += f * x.y;
       acc.z += f * x.z;
@@ -427,12 +669,10 @@ __global__ void __launch_bounds__(kThreads)
     }
     const bool some = all.y > 0.0f;
     const float v[4] = {acc.x, acc.y, acc.z, acc.w};
-    uint16_t h[4];
+    v4h y;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      h[i] = __builtin_bit_cast(uint16_t, (_Float16)(some ? v[i] / all.y : 0.0f));
-    *reinterpret_cast<uint2*>(a.out + (size_t)bh * D + 4 * d4) =
-        make_uint2(h[0] | ((uint32_t)h[1] << 16), h[2] | ((uint32_t)h[3] << 16));
+    for (int i = 0; i < 4; ++i) y[i] = (_Float16)(some ? v[i] / all.y : 0.0f);
+    *reinterpret_cast<v4h*>(a.out + (size_t)bh * D + 4 * d4) = y;
     if (d4 == 0 && a.lse)
       a.lse[bh] = some ? (all.x + __builtin_amdgcn_logf(all.y)) / kLog2e : -INFINITY;
     return;
@@ -442,17 +682,18 @@ __global__ void __launch_bounds__(kThreads)
   const int n = min(a.lengths[b], a.max_length);
   const int s0 = id % weight_blocks * (4 * kThreads);
   if (s0 >= n) return;
-  const int chunks = (n - 1) / plan.chunk + 1;
+  const int2 at = plan.of_seq[b];
   const int s = s0 + 4 * threadIdx.x;
   float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
   for (int g0 = 0; g0 < plan.group; g0 += kThreads) {
     const int heads = min(plan.group - g0, kThreads);
     const size_t bh0 = (size_t)b * a.heads + hk * plan.group + g0;
     __syncthreads();
-    if ((int)threadIdx.x < heads) {
-      const float2 all = join_stats(plan.stats + (bh0 + threadIdx.x) * plan.chunks, chunks);
-      top_of[threadIdx.x] = all.x;
-      inv_of[threadIdx.x] = all.y > 0.0f ? 1.0f / all.y : 0.0f;
+    for (int g = threadIdx.x >> 6; g < heads; g += kWaves) {
+      const float2 all = join_stats(
+          plan.stats + (size_t)at.x * a.heads + hk * plan.group + g0 + g, at.y, a.heads);
+      top_of[g] = all.x;
+      inv_of[g] = all.y > 0.0f ? 1.0f / all.y : 0.0f;
     }
     __syncthreads();
     if (s < n)
@@ -477,51 +718,73 @@ __global__ void __launch_bounds__(kThreads)
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Chunks: enough workgroups for the card (256 compute units, three workgroups each) a few times
-// over, since sequences are shorter than the longest; at least two tiles per wave.
+// Pieces of the sequences, in numbers that a launch may reach.
+long long max_pieces(const Plan& p, const KvView& c, int max_length) {
+  if (p.target == 0) return (long long)c.sequences * p.pieces;
+  const long long steps = (max_length - 1) / p.step + 1;
+  const long long most = (long long)c.sequences * ((steps - 1) / p.steps + 1);
+  const long long share = (long long)c.heads * p.row_blocks;
+  const long long want = p.target > share ? p.target / share : 1;
+  return most < want + c.sequences ? most : want + c.sequences;
+}
+
 Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, void* workspace,
                size_t* bytes) {
   Plan p{};
   p.group = heads / c.heads;
   p.row_blocks = (p.group + kRows - 1) / kRows;
-  const long long units = (long long)c.sequences * c.heads * p.row_blocks;
-  const int step = kWaves * (c.int4() ? 64 : 32);
-  long long chunk = ((long long)max_length * units / 1536 + step - 1) / step * step;
-  if (chunk < 2 * step) chunk = 2 * step;
-  if (chunk > max_length) chunk = ((long long)max_length + step - 1) / step * step;
-  p.chunk = (int)(chunk < (1 << 30) ? chunk : 1 << 30);
-  p.chunks = (max_length - 1) / p.chunk + 1;
+  const long long share = (long long)c.heads * p.row_blocks;
+  p.step = kWaves * (c.int4() ? 64 : c.dim == 256 ? 16 : 32);
+  // Workgroups that run at the same time where cutting every sequence gives no more; else four
+  // times as many, not too short, so that those that end last are a small part of the whole.
+  const int resident = 256 * (c.dim == 256 ? 2 : 3);
+  const bool one_round = c.sequences * share <= resident;
+  p.target = one_round ? resident : 4 * resident;
+  p.steps = one_round ? 2 : 8;
+  const long long steps = (max_length - 1) / p.step + 1;
+  if (c.sequences > kWidest || steps <= p.steps) {  // many balance each other; or nothing to cut
+    p.target = 0;
+    long long q = steps * c.sequences * share / (4 * resident);
+    q = q < p.steps ? p.steps : q;
+    p.steps = (int)(q < steps ? q : steps);
+    p.pieces = (int)((steps - 1) / p.steps + 1);
+  }
   p.ld_logits = (max_length + 15) & ~15;
-  const size_t bh = (size_t)c.sequences * heads;
-  const size_t stats = p.chunks > 1 || with_weights ? align256(bh * p.chunks * 8) : 0;
-  const size_t part = p.chunks > 1 ? align256(bh * p.chunks * c.dim * 4) : 0;
-  const size_t logits = with_weights ? align256(bh * (size_t)p.ld_logits * 4) : 0;
-  *bytes = stats + part + logits;
-  uint8_t* ws = static_cast<uint8_t*>(workspace);
-  if (ws) {
-    if (stats) p.stats = reinterpret_cast<float2*>(ws);
-    if (part) p.part = reinterpret_cast<float*>(ws + stats);
-    if (logits) p.logits = reinterpret_cast<float*>(ws + stats + part);
+  const size_t pieces = (size_t)max_pieces(p, c, max_length);
+  const bool joined = pieces > (size_t)c.sequences;
+  const size_t of_seq = joined || with_weights ? align256((size_t)c.sequences * 8) : 0;
+  const size_t stats = joined || with_weights ? align256(pieces * heads * 8) : 0;
+  const size_t part = joined ? align256(pieces * heads * c.dim * 4) : 0;
+  const size_t logits =
+      with_weights ? align256((size_t)c.sequences * heads * (size_t)p.ld_logits * 4) : 0;
+  *bytes = of_seq + stats + part + logits;
+  if (uint8_t* ws = static_cast<uint8_t*>(workspace)) {
+    if (of_seq) p.of_seq = reinterpret_cast<int2*>(ws);
+    if (stats) p.stats = reinterpret_cast<float2*>(ws + of_seq);
+    if (part) p.part = reinterpret_cast<float*>(ws + of_seq + stats);
+    if (logits) p.logits = reinterpret_cast<float*>(ws + of_seq + stats + part);
   }
   return p;
 }
 
 template <int D>
 hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
-  const long long units = (long long)c.sequences * c.heads * p.chunks;
+  const long long pieces = max_pieces(p, c, a.max_length);
+  const long long units = pieces * c.heads;
   const long long grid = p.row_blocks == 1 ? units : (units + 7) / 8 * 8 * p.row_blocks;
   if (grid >= (1ll << 31)) return hipErrorInvalidValue;
+  const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p); };
   if (c.int4())
-    attention_kernel<D, true><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p);
+    a.mask ? run(attention_kernel<D, true, true>) : run(attention_kernel<D, true, false>);
   else
-    attention_kernel<D, false><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p);
+    a.mask ? run(attention_kernel<D, false, true>) : run(attention_kernel<D, false, false>);
   if (hipError_t e = hipGetLastError()) return e;
   const int blocks = p.logits ? (a.max_length - 1) / (4 * kThreads) + 1 : 0;
-  const long long joins = (p.chunks > 1 ? (long long)c.sequences * a.heads : 0) +
-                          (long long)blocks * c.sequences * c.heads;
-  if (joins >= (1ll << 31)) return hipErrorInvalidValue;
-  if (joins > 0)
-    attention_join_kernel<D><<<(unsigned)joins, kThreads, 0, stream>>>(a, c, p, blocks);
+  const int joins = p.part ? c.sequences * a.heads : 0;
+  const long long wgs = joins + (long long)blocks * c.sequences * c.heads;
+  if (wgs >= (1ll << 31)) return hipErrorInvalidValue;
+  if (wgs > 0)
+    attention_join_kernel<D><<<(unsigned)wgs, kThreads, 0, stream>>>(a, c, p, joins, blocks);
   return hipGetLastError();
 }
 

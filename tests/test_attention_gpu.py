@@ -89,6 +89,18 @@ def test_mask(D, share, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("B,top,hk", [(1, 9000, 1), (70, 3000, 1), (200, 1500, 5), (256, 2500, 1),
+                                      (257, 700, 1), (300, 2500, 1)])
+def test_many_sequences(B, top, hk, fmt):
+    """Ragged batches on both sides of the limits at which lengths are cut into pieces."""
+    gen = torch.Generator().manual_seed(B)
+    lengths = torch.randint(0, 60, (B,), generator=gen).tolist()
+    for at in (0, B // 2, B - 1):   # a few long ones, at the ends of the batch too
+        lengths[at] = top - at % 7
+    _run(lengths, 2 * hk, hk, 64, 64, fmt, max_length=top, with_weights=True, seed=7)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
 def test_sharp_and_flat(fmt):
     """Logits in the hundreds (one slot takes all), and all of them equal."""
     _run([513, 64, 2000], 8, 2, 128, 32, fmt, sharp=40.0, with_weights=True, seed=6)
