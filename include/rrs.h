@@ -675,12 +675,15 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
  *   new_lengths           out : sequences int32, min(n, budget).
  *   weights_out, pos_out  out : as weights and slot_pos, of the moved slots; 0 and -1 from
  *                               new_lengths[b] on. They must not overlap the inputs.
+ *   workspace                 : at least rrs_kv_evict_workspace_bytes (0 up to 16384 slots: may
+ *                               be NULL); contents ignored.
  * k, v and the scales are moved in place. Pages past the new length are the caller's to reuse.
  */
+size_t rrs_kv_evict_workspace_bytes(const rrs_kv_cache* cache, int max_length, int budget);
 rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int max_length,
                         const float* weights, const int32_t* slot_pos, const int32_t* keep_from,
                         int budget, int32_t* kept, int32_t* new_lengths, float* weights_out,
-                        int32_t* pos_out, void* stream);
+                        int32_t* pos_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * The cached values as float16: K and V, each sequences x kv_heads x max_length x

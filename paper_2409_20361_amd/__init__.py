@@ -53,6 +53,7 @@ from ._kv import (  # noqa: F401
     KVCache,
     kv_cache,
     kv_evict,
+    kv_evict_workspace_bytes,
     kv_read,
     paged_attention,
     paged_attention_workspace_bytes,
@@ -61,7 +62,8 @@ from ._kv import (  # noqa: F401
 )
 
 __all__ = [
-    "KV_F16", "KV_INT4", "KVCache", "kv_cache", "kv_evict", "kv_read", "paged_attention",
+    "KV_F16", "KV_INT4", "KVCache", "kv_cache", "kv_evict", "kv_evict_workspace_bytes",
+    "kv_read", "paged_attention",
     "paged_attention_workspace_bytes", "rope_kv_append", "rope_table",
     "REORDER_BLOCK", "SCHEME_PER_CHANNEL", "SCHEME_RUNTIME_SMOOTH", "SCHEME_SUB_CHANNEL",
     "SKIP_ROTATION", "SKIP_SMOOTHING", "WEIGHT_TILED", "RRSError", "gemm_path", "gemm_scratch_bytes", "lib", "lib_path", "linear", "linear_noalloc", "linear_reorder",

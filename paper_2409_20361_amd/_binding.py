@@ -69,7 +69,9 @@ _SIGNATURES = {
     "rrs_paged_attention_workspace_bytes": (_sz, [_vp, _i, _i, _i]),
     "rrs_paged_attention": (ctypes.c_int32, [_vp, _i, _vp, _vp, _i, _f, _vp, _vp, _vp, _vp, _vp,
                                              _sz, _vp]),
-    "rrs_kv_evict": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp]),
+    "rrs_kv_evict": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp,
+                                      _sz, _vp]),
+    "rrs_kv_evict_workspace_bytes": (_sz, [_vp, _i, _i]),
     "rrs_kv_read": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp]),
 }
 

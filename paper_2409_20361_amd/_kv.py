@@ -71,6 +71,15 @@ def _kv(cache: KVCache):
             B, per_seq * P)
 
 
+def _workspace(t: Optional[torch.Tensor], device: torch.device):
+    """Pointer and bytes of a workspace (None: none)."""
+    if t is None:
+        return None, 0
+    if t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {device}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def kv_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, table: torch.Tensor,
              format: int = KV_F16) -> KVCache:
     """An empty cache of one layer on the table's device."""
@@ -179,19 +188,20 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, lengths: torch.Tensor,
         need = lib().rrs_paged_attention_workspace_bytes(ref, heads, max_length, wp is not None)
         if need:
             workspace = torch.empty((need,), dtype=torch.uint8, device=Q.device)
-    elif workspace.device != Q.device or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous and on {Q.device}")
-    wsp, wsb = (None, 0) if workspace is None else (
-        workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    wsp, wsb = _workspace(workspace, Q.device)
     _check(lib().rrs_paged_attention(qp, heads, ref, lp, max_length, scale, mp, wp, yp,
                                      None if lse is None else lse.data_ptr(), wsp, wsb,
                                      _stream(Q.device)), "rrs_paged_attention")
     return Y if lse is None else (Y, lse)
 
 
+def kv_evict_workspace_bytes(cache: KVCache, max_length: int, budget: int) -> int:
+    return lib().rrs_kv_evict_workspace_bytes(ctypes.byref(_kv(cache)[0]), max_length, budget)
+
+
 def kv_evict(cache: KVCache, lengths: torch.Tensor, weights: torch.Tensor, slot_pos: torch.Tensor,
-             keep_from: torch.Tensor, budget: int, max_length: Optional[int] = None, out=None
-             ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+             keep_from: torch.Tensor, budget: int, max_length: Optional[int] = None, out=None,
+             workspace: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
     """Brings every sequence down to its `budget` slots of largest weight, in place.
 
     weights, slot_pos: (sequences, KV heads, capacity) float32 / int32; keep_from: (sequences,)
@@ -220,8 +230,14 @@ def kv_evict(cache: KVCache, lengths: torch.Tensor, weights: torch.Tensor, slot_
     p2p = _dev(p2, "pos_out", torch.int32, (B, hk, capacity))
     if w2p == wp or p2p == pp or np_ == lp:
         raise ValueError("kv_evict: outputs must not be inputs")
-    _check(lib().rrs_kv_evict(ctypes.byref(st), lp, max_length, wp, pp, fp, budget, kp, np_, w2p,
-                              p2p, _stream(lengths.device)), "rrs_kv_evict")
+    ref = ctypes.byref(st)
+    if workspace is None:
+        need = lib().rrs_kv_evict_workspace_bytes(ref, max_length, budget)
+        if need:
+            workspace = torch.empty((need,), dtype=torch.uint8, device=lengths.device)
+    wsp, wsb = _workspace(workspace, lengths.device)
+    _check(lib().rrs_kv_evict(ref, lp, max_length, wp, pp, fp, budget, kp, np_, w2p, p2p, wsp, wsb,
+                              _stream(lengths.device)), "rrs_kv_evict")
     return kept, new, w2, p2
 
 

@@ -38,7 +38,6 @@ typedef float v4f __attribute__((ext_vector_type(4)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef int v2i __attribute__((ext_vector_type(2)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s;
 typedef __attribute__((address_space(3))) v2i* lds_v2i;
 
@@ -70,20 +69,6 @@ struct Plan {
 struct Piece {
   int b, n, begin, end, index, count, first;
 };
-
-// Inclusive prefix sums over the wave; the last lane holds the total.
-__device__ __forceinline__ int wave_prefix(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1 lane below in the row
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);  // 2
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);  // 4
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);  // 8
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // rows 0, 2 into 1, 3
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // the lower half's total
-  return x;
-}
-__device__ __forceinline__ int wave_total(int x) {
-  return __builtin_amdgcn_readlane(wave_prefix(x), 63);
-}
 
 // Which piece `index` is; false past the last. Every wave of every workgroup works this out for
 // itself from the lengths, so that sequences of any lengths are cut into pieces of about the same

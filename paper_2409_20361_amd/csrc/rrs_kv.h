@@ -95,11 +95,28 @@ struct EvictArgs {
   float* weights_out;
   int32_t* pos_out;
 };
-hipError_t launch_kv_evict(const EvictArgs& a, const KvView& c, hipStream_t stream);
+size_t evict_workspace_bytes(const KvView& c, int max_length, int budget);
+hipError_t launch_kv_evict(const EvictArgs& a, const KvView& c, void* workspace,
+                           hipStream_t stream);
+
+// Inclusive prefix sums over the wave; the last lane holds the total.
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1 lane below in the row
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);  // 2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);  // 4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);  // 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);  // rows 0, 2 into 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);  // the lower half's total
+  return x;
+}
+__device__ __forceinline__ int wave_total(int x) {
+  return __builtin_amdgcn_readlane(wave_prefix(x), 63);
+}
 
 // 8 packed codes (low nibble first) as float16 of q s, s a float16 scale.
-__device__ __forceinline__ uint4 dequant8(uint32_t codes, float s) {
-  uint32_t w[4];
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ v4u dequant8(uint32_t codes, float s) {
+  v4u w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const _Float16 lo = (_Float16)((float)((int)(codes << (28 - 8 * i)) >> 28) * s);
@@ -107,7 +124,7 @@ __device__ __forceinline__ uint4 dequant8(uint32_t codes, float s) {
     w[i] = (uint32_t)__builtin_bit_cast(uint16_t, lo) |
            ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
   }
-  return make_uint4(w[0], w[1], w[2], w[3]);
+  return w;
 }
 
 }  // namespace rrs

@@ -251,10 +251,17 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
   return from_hip(rrs::launch_paged_attention(a, view(c), static_cast<hipStream_t>(stream)));
 }
 
+size_t rrs_kv_evict_workspace_bytes(const rrs_kv_cache* cache, int max_length, int budget) {
+  if (!cache || !valid_shape(*cache) || !valid_format(*cache) || max_length < 1 ||
+      max_length > capacity(*cache) || budget < 1 || budget > capacity(*cache))
+    return 0;
+  return rrs::evict_workspace_bytes(view(*cache), max_length, budget);
+}
+
 rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int max_length,
                         const float* weights, const int32_t* slot_pos, const int32_t* keep_from,
                         int budget, int32_t* kept, int32_t* new_lengths, float* weights_out,
-                        int32_t* pos_out, void* stream) {
+                        int32_t* pos_out, void* workspace, size_t workspace_bytes, void* stream) {
   if (debug_enabled()) debug_print("kv_evict", cache);
   if (!lengths || !weights || !slot_pos || !keep_from || !kept || !new_lengths || !weights_out ||
       !pos_out || any_null(cache))
@@ -264,16 +271,19 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
       budget > capacity(c))
     return RRS_ERR_SHAPE;
   if (!valid_format(c)) return RRS_ERR_FLAGS;
-  if (!aligned(c) || !is_aligned(lengths) || !is_aligned(weights) || !is_aligned(slot_pos) ||
+  const size_t need = rrs::evict_workspace_bytes(view(c), max_length, budget);
+  if (need > 0 && !workspace) return RRS_ERR_NULL;
+  if (!aligned(c) || !is_aligned(workspace) || !is_aligned(lengths) || !is_aligned(weights) || !is_aligned(slot_pos) ||
       !is_aligned(keep_from) || !is_aligned(kept) || !is_aligned(new_lengths) ||
       !is_aligned(weights_out) || !is_aligned(pos_out))
     return RRS_ERR_ALIGN;
+  if (workspace_bytes < need) return RRS_ERR_WORKSPACE;
   if (rrs_status s = check_device()) return s;
   if (debug_enabled())
     if (rrs_status s = debug_check_lengths(c, lengths, max_length, stream)) return s;
   const rrs::EvictArgs a{lengths, max_length, weights,     slot_pos,    keep_from,
                          budget,  kept,       new_lengths, weights_out, pos_out};
-  return from_hip(rrs::launch_kv_evict(a, view(c), static_cast<hipStream_t>(stream)));
+  return from_hip(rrs::launch_kv_evict(a, view(c), workspace, static_cast<hipStream_t>(stream)));
 }
 
 rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int max_length, void* K,

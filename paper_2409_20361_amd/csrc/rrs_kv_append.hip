@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads)
   if (t >= max_length) return;
   const int b = bh / c.heads, h = bh % c.heads;
   const int i = threadIdx.x % kLanes;
-  uint4 k = make_uint4(0, 0, 0, 0), v = k;
+  v4u k = {}, v = {};
   if (t < lengths[b]) {
     const size_t row = c.row_of(b, h, t);
     if constexpr (kInt4) {
@@ -192,13 +192,13 @@ __global__ void __launch_bounds__(kThreads)
       k = dequant8(reinterpret_cast<const uint32_t*>(c.k + row * (D / 2))[i], ks);
       v = dequant8(reinterpret_cast<const uint32_t*>(c.v + row * (D / 2))[i], vs);
     } else {
-      k = reinterpret_cast<const uint4*>(c.k + row * (2 * D))[i];
-      v = reinterpret_cast<const uint4*>(c.v + row * (2 * D))[i];
+      k = reinterpret_cast<const v4u*>(c.k + row * (2 * D))[i];
+      v = reinterpret_cast<const v4u*>(c.v + row * (2 * D))[i];
     }
   }
   const size_t out = ((size_t)bh * max_length + t) * D + 8 * i;
-  *reinterpret_cast<uint4*>(K + out) = k;
-  *reinterpret_cast<uint4*>(V + out) = v;
+  __builtin_nontemporal_store(k, reinterpret_cast<v4u*>(K + out));
+  __builtin_nontemporal_store(v, reinterpret_cast<v4u*>(V + out));
 }
 
 template <int D>

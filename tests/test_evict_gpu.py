@@ -93,6 +93,28 @@ def test_long(n, budget):
     _check(cache, [n], w, pos, [n - 50], budget)
 
 
+@pytest.mark.parametrize("kind", ["random", "ties", "equal", "odd"])
+@pytest.mark.parametrize("budget", [1, 8191, 8192, 8193, 20000, 24999])
+def test_long_ragged(budget, kind):
+    """Rows of several segments, of one, and of none, with ties across the segments' borders."""
+    gen = torch.Generator().manual_seed(budget)
+    lengths = [25000, 8192, 16385, 0, 24577]
+    cache = make_cache(gen, len(lengths), 25000, 1, 64, 256, "int4")
+    w, pos = _state(gen, len(lengths), 1, cache.capacity, kind)
+    _check(cache, lengths, w, pos, [24900, 10 ** 6, 0, 0, 20000], budget, 25000)
+
+
+@pytest.mark.parametrize("n,budget", [(16384, 9000), (16385, 9000), (4096, 4000), (4097, 64),
+                                      (1024, 1020), (2000, 64), (2000, 65)])
+def test_sides_of_the_kernels(n, budget):
+    """Lengths and numbers of moves around those at which another kernel takes over."""
+    gen = torch.Generator().manual_seed(n + budget)
+    for fmt, D in (("f16", 256), ("int4", 64)):
+        cache = make_cache(gen, 2, n, 2, D, 64, fmt)
+        w, pos = _state(gen, 2, 2, cache.capacity, "ties")
+        _check(cache, [n, n // 3], w, pos, [n - 9, 3], budget, n)
+
+
 def test_bound_of_the_lengths():
     gen = torch.Generator().manual_seed(5)
     cache = make_cache(gen, 3, 300, 2, 64, 16, "f16")
@@ -143,6 +165,12 @@ def test_refusals():
         rrs.kv_evict(cache, n, w.double(), pos, keep, 8)
     with pytest.raises(ValueError):
         rrs.kv_evict(cache, n, w[:, :1], pos, keep, 8)
+    long = make_cache(gen, 1, 20000, 1, 64, 256, "int4")
+    w2, pos2 = _state(gen, 1, 1, long.capacity)
+    need = rrs.kv_evict_workspace_bytes(long, 20000, 9)
+    with pytest.raises(rrs.RRSError, match="WORKSPACE"):
+        rrs.kv_evict(long, n[:1], w2, pos2, keep[:1], 9, 20000,
+                     workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
     out = rrs.kv_evict(cache, n, w, pos, keep, 8)
     with pytest.raises(ValueError):
         rrs.kv_evict(cache, n, w, pos, keep, 8, out=(out[0], out[1], w, out[3]))

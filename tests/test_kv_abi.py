@@ -51,7 +51,7 @@ def _attend(cache=None, **kw):
 
 def _evict(cache=None, **kw):
     a = dict(cache=ctypes.byref(cache or _cache()), lengths=P, top=80, w=P, pos=P, keep=P,
-             budget=7, kept=P, new=P, w2=P, pos2=P)
+             budget=7, kept=P, new=P, w2=P, pos2=P, ws=None, bytes=0)
     a.update(kw)
     return rrs.lib().rrs_kv_evict(*a.values(), None)
 
@@ -121,6 +121,20 @@ def test_attend_workspace():
 ])
 def test_evict(kw, want):
     assert _evict(**kw) == want
+
+
+def test_evict_workspace():
+    q = rrs.lib().rrs_kv_evict_workspace_bytes
+    assert q(ctypes.byref(_cache()), 80, 7) == 0   # few slots: none
+    c = _cache(max_pages=2000)
+    assert q(ctypes.byref(c), 16384, 7) == 0
+    need = q(ctypes.byref(c), 20000, 7)
+    assert need > 0
+    assert _evict(c, top=20000, ws=None, bytes=need) == NULL
+    assert _evict(c, top=20000, ws=MIS, bytes=need) == ALIGN
+    assert _evict(c, top=20000, ws=P, bytes=need - 1) == WS
+    for top, budget in ((0, 7), (32001, 7), (20000, 0), (20000, 32001)):
+        assert q(ctypes.byref(c), top, budget) == 0
 
 
 @pytest.mark.parametrize("kw,want", [
