@@ -26,6 +26,15 @@ __device__ __forceinline__ uint4 pack_halves(const float (&v)[8]) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+__device__ __forceinline__ void unpack_halves(const uint4& w, float (&v)[8]) {
+  const uint32_t d[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = half_to_float(d[i] & 0xFFFFu);
+    v[2 * i + 1] = half_to_float(d[i] >> 16);
+  }
+}
+
 __device__ __forceinline__ float max_abs(const float (&v)[8]) {
   float m = 0.0f;
 #pragma unroll
@@ -65,6 +74,19 @@ __global__ void __launch_bounds__(kThreads) rope_kv_append_kernel(RopeArgs a, Kv
     o0 = 8 * i;
     o1 = F + 8 * i;
   }
+  // The first row is on its way while positions, cosines and the token's place are looked up.
+  const int total = a.heads + 2 * c.heads;
+  const uint16_t* src = a.qkv + (size_t)m * a.row_stride;
+  const int step = kHeads * gridDim.y;
+  int h = blockIdx.y * kHeads + threadIdx.x / kLanes;
+  uint4 x_next = make_uint4(0, 0, 0, 0), y_next = x_next;
+  const auto load = [&](int head) {
+    if (head >= total) return;
+    x_next = *reinterpret_cast<const uint4*>(src + (size_t)head * D + o0);
+    y_next = *reinterpret_cast<const uint4*>(src + (size_t)head * D + o1);
+  };
+  load(h);
+
   float cs[8], sn[8];
   if (turns) {
     int p[4];
@@ -73,14 +95,17 @@ __global__ void __launch_bounds__(kThreads) rope_kv_append_kernel(RopeArgs a, Kv
       p[x] = x < a.axes ? a.positions[(size_t)m * a.axes + x] : 0;
       p[x] = min(max(p[x], 0), a.rope_rows - 1);
     }
+    const auto axis = [&](int j) {
+      return (j >= a.bound[0]) + (j >= a.bound[1]) + (j >= a.bound[2]);
+    };
     const auto position = [&](int j) {
-      return j < a.bound[0] ? p[0] : j < a.bound[1] ? p[1] : j < a.bound[2] ? p[2] : p[3];
+      const int x = axis(j);
+      return x == 0 ? p[0] : x == 1 ? p[1] : x == 2 ? p[2] : p[3];
     };
     const int j0 = 8 * i;
-    if (position(j0) == position(j0 + 7) && position(j0 + 3) == position(j0) &&
-        a.axes == 1) {
+    if (axis(j0) == axis(j0 + 7)) {  // of one axis: neighbours in its row
       const float4* row =
-          reinterpret_cast<const float4*>(a.rope + (size_t)p[0] * a.rotary_dim + j0);
+          reinterpret_cast<const float4*>(a.rope + (size_t)position(j0) * a.rotary_dim + j0);
       const float4 c0 = row[0], c1 = row[1], s0 = row[F / 4], s1 = row[F / 4 + 1];
       const float cc[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
       const float ss[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
@@ -110,17 +135,15 @@ __global__ void __launch_bounds__(kThreads) rope_kv_append_kernel(RopeArgs a, Kv
       if (a.slot_pos) a.slot_pos[at] = a.positions[(size_t)m * a.axes];
     }
 
-  const int total = a.heads + 2 * c.heads;
-  const uint16_t* src = a.qkv + (size_t)m * a.row_stride;
-  for (int h = blockIdx.y * kHeads + threadIdx.x / kLanes; h < total;
-       h += kHeads * gridDim.y) {
+  for (; h < total; h += step) {
     const bool query = h < a.heads;
     const bool value = h >= a.heads + c.heads;
+    uint4 xo = x_next, yo = y_next;
+    load(h + step);
     if (!query && !stored) continue;
     float x[8], y[8];
-    load_halves<8>(src + (size_t)h * D + o0, x);
-    load_halves<8>(src + (size_t)h * D + o1, y);
-    uint4 xo = pack_halves(x), yo = pack_halves(y);
+    unpack_halves(xo, x);
+    unpack_halves(yo, y);
     if (turns && !value) {
       if (a.interleaved) {
 #pragma unroll
@@ -206,7 +229,7 @@ hipError_t append(const RopeArgs& a, const KvView& c, hipStream_t stream) {
   const int per_pass = kThreads / (D / 16);
   const int passes = (a.heads + 2 * c.heads + per_pass - 1) / per_pass;
   // Few tokens: a workgroup per pass, so that all rows are in flight at once.
-  const dim3 grid(a.M, a.M < 512 && passes <= 65535 ? passes : 1);
+  const dim3 grid(a.M, a.M < 2048 && passes <= 65535 ? passes : 1);
   if (c.int4())
     rope_kv_append_kernel<D, true><<<grid, kThreads, 0, stream>>>(a, c);
   else
