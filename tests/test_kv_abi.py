@@ -5,7 +5,12 @@ import ctypes
 import pytest
 
 import paper_2409_20361_amd as rrs
-from paper_2409_20361_amd._kv import _Struct
+
+
+class _Struct(ctypes.Structure):   # rrs_kv_cache
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale", "table")] + [
+        (n, ctypes.c_int32) for n in ("format", "pages", "kv_heads", "page_size", "head_dim",
+                                      "sequences", "max_pages")]
 
 NULL, SHAPE, ALIGN, WS, FLAGS = -1, -2, -4, -5, -9
 P, MIS = 0x10000, 0x10004
