@@ -57,6 +57,7 @@ struct Plan {
   int target;      // workgroups to aim at; 0: pieces of `steps` steps each, `pieces` per sequence
   int steps;       // at least so many steps to a piece
   int pieces;
+  int team;        // waves that share a piece: kWaves, or 1
   int ld_logits;   // row stride of the logits: max_length rounded up to whole blocks of 16
   int2* of_seq;    // sequences: first piece and number of pieces
   float* part;     // pieces x heads x dim: sums relative to the piece's m
@@ -239,12 +240,14 @@ constexpr float kSlack = 8.0f;
 
 // Grid: pieces x KV heads x row blocks. The row blocks of a piece and head read the same rows: they
 // are 8 apart, on one XCD, and share its L2.
-template <int D, bool kInt4, bool kMask>
+// kTeam: waves that share a piece; 1: every wave takes a whole sequence by itself.
+template <int D, bool kInt4, bool kMask, int kTeam>
 __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask && D == 128)))
     attention_kernel(AttentionArgs a, KvView c, Plan plan) {
   using S = Shape<D, kInt4>;
-  __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * S::kLds];
-  __shared__ float2 wave_stats[kWaves][kRows];
+  constexpr int kLds = kTeam == 1 ? S::kValues : S::kLds;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds];
+  __shared__ float2 wave_stats[kTeam][kRows];
 
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -252,6 +255,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
   const int quarter = lane >> 4;
 
   int unit = blockIdx.x, rb = 0;
+  if constexpr (kTeam == 1) unit = unit * kWaves + wave;
   if (plan.row_blocks > 1) {
     rb = unit / 8 % plan.row_blocks;
     unit = unit / (8 * plan.row_blocks) * 8 + unit % 8;
@@ -261,7 +265,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
   if (!find_piece(a, c, plan, unit / c.heads, &piece)) return;
   const int b = piece.b, n = piece.n, begin = piece.begin, end = piece.end;
   const bool whole = piece.count == 1;  // the piece is the sequence
-  if (plan.of_seq && threadIdx.x == 0 && hk == 0 && rb == 0 && piece.index == piece.first)
+  if (plan.of_seq && (kTeam == 1 ? lane : threadIdx.x) == 0 && hk == 0 && rb == 0 && piece.index == piece.first)
     plan.of_seq[b] = make_int2(piece.first, piece.count);
 
   // Queries as the second operand: column col, channels as the keys' lanes hold them.
@@ -297,7 +301,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
   float m = -INFINITY, sum = 0.0f;
   float rounded = 0.0f;  // float16 values: the sum of p as the products take it
   float vnorm = 0x1p-14f;  // INT4: the power of two that value scales and o are in units of
-  uint8_t* tile = lds + wave * S::kLds;
+  uint8_t* tile = lds + wave * kLds;
 
   // Pages: lane i holds page page0 + i of the sequence.
   const int last = (n - 1) & ~15;  // the last block of 16 slots
@@ -358,14 +362,14 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
       }
   };
 
-  int t0 = begin + wave * S::kTile;
+  int t0 = begin + (kTeam == 1 ? 0 : wave * S::kTile);
   if (t0 < end) {
     load_pages(t0 >> c.log_page);
     load_keys(t0);
     load_values();
   }
-  for (; t0 < end; t0 += kWaves * S::kTile) {
-    const int next = t0 + kWaves * S::kTile;
+  for (; t0 < end; t0 += kTeam * S::kTile) {
+    const int next = t0 + kTeam * S::kTile;
     // Logits, without the scale.
     float l[S::kBlocks][4];
     v4u vscale[(S::kBlocks + 1) / 2];  // INT4: the tile's value scales, two to a dword
@@ -557,14 +561,33 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
     rounded += __shfl_xor(rounded, 32);
     unit_o = rounded > 0.0f ? sum / rounded : 0.0f;
   }
+  if constexpr (kTeam == 1) {
+    unit_o = sum > 0.0f ? unit_o / sum : 0.0f;
+    if (col < rows) {
+      const size_t bh = (size_t)b * a.heads + head0 + col;
+#pragma unroll
+      for (int j = 0; j < S::kOut; ++j) {
+        const v4f x = o[j] * unit_o;
+        *reinterpret_cast<v4h*>(a.out + bh * D + 16 * j + 4 * quarter) =
+            v4h{(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
+      }
+      if (quarter == 0) {
+        if (a.lse)
+          a.lse[bh] = sum > 0.0f ? (m + __builtin_amdgcn_logf(sum)) / kLog2e : -INFINITY;
+        if (plan.stats)
+          plan.stats[(size_t)piece.index * a.heads + head0 + col] = make_float2(m, sum);
+      }
+    }
+    return;
+  }
   if (quarter == 0) wave_stats[wave][col] = make_float2(m, sum);
   __syncthreads();
   float top = -INFINITY, total = 0.0f;  // of the column, over the waves
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, wave_stats[w][col].x);
+  for (int w = 0; w < kTeam; ++w) top = fmaxf(top, wave_stats[w][col].x);
   const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w)
+  for (int w = 0; w < kTeam; ++w)
     total += wave_stats[w][col].y * __builtin_amdgcn_exp2f(wave_stats[w][col].x - base);
   unit_o *= __builtin_amdgcn_exp2f(m - base);
   if (whole) unit_o = total > 0.0f ? unit_o / total : 0.0f;
@@ -583,8 +606,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
     const int r = i / (D / 4), d = 4 * (i % (D / 4));
     v4f acc = {};
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w)
-      acc += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds + w * S::kLds) +
+    for (int w = 0; w < kTeam; ++w)
+      acc += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds + w * kLds) +
                                            r * S::kLdO + d);
     const size_t bh = (size_t)b * a.heads + head0 + r;
     if (whole)
@@ -734,6 +757,14 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
     p.steps = (int)(q < steps ? q : steps);
     p.pieces = (int)((steps - 1) / p.steps + 1);
   }
+  // Short sequences in more than one round of workgroups: a wave each, which saves the meeting of
+  // the four. 250 x 32 heads of 30 slots, INT4, dim 64: 31.5 -> 14.3 us; 200 x 64 of 64,
+  // float16: 77 -> 59 us. Longer ones gain from it with INT4 alone, which computes more per byte
+  // (250 x 32 of 300: 66 -> 49 us; float16 119 -> 127 us), or within one round not at all
+  // (60 x 8 of 200, INT4: 7.3 -> 10.3 us).
+  const long long units = c.sequences * share;
+  const long long team_steps = c.int4() && units > 4 * resident ? 2 : 1;
+  p.team = p.pieces == 1 && units > resident && steps <= team_steps ? 1 : kWaves;
   p.ld_logits = (max_length + 15) & ~15;
   const size_t pieces = (size_t)max_pieces(p, c, max_length);
   const bool joined = pieces > (size_t)c.sequences;
@@ -756,13 +787,23 @@ template <int D>
 hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
   const long long pieces = max_pieces(p, c, a.max_length);
   const long long units = pieces * c.heads;
-  const long long grid = p.row_blocks == 1 ? units : (units + 7) / 8 * 8 * p.row_blocks;
+  long long grid = p.row_blocks == 1 ? units : (units + 7) / 8 * 8 * p.row_blocks;
+  if (p.team == 1) grid = (grid + kWaves - 1) / kWaves;
   if (grid >= (1ll << 31)) return hipErrorInvalidValue;
   const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p); };
-  if (c.int4())
-    a.mask ? run(attention_kernel<D, true, true>) : run(attention_kernel<D, true, false>);
-  else
-    a.mask ? run(attention_kernel<D, false, true>) : run(attention_kernel<D, false, false>);
+  if (p.team == 1) {
+    if (c.int4())
+      a.mask ? run(attention_kernel<D, true, true, 1>) : run(attention_kernel<D, true, false, 1>);
+    else
+      a.mask ? run(attention_kernel<D, false, true, 1>) : run(attention_kernel<D, false, false, 1>);
+  } else {
+    if (c.int4())
+      a.mask ? run(attention_kernel<D, true, true, kWaves>)
+             : run(attention_kernel<D, true, false, kWaves>);
+    else
+      a.mask ? run(attention_kernel<D, false, true, kWaves>)
+             : run(attention_kernel<D, false, false, kWaves>);
+  }
   if (hipError_t e = hipGetLastError()) return e;
   const int blocks = p.logits ? (a.max_length - 1) / (4 * kThreads) + 1 : 0;
   const int joins = p.part ? c.sequences * a.heads : 0;

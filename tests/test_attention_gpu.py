@@ -101,6 +101,18 @@ def test_many_sequences(B, top, hk, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("B,top,heads,hk,D", [(40, 60, 32, 32, 64), (100, 100, 8, 8, 128),
+                                              (30, 64, 54, 27, 256), (27, 33, 34, 17, 64),
+                                              (260, 20, 51, 3, 64), (97, 400, 32, 32, 64)])
+@pytest.mark.parametrize("mask", [None, 0.7])
+def test_many_short_sequences(B, top, heads, hk, D, mask, fmt):
+    """More (sequence, KV head) pairs than fit the card at once: a wave for each."""
+    gen = torch.Generator().manual_seed(B)
+    lengths = torch.randint(0, top + 1, (B,), generator=gen).tolist()
+    _run(lengths, heads, hk, D, 32, fmt, max_length=top, mask=mask, with_weights=True, seed=14)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
 def test_sharp_and_flat(fmt):
     """Logits in the hundreds (one slot takes all), and all of them equal."""
     _run([513, 64, 2000], 8, 2, 128, 32, fmt, sharp=40.0, with_weights=True, seed=6)
