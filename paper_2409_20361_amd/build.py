@@ -1,7 +1,8 @@
-"""Build librrs.so (the C-ABI HIP library) in-tree for gfx950 with hipcc.
+"""Build librrs.so (the C-ABI HIP library) in-tree for gfx950 with hipcc, and _torch_calls.so
+(the calls on torch tensors) with the host compiler.
 
 Each source is compiled to an object in parallel, then linked into
-paper_2409_20361_amd/librrs.so. Always recompiles.
+paper_2409_20361_amd/librrs.so and _torch_calls.so. Always recompiles.
 """
 from __future__ import annotations
 
@@ -9,6 +10,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -16,6 +18,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "librrs.so")
+TORCH_LIB = os.path.join(PKG, "_torch_calls.so")
 OBJDIR = os.path.join(PKG, "_build")
 
 SOURCES = ["rrs_api.cpp", "rrs_gemm_route.cpp", "rrs_quant.hip", "rrs_weight.hip", "rrs_gemm.hip",
@@ -52,6 +55,42 @@ def hipcc() -> str:
     raise RuntimeError("hipcc not found (ROCm is required to build librrs.so)")
 
 
+def _run(cmd, what: str) -> str:
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{what} failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    return r.stderr
+
+
+def _compile_torch() -> str:
+    """rrs_torch.cpp: host code only, against the headers of the torch that is installed."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    obj = os.path.join(OBJDIR, "rrs_torch.o")
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall",
+           "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I" + INCLUDE]
+    for inc in (os.path.join(root, "include"),
+                os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"],
+                os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")):
+        cmd += ["-isystem", inc]
+    noise = _run(cmd + ["-c", os.path.join(CSRC, "rrs_torch.cpp"), "-o", obj], "compile")
+    if noise:
+        sys.stderr.write(f"[build] rrs_torch.cpp:\n{noise}\n")
+    return obj
+
+
+def _link_torch(obj: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = TORCH_LIB + ".tmp"
+    _run([os.environ.get("CXX", "g++"), "-shared", "-o", tmp, obj, "-L" + PKG, "-l:librrs.so",
+          "-L" + libs, "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python",
+          "-Wl,-rpath,$ORIGIN:" + libs], "link")
+    os.replace(tmp, TORCH_LIB)
+
+
 def _compile(src: str) -> str:
     obj = os.path.join(OBJDIR, os.path.splitext(src)[0] + ".o")
     lang = ["-x", "hip"] if src.endswith(".hip") else []
@@ -69,16 +108,19 @@ def _compile(src: str) -> str:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 4)) as ex:
+    with ThreadPoolExecutor(max_workers=min(len(SOURCES) + 1, os.cpu_count() or 4)) as ex:
+        torch_obj = ex.submit(_compile_torch)
         objs = list(ex.map(_compile, SOURCES))
+        torch_obj = torch_obj.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    _link_torch(torch_obj)
     if verbose:
-        print(f"[build] wrote {LIB}")
+        print(f"[build] wrote {LIB} and {TORCH_LIB}")
     return LIB
 
 

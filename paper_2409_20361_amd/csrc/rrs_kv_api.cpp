@@ -159,7 +159,8 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
                               const float* rope, int rope_rows, int rotary_dim, int flags,
                               const rrs_kv_cache* cache, const int32_t* seq, const int32_t* slot,
                               void* Q, float* weights, int32_t* slot_pos, void* stream) {
-  if (debug_enabled()) debug_print("rope_kv_append", cache);
+  const bool debug = debug_enabled();
+  if (debug) debug_print("rope_kv_append", cache);
   if (!qkv || !positions || !sections || !rope || !seq || !slot || !Q || any_null(cache))
     return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
@@ -185,7 +186,7 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
       !is_aligned(slot_pos))
     return RRS_ERR_ALIGN;
   if (rrs_status s = check_device()) return s;
-  if (debug_enabled()) {
+  if (debug) {
     for (int m = 0; m < M; ++m)
       if (rrs_status s = debug_check_finite_f16(
               static_cast<const uint16_t*>(qkv) + (size_t)m * (size_t)row_stride, (size_t)width,
@@ -226,7 +227,8 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
                                const int32_t* lengths, int max_length, float scale,
                                const uint8_t* mask, float* weights, void* out, float* lse,
                                void* workspace, size_t workspace_bytes, void* stream) {
-  if (debug_enabled()) debug_print("paged_attention", cache);
+  const bool debug = debug_enabled();
+  if (debug) debug_print("paged_attention", cache);
   if (!Q || !lengths || !out || any_null(cache)) return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
   if (!valid_shape(c) || !valid_heads(c, heads) || max_length < 1 || max_length > capacity(c))
@@ -240,7 +242,7 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
     return RRS_ERR_ALIGN;
   if (workspace_bytes < need) return RRS_ERR_WORKSPACE;
   if (rrs_status s = check_device()) return s;
-  if (debug_enabled()) {
+  if (debug) {
     if (rrs_status s = debug_check_finite_f16(
             Q, (size_t)c.sequences * (size_t)heads * (size_t)c.head_dim, "Q", stream))
       return s;
@@ -262,7 +264,8 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
                         const float* weights, const int32_t* slot_pos, const int32_t* keep_from,
                         int budget, int32_t* kept, int32_t* new_lengths, float* weights_out,
                         int32_t* pos_out, void* workspace, size_t workspace_bytes, void* stream) {
-  if (debug_enabled()) debug_print("kv_evict", cache);
+  const bool debug = debug_enabled();
+  if (debug) debug_print("kv_evict", cache);
   if (!lengths || !weights || !slot_pos || !keep_from || !kept || !new_lengths || !weights_out ||
       !pos_out || any_null(cache))
     return RRS_ERR_NULL;
@@ -279,7 +282,7 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
     return RRS_ERR_ALIGN;
   if (workspace_bytes < need) return RRS_ERR_WORKSPACE;
   if (rrs_status s = check_device()) return s;
-  if (debug_enabled())
+  if (debug)
     if (rrs_status s = debug_check_lengths(c, lengths, max_length, stream)) return s;
   const rrs::EvictArgs a{lengths, max_length, weights,     slot_pos,    keep_from,
                          budget,  kept,       new_lengths, weights_out, pos_out};
@@ -288,7 +291,8 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
 
 rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int max_length, void* K,
                        void* V, void* stream) {
-  if (debug_enabled()) debug_print("kv_read", cache);
+  const bool debug = debug_enabled();
+  if (debug) debug_print("kv_read", cache);
   if (!lengths || !K || !V || any_null(cache)) return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
   if (!valid_shape(c) || max_length < 1 || max_length > capacity(c)) return RRS_ERR_SHAPE;
@@ -296,7 +300,7 @@ rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int ma
   if (!aligned(c) || !is_aligned(lengths) || !is_aligned(K) || !is_aligned(V))
     return RRS_ERR_ALIGN;
   if (rrs_status s = check_device()) return s;
-  if (debug_enabled())
+  if (debug)
     if (rrs_status s = debug_check_lengths(c, lengths, max_length, stream)) return s;
   return from_hip(rrs::launch_kv_read(view(c), lengths, max_length, static_cast<uint16_t*>(K),
                                       static_cast<uint16_t*>(V),
