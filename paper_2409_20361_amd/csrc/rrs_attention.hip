@@ -619,21 +619,22 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
   }
 }
 
-// The common maximum of a head's pieces and the sum relative to it, by a whole wave. stats: the
-// head's first piece; `heads` apart.
-__device__ __forceinline__ float2 join_stats(const float2* stats, int count, int heads) {
-  const int lane = threadIdx.x & 63;
+// The common maximum of a head's pieces and the sum relative to it, by `lanes` neighbouring lanes
+// of a wave (a power of two). stats: the head's first piece; `heads` apart.
+__device__ __forceinline__ float2 join_stats(const float2* stats, int count, int heads,
+                                             int lanes) {
+  const int lane = threadIdx.x & (lanes - 1);
   float top = -INFINITY, total = 0.0f;
-  for (int i = lane; i < count; i += 64) top = fmaxf(top, stats[(size_t)i * heads].x);
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if (top == -INFINITY) return make_float2(top, 0.0f);
-  for (int i = lane; i < count; i += 64) {
+#pragma unroll 4
+  for (int i = lane; i < count; i += lanes) top = fmaxf(top, stats[(size_t)i * heads].x);
+  for (int d = lanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+  for (int i = lane; i < count; i += lanes) {
     const float2 st = stats[(size_t)i * heads];
-    total += st.y * __builtin_amdgcn_exp2f(st.x - top);
+    total += st.y * __builtin_amdgcn_exp2f(st.x - base);
   }
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+  for (int d = lanes / 2; d > 0; d >>= 1) total += __shfl_xor(total, d);
   return make_float2(top, total);
 }
 
@@ -650,7 +651,7 @@ __global__ void __launch_bounds__(kThreads)
     const int2 at = plan.of_seq[b];  // first piece, pieces
     if (at.y == 1) return;
     const float2* stats = plan.stats + (size_t)at.x * a.heads + h;
-    const float2 all = join_stats(stats, at.y, a.heads);
+    const float2 all = join_stats(stats, at.y, a.heads, 64);
     const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
     const float4* src = reinterpret_cast<const float4*>(
         plan.part + ((size_t)at.x * a.heads + h) * D);
@@ -697,19 +698,23 @@ __global__ void __launch_bounds__(kThreads)
     const int heads = min(plan.group - g0, kThreads);
     const size_t bh0 = (size_t)b * a.heads + hk * plan.group + g0;
     __syncthreads();
-    for (int g = threadIdx.x >> 6; g < heads; g += kWaves) {
+    // All heads at once, as many lanes to each as there are: by whole waves in turn, 40 heads took
+    // 20 us.
+    int lanes = 64;
+    while (lanes > 1 && lanes * heads > kThreads) lanes >>= 1;
+    for (int g = threadIdx.x / lanes; g < heads; g += kThreads / lanes) {
       const float2 all = join_stats(
-          plan.stats + (size_t)at.x * a.heads + hk * plan.group + g0 + g, at.y, a.heads);
+          plan.stats + (size_t)at.x * a.heads + hk * plan.group + g0 + g, at.y, a.heads, lanes);
       top_of[g] = all.x;
       inv_of[g] = all.y > 0.0f ? 1.0f / all.y : 0.0f;
     }
     __syncthreads();
     if (s < n)
+#pragma unroll 4
       for (int g = 0; g < heads; ++g) {
-        if (inv_of[g] == 0.0f) continue;
         const float4 l =
             *reinterpret_cast<const float4*>(plan.logits + (bh0 + g) * plan.ld_logits + s);
-        const float t = top_of[g], f = inv_of[g];
+        const float f = inv_of[g], t = f == 0.0f ? 0.0f : top_of[g];  // 0: every logit is -inf
         w.x += __builtin_amdgcn_exp2f(l.x - t) * f;
         w.y += __builtin_amdgcn_exp2f(l.y - t) * f;
         w.z += __builtin_amdgcn_exp2f(l.z - t) * f;
