@@ -571,7 +571,7 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *    read. No page belongs to two rows of the table in a call that writes the cache.
  * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,
  * sequences, max_pages, pages >= 1; sequences * kv_heads < 2^23; max_pages * page_size
- * < 2^31. The struct is read on the host during the call only.
+ * <= 2^30. The struct is read on the host during the call only.
  *
  * The calls below follow the conventions at the top of this file; wrong sizes are
  * RRS_ERR_SHAPE, an unknown format or flag RRS_ERR_FLAGS. Every device array is 16-byte
@@ -649,8 +649,10 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
  *                 (-inf where no slot takes part), with which outputs over parts of
  *                 a context are joined.
  *   workspace   : at least rrs_paged_attention_workspace_bytes; contents ignored.
- * Logits, softmax and sums in float32. Results do not depend on the other sequences of the
- * batch's values, and repeat bit for bit for the same shapes and max_length.
+ *   scale       : finite, else RRS_ERR_FLAGS.
+ * Logits, softmax and sums in float32; weights are rounded to float16 for the product with V. A
+ * sequence's result depends on the other sequences only through their lengths, which decide where the
+ * sums are cut; it repeats bit for bit for the same lengths and max_length.
  */
 size_t rrs_paged_attention_workspace_bytes(const rrs_kv_cache* cache, int heads, int max_length,
                                            int with_weights);

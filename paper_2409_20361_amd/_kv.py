@@ -4,6 +4,9 @@ Names follow include/rrs.h without the prefix. The calls check their tensors, pa
 pointers and the current HIP stream to librrs.so, and raise on a non-zero status, in a
 compiled module (_torch_calls.so, csrc/rrs_torch.cpp): host time counts for calls that a decode
 step makes once per layer. Every step of the computation runs in the library's kernels.
+
+A call without `workspace` takes what it needs from torch's caching allocator, also under
+torch.cuda.graph; under a capture that torch does not manage, pass one that outlives the graph.
 """
 from __future__ import annotations
 

@@ -801,7 +801,7 @@ hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStr
   const long long units = pieces * c.heads;
   long long grid = p.row_blocks == 1 ? units : (units + 7) / 8 * 8 * p.row_blocks;
   if (p.team == 1) grid = (grid + kWaves - 1) / kWaves;
-  if (grid >= (1ll << 31)) return hipErrorInvalidValue;
+  if (!fits_grid(grid, kThreads)) return hipErrorInvalidValue;
   const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p); };
   if (p.team == 1) {
     if (c.int4())
@@ -820,7 +820,7 @@ hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStr
   const int blocks = p.logits ? (a.max_length - 1) / (4 * kThreads) + 1 : 0;
   const int joins = p.part ? c.sequences * a.heads : 0;
   const long long wgs = joins + (long long)blocks * c.sequences * c.heads;
-  if (wgs >= (1ll << 31)) return hipErrorInvalidValue;
+  if (!fits_grid(wgs, kThreads)) return hipErrorInvalidValue;
   if (wgs > 0)
     attention_join_kernel<D><<<(unsigned)wgs, kThreads, 0, stream>>>(a, c, p, joins, blocks);
   return hipGetLastError();

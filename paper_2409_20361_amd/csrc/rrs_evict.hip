@@ -628,7 +628,8 @@ hipError_t launch(const EvictArgs& a, const KvView& c, void* workspace, hipStrea
     const LongPlan plan = long_plan(a.max_length, a.budget, workspace);
     const long long grid = (long long)rows * plan.segments;
     const int blocks = (moves + kMoveRows - 1) / kMoveRows;
-    if (grid >= (1ll << 31) || (long long)rows * blocks >= (1ll << 31)) return hipErrorInvalidValue;
+    if (!fits_grid(grid, kThreads) || !fits_grid((long long)rows * blocks, kMoveThreads))
+      return hipErrorInvalidValue;
     if (moves > 0) {
       evict_digit_kernel<0><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, plan);
       evict_digit_kernel<1><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, plan);
@@ -640,6 +641,7 @@ hipError_t launch(const EvictArgs& a, const KvView& c, void* workspace, hipStrea
           <<<(unsigned)(rows * blocks), kMoveThreads, 0, stream>>>(a, c, plan, blocks);
     return hipGetLastError();
   }
+  if (!fits_grid(rows, kThreads)) return hipErrorInvalidValue;
   // One round of a workgroup's lanes moves so many rows; with no more, they are moved right there.
   const bool moves_too = moves <= 16 * kThreads / kRow;
   const auto run = [&](auto kernel) { kernel<<<rows, kThreads, 0, stream>>>(a, c); };
@@ -655,7 +657,7 @@ hipError_t launch(const EvictArgs& a, const KvView& c, void* workspace, hipStrea
   if (moves_too) return hipSuccess;
   const int blocks = (a.budget + kMoveRows - 1) / kMoveRows;
   const long long grid = (long long)blocks * rows;
-  if (grid >= (1ll << 31)) return hipErrorInvalidValue;
+  if (!fits_grid(grid, kMoveThreads)) return hipErrorInvalidValue;
   evict_move_kernel<kRow><<<(unsigned)grid, kMoveThreads, 0, stream>>>(a.kept, a.budget, blocks, c);
   return hipGetLastError();
 }

@@ -45,6 +45,11 @@ struct KvView {
   }
 };
 
+// A grid of so many workgroups can be launched (the runtime counts threads in 32 bits).
+inline bool fits_grid(long long workgroups, int threads) {
+  return workgroups * threads < (1ll << 32);
+}
+
 struct RopeArgs {
   const uint16_t* qkv;
   int64_t row_stride;

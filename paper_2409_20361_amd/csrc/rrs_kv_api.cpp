@@ -2,6 +2,7 @@
 // stream. Every check runs on the host before any device work is enqueued.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdio>
 #include <memory>
 #include <new>
@@ -30,7 +31,7 @@ bool valid_shape(const rrs_kv_cache& c) {
          (P == 16 || P == 32 || P == 64 || P == 128 || P == 256) && c.pages >= 1 &&
          c.kv_heads >= 1 && c.sequences >= 1 && c.max_pages >= 1 &&
          (int64_t)c.sequences * c.kv_heads < ((int64_t)1 << 23) &&
-         (int64_t)c.max_pages * P < ((int64_t)1 << 31);
+         (int64_t)c.max_pages * P <= ((int64_t)1 << 30);
 }
 
 int capacity(const rrs_kv_cache& c) { return c.max_pages * c.page_size; }
@@ -233,7 +234,7 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
   const rrs_kv_cache& c = *cache;
   if (!valid_shape(c) || !valid_heads(c, heads) || max_length < 1 || max_length > capacity(c))
     return RRS_ERR_SHAPE;
-  if (!valid_format(c)) return RRS_ERR_FLAGS;
+  if (!valid_format(c) || !std::isfinite(scale)) return RRS_ERR_FLAGS;
   const size_t need =
       rrs::attention_workspace_bytes(view(c), heads, max_length, weights != nullptr);
   if (need > 0 && !workspace) return RRS_ERR_NULL;

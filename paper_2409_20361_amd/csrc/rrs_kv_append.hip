@@ -233,6 +233,7 @@ template <int D>
 hipError_t append(const RopeArgs& a, const KvView& c, hipStream_t stream) {
   const int per_pass = kThreads / (D / 16);
   const int passes = (a.heads + 2 * c.heads + per_pass - 1) / per_pass;
+  if (!fits_grid(a.M, kThreads)) return hipErrorInvalidValue;
   // Few tokens: a workgroup per pass, so that all rows are in flight at once.
   const dim3 grid(a.M, a.M < 2048 && passes <= 65535 ? passes : 1);
   if (c.int4())
@@ -248,7 +249,7 @@ hipError_t read(const KvView& c, const int32_t* lengths, int max_length, uint16_
   const int rows = kThreads / (D / 8);
   const int blocks = (max_length - 1) / rows + 1;
   const long long grid = (long long)blocks * c.sequences * c.heads;
-  if (grid >= (1ll << 31)) return hipErrorInvalidValue;
+  if (!fits_grid(grid, kThreads)) return hipErrorInvalidValue;
   if (c.int4())
     kv_read_kernel<D, true>
         <<<(unsigned)grid, kThreads, 0, stream>>>(c, lengths, max_length, blocks, K, V);

@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -102,9 +103,13 @@ PyObject* check(rrs_status s, const char* where, PyObject* result) {
   return nullptr;
 }
 
-void* stream_of(const at::Tensor& t) {
-  return c10::hip::getCurrentHIPStream(t.get_device()).stream();
-}
+// The tensor's device made current for the call, and its current stream.
+struct Launch {
+  c10::DeviceGuard guard;
+  void* stream;
+  explicit Launch(const at::Tensor& t)
+      : guard(t.device()), stream(c10::hip::getCurrentHIPStream(t.get_device()).stream()) {}
+};
 
 struct Cache {
   rrs_kv_cache c{};
@@ -237,13 +242,14 @@ RRS_CALL(rope_kv_append) {
   } else {
     qp = dev(a[15], "out", at::kHalf, {M, heads, cache.dim});
   }
+  const Launch launch(qkv);
   const rrs_status s = rrs_rope_kv_append(
       qkv.data_ptr(), M > 1 ? qkv.stride(0) : width, (int)M, heads,
       static_cast<const int32_t*>(pp), (int)axes, sections,
       static_cast<const float*>(rope.data_ptr()), (int)rope.size(0), (int)rope.size(1),
       to_bool(a[12]) ? RRS_ROPE_INTERLEAVED : 0, &cache.c, static_cast<const int32_t*>(sp),
       static_cast<const int32_t*>(tp), qp, static_cast<float*>(wp), static_cast<int32_t*>(op),
-      stream_of(qkv));
+      launch.stream);
   if (s != RRS_OK) return check(s, "rrs_rope_kv_append", nullptr);
   return a[15] == Py_None ? wrap(made) : Py_NewRef(a[15]);
 }
@@ -281,10 +287,11 @@ RRS_CALL(paged_attention) {
           ? rrs_paged_attention_workspace_bytes(&cache.c, (int)heads, top, wp != nullptr)
           : 0;
   const Workspace ws(a[12], need, Q);
+  const Launch launch(Q);
   const rrs_status s = rrs_paged_attention(
       qp, (int)heads, &cache.c, static_cast<const int32_t*>(lp), top, (float)scale,
       static_cast<const uint8_t*>(mp), static_cast<float*>(wp), yp,
-      want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, ws.p, ws.bytes, stream_of(Q));
+      want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, ws.p, ws.bytes, launch.stream);
   if (s != RRS_OK) return check(s, "rrs_paged_attention", nullptr);
   PyObject* y = a[13] == Py_None ? wrap(made) : Py_NewRef(a[13]);
   if (!want_lse || !y) return y;
@@ -338,11 +345,12 @@ RRS_CALL(kv_evict) {
   const size_t need =
       a[12] == Py_None ? rrs_kv_evict_workspace_bytes(&cache.c, top, budget) : 0;
   const Workspace ws(a[12], need, lengths);
+  const Launch launch(lengths);
   const rrs_status s = rrs_kv_evict(
       &cache.c, static_cast<const int32_t*>(lp), top, static_cast<const float*>(wp),
       static_cast<const int32_t*>(pp), static_cast<const int32_t*>(fp), budget,
       static_cast<int32_t*>(out[0]), static_cast<int32_t*>(out[1]), static_cast<float*>(out[2]),
-      static_cast<int32_t*>(out[3]), ws.p, ws.bytes, stream_of(lengths));
+      static_cast<int32_t*>(out[3]), ws.p, ws.bytes, launch.stream);
   if (s != RRS_OK) return check(s, "rrs_kv_evict", nullptr);
   if (a[11] != Py_None) return Py_NewRef(a[11]);
   PyObject* r = PyTuple_New(4);
@@ -390,8 +398,9 @@ RRS_CALL(kv_read) {
     out[0] = dev(PyTuple_GET_ITEM(a[7], 0), "K", at::kHalf, shape);
     out[1] = dev(PyTuple_GET_ITEM(a[7], 1), "V", at::kHalf, shape);
   }
+  const Launch launch(lengths);
   const rrs_status s = rrs_kv_read(&cache.c, static_cast<const int32_t*>(lp), top, out[0], out[1],
-                                   stream_of(lengths));
+                                   launch.stream);
   if (s != RRS_OK) return check(s, "rrs_kv_read", nullptr);
   if (a[7] != Py_None) return Py_NewRef(a[7]);
   PyObject* k = wrap(made[0]);

@@ -30,6 +30,7 @@ BAD_CACHES = [
     (dict(page_size=48), SHAPE), (dict(page_size=512), SHAPE), (dict(pages=0), SHAPE),
     (dict(kv_heads=0), SHAPE), (dict(sequences=0), SHAPE), (dict(max_pages=0), SHAPE),
     (dict(sequences=1 << 23, kv_heads=1), SHAPE), (dict(max_pages=1 << 27), SHAPE),
+    (dict(max_pages=(1 << 26) + 1), SHAPE),
     (dict(format=2), FLAGS), (dict(format=-1), FLAGS),
     (dict(k=MIS), ALIGN), (dict(v=MIS), ALIGN), (dict(table=MIS), ALIGN),
     (dict(format=1, k_scale=MIS, v_scale=P), ALIGN),
@@ -103,6 +104,7 @@ def test_append_sections():
     (dict(top=0), SHAPE), (dict(top=81), SHAPE),
     *[({n: MIS}, ALIGN) for n in ("Q", "lengths", "out", "mask", "weights", "lse", "ws")],
     (dict(weights=P, ws=None), NULL), (dict(weights=P, bytes=0), WS),
+    *[(dict(scale=x), FLAGS) for x in (float("nan"), float("inf"), -float("inf"))],
 ])
 def test_attend(kw, want):
     assert _attend(**kw) == want
