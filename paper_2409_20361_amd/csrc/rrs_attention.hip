@@ -762,6 +762,12 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
   p.target = one_round ? resident : 4 * resident;
   p.steps = one_round ? 2 : 8;
   const long long steps = (max_length - 1) / p.step + 1;
+  // Sequences of a few steps stay whole, which spares them the second launch (17 x 3 KV heads
+  // of 128, float16: 4 steps 8.6 against 11.1 us in two pieces, 6 steps 10.9 against 11.2, 8 steps 14.4
+  // against 11.5; INT4, whose steps are longer, 10.5 against 11.8 at 4 and 13.7 against 11.8 at
+  // 6); of up to 8 where whole ones already fill the card (60 x 8, 8 steps: 29 against 32 us).
+  const long long units = c.sequences * share;
+  if (steps <= (units >= 256 ? 8 : c.int4() ? 4 : 6)) p.steps = (int)steps;
   if (c.sequences > kWidest || steps <= p.steps) {  // many balance each other; or nothing to cut
     p.target = 0;
     long long q = steps * c.sequences * share / (4 * resident);
@@ -774,7 +780,6 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
   // float16: 77 -> 59 us. Longer ones gain from it with INT4 alone, which computes more per byte
   // (250 x 32 of 300: 66 -> 49 us; float16 119 -> 127 us), or within one round not at all
   // (60 x 8 of 200, INT4: 7.3 -> 10.3 us).
-  const long long units = c.sequences * share;
   const long long team_steps = c.int4() && units > 4 * resident ? 2 : 1;
   p.team = p.pieces == 1 && units > resident && steps <= team_steps ? 1 : kWaves;
   p.ld_logits = (max_length + 15) & ~15;
