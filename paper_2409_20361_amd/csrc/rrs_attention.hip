@@ -707,21 +707,36 @@ __global__ void __launch_bounds__(kThreads)
     const int2 at = plan.of_seq[b];  // first piece, pieces
     if (at.y == 1) return;
     const float2* stats = plan.stats + (size_t)at.x * a.heads + h;
-    const float2 all = join_stats(stats, at.y, a.heads, 64);
     const int d4 = threadIdx.x % (D / 4), part = threadIdx.x / (D / 4);
-    const float4* src = reinterpret_cast<const float4*>(
-        plan.part + ((size_t)at.x * a.heads + h) * D);
+    const float4* src =
+        reinterpret_cast<const float4*>(plan.part + ((size_t)at.x * a.heads + h) * D) + d4;
+    const size_t stride = (size_t)a.heads * (D / 4);
+    // The thread's first pieces are on their way while the stats are joined.
+    constexpr int kAhead = 4;
+    float4 ahead[kAhead];
+    float2 own[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = min(part + k * kParts, at.y - 1);
+      ahead[k] = src[i * stride];
+      own[k] = stats[(size_t)i * a.heads];
+    }
+    const float2 all = join_stats(stats, at.y, a.heads, 64);
     float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const float base = all.x == -INFINITY ? 0.0f : all.x;
-#pragma unroll 4
-    for (int i = part; i < at.y; i += kParts) {
-      const float f = __builtin_amdgcn_exp2f(stats[(size_t)i * a.heads].x - base);
-      const float4 x = src[(size_t)i * a.heads * (D / 4) + d4];
+    const auto add = [&](float m, const float4& x) {
+      const float f = __builtin_amdgcn_exp2f(m - base);  // 0 for a piece without slots
       acc.x += f * x.x;
       acc.y += f * x.y;
       acc.z += f * x.z;
       acc.w += f * x.w;
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (part + k * kParts < at.y) add(own[k].x, ahead[k]);
+#pragma unroll 4
+    for (int i = part + kAhead * kParts; i < at.y; i += kParts)
+      add(stats[(size_t)i * a.heads].x, src[i * stride]);
     acc_of[threadIdx.x] = acc;
     __syncthreads();
     if (part != 0) return;
