@@ -481,12 +481,14 @@ __global__ void __launch_bounds__(kThreads) evict_list_kernel(EvictArgs a, KvVie
   const int C = a.budget;
   const int segments = (n + kSegment - 1) / kSegment;
   const LongRow r = plan.row(bh);
-  clear_from(a, c, bh, min(n, C), seg * kThreads + t, plan.segments * kThreads);
   if (seg == 0) {
     if (t == 0 && bh % c.heads == 0) a.new_lengths[b] = min(n, C);
     if (t == 0 && n <= C) r.state[4] = 0;
   }
-  if (seg >= segments) return;
+  const auto clear = [&] {
+    clear_from(a, c, bh, min(n, C), seg * kThreads + t, plan.segments * kThreads);
+  };
+  if (seg >= segments) return clear();
   const size_t base = (size_t)bh * c.capacity();
   const int j0 = seg * kSegment + wave * kSegItems * 64 + lane;  // slot of item k: j0 + 64 k
   float wr[kSegItems];
@@ -582,6 +584,7 @@ __global__ void __launch_bounds__(kThreads) evict_list_kernel(EvictArgs a, KvVie
       a.pos_out[base + j] = pr[k];
     }
   }
+  clear();  // last: loads issued after these stores would wait for them
 }
 
 // Move number i of a row: hole i takes source (moves - 1 - i) of the descending list.
