@@ -155,10 +155,12 @@ __device__ __forceinline__ bool find_piece(const AttentionArgs& a, const KvView&
   return true;
 }
 
-template <int D, bool kInt4>
+template <int D, bool kInt4, int kTeam = kWaves>
 struct Shape {
-  // Slots per wave and step. 16 where 32 rows would not leave registers for a second wave.
-  static constexpr int kTile = kInt4 ? 64 : D == 256 ? 16 : 32;
+  // Slots per wave and step. 16 where 32 rows would not leave registers for a second wave, and for
+  // short sequences: more waves hide more of the chain of length, page and rows (179 x 64 heads of up to
+  // 5 slots 26 -> 21 us, 200 x 64 of up to 64 within 3 %).
+  static constexpr int kTile = kInt4 ? 64 : D == 256 || kTeam == 1 ? 16 : 32;
   static constexpr int kBlocks = kTile / 16;         // of 16 slots
   static constexpr int kRow = kInt4 ? D / 2 : 2 * D; // bytes of a cache row
   static constexpr int kSteps = D / 32;              // mfma steps of a logit
@@ -171,7 +173,8 @@ struct Shape {
   static constexpr int kValues = kTile * kRow;       // bytes of a wave's value tile
   static constexpr int kSums = kRows * kLdO * 4;
   static constexpr int kLds = kValues > kSums ? kValues : kSums;  // per wave
-  static constexpr int kPerSimd = D == 256 ? 2 : 3;  // waves: limits the registers
+  // Waves: limits the registers.
+  static constexpr int kPerSimd = D == 256 ? 2 : kTeam == 1 && !kInt4 ? 4 : 3;
 
   // Where 16-byte chunk c of slot t's value row lies in the wave's tile. The chunks of a row are
   // permuted by the slot, so that the rows that one transposed read touches lie in
@@ -281,9 +284,9 @@ __device__ __forceinline__ float2 weight_row(float top, float total) {
 // are 8 apart, on one XCD, and share its L2.
 // kTeam: waves that share a piece; 1: every wave takes a whole sequence by itself.
 template <int D, bool kInt4, bool kMask, int kTeam>
-__global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask && D == 128)))
+__global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd - (kMask && D == 128)))
     attention_kernel(AttentionArgs a, KvView c, Plan plan) {
-  using S = Shape<D, kInt4>;
+  using S = Shape<D, kInt4, kTeam>;
   constexpr int kLds = kTeam == 1 ? S::kValues : S::kLds;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds];
   __shared__ float2 wave_stats[kTeam][kRows], row_stats[kWaves / kTeam][kRows];
@@ -304,7 +307,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
   if (!find_piece(a, c, plan, unit / c.heads, &piece)) return;
   const int b = piece.b, n = piece.n, begin = piece.begin, end = piece.end;
   const bool whole = piece.count == 1;  // the piece is the sequence
-  if (plan.of_seq && (kTeam == 1 ? lane : threadIdx.x) == 0 && hk == 0 && rb == 0 && piece.index == piece.first)
+  if (plan.of_seq && (kTeam == 1 ? lane : threadIdx.x) == 0 && hk == 0 && rb == 0 &&
+      piece.index == piece.first)
     plan.of_seq[b] = make_int2(piece.first, piece.count);
 
   // Queries as the second operand: column col, channels as the keys' lanes hold them.
@@ -357,7 +361,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
   v2u ks[S::kBlocks], vs[S::kBlocks];
   uint32_t mask[S::kBlocks];
   size_t row[S::kBlocks];  // the blocks' first rows
-  const uint32_t key_at = col * S::kRow + quarter * (kInt4 ? S::kKey : 16);
+  // A block's last row, in whose place rows past it are not loaded: thousands of short sequences
+  // would spend much of the bandwidth on those past their ends (200 x 64 heads of up to 30 slots 31 -> 23
+  // us, of up to 100 76 -> 69). Longer sequences spare the instructions.
+  int lim[S::kBlocks];
+  const uint32_t quarter_at = quarter * (kInt4 ? S::kKey : 16);
+  const uint32_t key_at0 = col * S::kRow + quarter_at;
   const auto load_keys = [&](int t0) {
     if ((min(t0 + S::kTile - 16, last) >> c.log_page) - page0 >= 64) load_pages(t0 >> c.log_page);
 #pragma unroll
@@ -366,6 +375,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
       const int page = t >> c.log_page;
       row[u] = c.page_row(__builtin_amdgcn_readlane(pages, page - page0), hk) +
                (t & ((1 << c.log_page) - 1));
+      lim[u] = kTeam == 1 ? min(n - 1 - t, 15) : 15;
+      const uint32_t key_at =
+          kTeam == 1 ? min(col, lim[u]) * S::kRow + quarter_at : key_at0;
       const uint8_t* p = c.k + row[u] * S::kRow;
       if constexpr (S::kKey < 16) {
         const v2u w = load_at<v2u>(p, key_at);
@@ -391,7 +403,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4>::kPerSimd - (kMask 
     for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
       for (int i = 0; i < S::kPieces; ++i) {
-        const uint8_t* p = c.v + (row[u] + i * kRowsPerLoad) * S::kRow;
+        const int first = min(i * kRowsPerLoad, lim[u] & -kRowsPerLoad);
+        const uint8_t* p = c.v + (row[u] + first) * S::kRow;
         if constexpr (S::kPiece < 16) {
           const v2u w = load_at<v2u>(p, val_at);
           val[u][i] = v4u{w[0], w[1], 0u, 0u};
@@ -832,8 +845,8 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
   }
   // Short sequences in more than one round of workgroups: a wave each, which saves the meeting of
   // the four. 250 x 32 heads of 30 slots, INT4, dim 64: 31.5 -> 14.3 us; 200 x 64 of 64,
-  // float16: 77 -> 59 us. Longer ones gain from it with INT4 alone, which computes more per byte
-  // (250 x 32 of 300: 66 -> 49 us; float16 119 -> 127 us), or within one round not at all
+  // float16: 77 -> 52 us. Longer ones gain from it with INT4 alone, which computes more per byte
+  // (250 x 32 of 300: 66 -> 49 us; float16, of 250, 103 -> 108), or within one round not at all
   // (60 x 8 of 200, INT4: 7.3 -> 10.3 us).
   const long long team_steps = c.int4() && units > 4 * resident ? 2 : 1;
   p.team = p.pieces == 1 && units > resident && steps <= team_steps ? 1 : kWaves;
