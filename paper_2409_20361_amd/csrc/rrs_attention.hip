@@ -284,7 +284,7 @@ __device__ __forceinline__ float2 weight_row(float top, float total) {
 // are 8 apart, on one XCD, and share its L2.
 // kTeam: waves that share a piece; 1: every wave takes a whole sequence by itself.
 template <int D, bool kInt4, bool kMask, int kTeam>
-__global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd - (kMask && D == 128)))
+__global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     attention_kernel(AttentionArgs a, KvView c, Plan plan) {
   using S = Shape<D, kInt4, kTeam>;
   constexpr int kLds = kTeam == 1 ? S::kValues : S::kLds;
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd - 
   v4u key[S::kBlocks][(S::kKey + 15) / 16];
   v4u val[S::kBlocks][S::kPieces];
   v2u ks[S::kBlocks], vs[S::kBlocks];
-  uint32_t mask[S::kBlocks];
+  uint8_t mask = 0;  // of slot t0 + lane
   size_t row[S::kBlocks];  // the blocks' first rows
   // A block's last row, in whose place rows past it are not loaded: thousands of short sequences
   // would spend much of the bandwidth on those past their ends (200 x 64 heads of up to 30 slots 31 -> 23
@@ -391,9 +391,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd - 
         ks[u] = load_at<v2u>(c.k_scale + row[u], 8 * quarter);
         vs[u] = load_at<v2u>(c.v_scale + row[u], 8 * quarter);
       }
-      if constexpr (kMask)  // four slots: aligned, inside the row
-        mask[u] = load_at<uint32_t>(a.mask + (size_t)b * c.capacity() + t, 4 * quarter);
     }
+    if constexpr (kMask)  // up to the last block's end: inside the row
+      mask = load_at<uint8_t>(a.mask + (size_t)b * c.capacity() + t0, min(lane, last + 15 - t0));
   };
   constexpr int kPerRow = S::kRow / S::kPiece;   // pieces of a row
   constexpr int kRowsPerLoad = 64 / kPerRow;     // rows that the wave loads at a time
@@ -453,12 +453,14 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd - 
     // Slots that take no part: a logit of -inf, a value scale of 0 (whatever was there).
     bool live[S::kBlocks * 4];
     if (kMask || t0 + S::kTile > end) {
+      uint64_t in_tile = end - t0 >= 64 ? ~0ull : (1ull << (end - t0)) - 1;  // bit: slot t0 + it
+      if constexpr (kMask) in_tile &= __ballot(mask != 0);
+      const uint64_t mine = in_tile >> (4 * quarter);
 #pragma unroll
       for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool in = t0 + 16 * u + 4 * quarter + r < end &&
-                          (!kMask || ((mask[u] >> (8 * r)) & 255u) != 0);
+          const bool in = mine >> (16 * u + r) & 1;
           live[4 * u + r] = in;
           l[u][r] = in ? l[u][r] : -INFINITY;
         }
