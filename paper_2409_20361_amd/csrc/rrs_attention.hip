@@ -613,10 +613,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
   if constexpr (!kInt4) {
     rounded += __shfl_xor(rounded, 16);
     rounded += __shfl_xor(rounded, 32);
-    unit_o = rounded > 0.0f ? sum / rounded : 0.0f;
+    unit_o = rounded != 0.0f ? sum / rounded : 0.0f;
   }
   if constexpr (kTeam == 1) {
-    unit_o = sum > 0.0f ? unit_o / sum : 0.0f;
+    unit_o = sum != 0.0f ? unit_o / sum : 0.0f;  // (NaN where the sum is)
     if (col < rows) {
       const size_t bh = (size_t)b * a.heads + head0 + col;
 #pragma unroll
@@ -627,7 +627,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
       }
       if (quarter == 0) {
         if (a.lse)
-          a.lse[bh] = sum > 0.0f ? (m + __builtin_amdgcn_logf(sum)) / kLog2e : -INFINITY;
+          a.lse[bh] = sum != 0.0f ? (m + __builtin_amdgcn_logf(sum)) / kLog2e : -INFINITY;
         if (plan.stats)
           plan.stats[(size_t)piece.index * a.heads + head0 + col] = make_float2(m, sum);
       }
@@ -653,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
   for (int w = 0; w < kTeam; ++w)
     total += wave_stats[w][col].y * __builtin_amdgcn_exp2f(wave_stats[w][col].x - base);
   unit_o *= __builtin_amdgcn_exp2f(m - base);
-  if (whole) unit_o = total > 0.0f ? unit_o / total : 0.0f;
+  if (whole) unit_o = total != 0.0f ? unit_o / total : 0.0f;
   float* mine = reinterpret_cast<float*>(tile);
 #pragma unroll
   for (int j = 0; j < S::kOut; ++j)
@@ -663,7 +663,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
   if (threadIdx.x < rows) {
     const size_t bh = (size_t)b * a.heads + head0 + threadIdx.x;
     if (whole && a.lse)
-      a.lse[bh] = total > 0.0f ? (top + __builtin_amdgcn_logf(total)) / kLog2e : -INFINITY;
+      a.lse[bh] = total != 0.0f ? (top + __builtin_amdgcn_logf(total)) / kLog2e : -INFINITY;
     if (plan.stats) plan.stats[(size_t)piece.index * a.heads + head0 + threadIdx.x] = make_float2(top, total);
   }
   __syncthreads();
@@ -762,7 +762,7 @@ __global__ void __launch_bounds__(kThreads)
       acc.z += x.z;
       acc.w += x.w;
     }
-    const bool some = all.y > 0.0f;
+    const bool some = all.y != 0.0f;
     const float v[4] = {acc.x, acc.y, acc.z, acc.w};
     v4h y;
 #pragma unroll

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import paper_2409_20361_amd as rrs
-from _kv_util import attention, make_cache
+from _kv_util import attention, make_cache, values
 
 pytestmark = pytest.mark.gpu
 
@@ -280,3 +280,32 @@ def test_refusals():
         call(Q, cache, n, 64, weights=torch.ones((2, 2, 64), device="cuda"),
              workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
     assert rrs.paged_attention_workspace_bytes(cache, 3, 64) == 0
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("B,lengths", [(2, [40, 33]), (2, [9000, 7000]), (200, [40, 33])])
+def test_not_a_number_is_not_hidden(B, lengths, bad, fmt):
+    """A live key that gives no finite logit: its heads' outputs and lse are NaN, the others' are not."""
+    gen = torch.Generator().manual_seed(15)
+    hk, D, page = 8, 128, 16
+    lengths = [lengths[b % 2] for b in range(B)]
+    cache = make_cache(gen, B, max(lengths), hk, D, page, fmt)
+    Q = torch.randn((B, 2 * hk, D), generator=gen).half().cuda()
+    t = lengths[1] - 2   # of sequence 1, KV head 3
+    where = (cache.table[1, t // page].long(), 3, t % page)
+    # An infinite key may push its head's logit to -inf, which is a weight of 0: both queries are
+    # turned so that it does not.
+    if bad == math.inf:
+        k = torch.ones(D) if fmt == "f16" else values(cache, 1, lengths[1])[0][3, t].sign()
+        Q[1, 6:8] = torch.where(k == 0, 1.0, k).half().cuda()
+    if fmt == "f16":
+        cache.k[where] = bad
+    else:
+        cache.k_scale[where] = bad
+    n = torch.tensor(lengths, dtype=torch.int32).cuda()
+    out, lse = rrs.paged_attention(Q, cache, n, max(lengths), return_lse=True)
+    hit = torch.zeros((B, 2 * hk), dtype=torch.bool)
+    hit[1, 6:8] = True
+    assert torch.equal(out.isnan().all(-1).cpu(), hit) and torch.equal(out.isnan().any(-1).cpu(), hit)
+    assert torch.equal(lse.isnan().cpu(), hit)
