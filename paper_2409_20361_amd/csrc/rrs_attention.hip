@@ -235,14 +235,20 @@ __device__ __forceinline__ V mask_halves(V x, const bool* live) {
   return __builtin_bit_cast(V, w);
 }
 
+// NaN if one of them is (the column's result is NaN then, whatever its maximum): two of these are one
+// instruction, where fmaxf first quiets its operands.
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+
 // The largest of x over the four lanes of a column.
 __device__ __forceinline__ float column_max(float x) {
   const uint32_t u = __builtin_bit_cast(uint32_t, x);
   const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
-  x = fmaxf(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
+  x = larger(__builtin_bit_cast(float, (uint32_t)a[0]), __builtin_bit_cast(float, (uint32_t)a[1]));
   const uint32_t v = __builtin_bit_cast(uint32_t, x);
   const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
-  return fmaxf(__builtin_bit_cast(float, (uint32_t)b[0]),
+  return larger(__builtin_bit_cast(float, (uint32_t)b[0]),
                __builtin_bit_cast(float, (uint32_t)b[1]));
 }
 
@@ -483,7 +489,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u)
-      top = fmaxf(fmaxf(fmaxf(top, l[u][0]), fmaxf(l[u][1], l[u][2])), l[u][3]);
+      top = larger(larger(larger(larger(top, l[u][0]), l[u][1]), l[u][2]), l[u][3]);
     top = column_max(top) * scale;
     if (__any(top > m + kSlack)) {
       const float up = fmaxf(m, top);
@@ -515,7 +521,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
           for (int j = 0; j < S::kOut; ++j) o[j] *= shrink;
         }
       }
-      const _Float16 inv = (_Float16)(1.0f / vnorm);
+      // 1 / vnorm: for a power of two the two exponents add up to twice that of 1.
+      const _Float16 inv =
+          (_Float16)__builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, vnorm));
 #pragma unroll
       for (int u = 0; u < S::kBlocks / 2; ++u)
         vscale[u] = __builtin_bit_cast(
@@ -527,11 +535,13 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
         sum += x;
-        if constexpr (kInt4)
-          x *= (float)__builtin_bit_cast(v8h, vscale[u / 2])[4 * (u & 1) + r];
-        p[4 * u + r] = (_Float16)x;
+        if constexpr (kInt4)  // as a mixed fma, which takes the float16 factor as it is
+          p[4 * u + r] = (_Float16)__builtin_fmaf(
+              x, (float)__builtin_bit_cast(v8h, vscale[u / 2])[4 * (u & 1) + r], 0.0f);
+        else
+          p[4 * u + r] = (_Float16)x;
       }
 
     if constexpr (!kInt4) {
