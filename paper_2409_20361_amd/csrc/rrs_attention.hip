@@ -28,11 +28,12 @@
 // more than the rounding of the output itself. Everything else is float32.
 //
 // Measured (kernel time; bytes of K, V and scales read): 256 sequences of 1 to 4096 slots, 8 KV
-// heads of 128, float16, 382 us (5.7 TB/s); one of 131071 slots 95 us (5.7 TB/s); 49 sequences of 1 to
-// 4096, INT4, 34 us (3.5 TB/s: 53 % of the cycles issue vector instructions, half of them
-// the codes' way to float16, at three waves per SIMD); 8 x 40 heads over one KV head of 256 with
-// a mask, 19 us (2.0 TB/s: latency of three or four tiles per wave, the rows read by three row blocks);
-// one sequence of 117 slots, 32 heads, 5 us (latency).
+// heads of 128, float16, 383 us (5.6 TB/s); one of 131071 slots 94 us (5.7 TB/s); 49 sequences of
+// 1 to 4096, INT4, 33.7 us (3.5 TB/s: half of the cycles issue vector instructions, half of them
+// the codes' way to float16, at three waves per SIMD; 64 of 1 to 8192 with 16 KV heads
+// 123 us, 4.6 TB/s); 8 x 40 heads over one KV head of 256 with a mask, 19 us (2.0 TB/s: latency of three or
+// four tiles per wave, the rows read by three row blocks); one sequence of 117 slots, 32 heads, 5
+// us (latency); 179 x 64 heads of up to 5 slots 14 us.
 #include "rrs_device.h"
 #include "rrs_kv.h"
 
@@ -674,7 +675,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     const size_t bh = (size_t)b * a.heads + head0 + threadIdx.x;
     if (whole && a.lse)
       a.lse[bh] = total != 0.0f ? (top + __builtin_amdgcn_logf(total)) / kLog2e : -INFINITY;
-    if (plan.stats) plan.stats[(size_t)piece.index * a.heads + head0 + threadIdx.x] = make_float2(top, total);
+    if (plan.stats)
+      plan.stats[(size_t)piece.index * a.heads + head0 + threadIdx.x] = make_float2(top, total);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < rows * (D / 4); i += kThreads) {

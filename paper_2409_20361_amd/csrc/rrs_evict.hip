@@ -13,7 +13,7 @@
 // that meet in the workspace.
 //
 // Measured: 64 rows of 2049 slots to 2048, 5.9 us; 128 rows of up to 8192 to 2048, 13.8 us, their moves
-// (INT4 rows of 64 bytes) 12.4 us; 16 rows of 131072 to 16384, three digits 7.5 us each, lists 17 us,
+// (INT4 rows of 64 bytes) 12.4 us; 16 rows of 131072 to 16384, three digits 7.7 us each, lists 15.6 us,
 // moves 52 us (4.5 TB/s).
 //
 // Moves. The evicted slots below the budget (holes) take the kept slots above it, in order. No slot is

@@ -11,7 +11,8 @@
 // 32 + 8 + 8 into INT4, 9.6 us, one token 2.4 us (latency).
 //
 // Read-back. One row of K and V per D / 8 lanes; bound by the writes, which go past the caches
-// (134 MB from 2048 slots of 4 x 32 INT4 heads: 25.7 us, 40.8 with ordinary stores).
+// (134 MB from 2048 slots of 4 x 32 INT4 heads: 25.7 us, 40.8 with ordinary stores;
+// 41 with both where inputs and outputs in use outgrow the last-level cache).
 #include "rrs_device.h"
 #include "rrs_kv.h"
 
