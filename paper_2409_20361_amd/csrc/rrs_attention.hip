@@ -20,9 +20,9 @@
 // workgroup that has the whole sequence (15 x 3 KV heads of 65 slots: 9.7 -> 6.6 us).
 //
 // INT4. Codes become float16 exactly (an exponent is or-ed on, an offset taken off). A key's scale
-// multiplies its logit; a value's scale multiplies its p before p is rounded to float16. So that
-// this product neither overflows nor loses bits to subnormals, the scales are in units
-// of a power of two above the largest seen so far, kept like the softmax's maximum.
+// multiplies its logit; a value's scale multiplies its p before p is rounded to float16. m follows
+// the largest of these products, not the largest p or scale: a slot whose values are large and
+// whose weight is next to nothing, or the other way round, takes no bits from the others.
 //
 // p is rounded to float16 (as the matrix instruction needs it): 2^-11 relative per term, no
 // more than the rounding of the output itself. Everything else is float32.
@@ -257,6 +257,16 @@ __device__ __forceinline__ float column_max(float x) {
 // and float16 holds such p with the same relative precision.
 constexpr float kSlack = 8.0f;
 
+// INT4: the products of p and value scales are float16 of up to 2^15. A column's m is set so that
+// its largest product lies in [2^(kLift - 1), 2^kLift), and again where one outgrows 2^15;
+// smaller ones are off by 2^-11 relative or half a subnormal step, 2^-25, at most: 2^-36 of the largest.
+// Where all products are small m is kDeepest below the largest logit, and what a product loses
+// is at most 2^-25 2^-kDeepest of a weight of 1, times a code: 7 x 2^-45 of the output, which
+// is float16. p itself stays below 2^kFar; its sum and that of the products are float32.
+constexpr int kLift = 12;
+constexpr int kDeepest = 20;
+constexpr float kFar = 24.0f;
+
 // The weights of four slots: the sum over `rows` rows, ld apart, of 2^(logit - top) inv of the row;
 // at(g): top and inv of row g.
 template <typename At>
@@ -280,6 +290,14 @@ __device__ __forceinline__ void add_slots(float* out, int s, int n, const float4
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     if (s + i < n) out[s + i] += add[i];
+}
+
+// log(2^m sum): the exponents are added before the logarithm, so that a sum far from 1 costs
+// no digits.
+__device__ __forceinline__ float log_sum(float m, float sum) {
+  if (sum == 0.0f) return -INFINITY;
+  const float e = m + (float)__builtin_amdgcn_frexp_expf(sum);
+  return (e + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(sum))) / kLog2e;
 }
 
 // top and inv of a row for slot_weights; a row without slots has logits of -inf only.
@@ -350,7 +368,6 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
   v4f o[S::kOut] = {};
   float m = -INFINITY, sum = 0.0f;
   float rounded = 0.0f;  // float16 values: the sum of p as the products take it
-  float vnorm = 0x1p-14f;  // INT4: the power of two that value scales and o are in units of
   uint8_t* tile = lds + wave * kLds;
 
   // Pages: lane i holds page page0 + i of the sequence.
@@ -491,9 +508,14 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u)
       top = larger(larger(larger(larger(top, l[u][0]), l[u][1]), l[u][2]), l[u][3]);
-    top = column_max(top) * scale;
-    if (__any(top > m + kSlack)) {
-      const float up = fmaxf(m, top);
+    bool fresh = false;  // INT4: m is to be set from the products
+    if (__any(top * scale > m + (kInt4 ? kFar : kSlack))) {
+      top = column_max(top) * scale;
+      float up = fmaxf(m, top);
+      if constexpr (kInt4) {
+        fresh = top > m + kFar;
+        up = fresh ? top : m;
+      }
       const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
       m = up;
       sum *= shrink;
@@ -501,49 +523,44 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
 #pragma unroll
       for (int j = 0; j < S::kOut; ++j) o[j] *= shrink;
     }
-    if constexpr (kInt4) {
-      // The power of two above the largest value scale so far, at least 2^-14 (its inverse is a
-      // float16 then; a smaller scale's values are below float16's normal range).
-      v2h big = __builtin_bit_cast(v2h, (uint32_t)vscale[0][0]);
-#pragma unroll
-      for (int u = 0; u < S::kBlocks / 2; ++u)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          big = __builtin_elementwise_max(big, __builtin_bit_cast(v2h, (uint32_t)vscale[u][i]));
-      const float largest = fmaxf((float)big[0], (float)big[1]);
-      if (__any(largest > vnorm)) {
-        const float all = column_max(largest);  // of the tile: the same in every column
-        const int e = __builtin_amdgcn_frexp_expf(all);
-        const float norm = __builtin_amdgcn_ldexpf(1.0f, min(e, 14));
-        if (norm > vnorm) {
-          const float shrink = vnorm / norm;  // powers of two
-          vnorm = norm;
-#pragma unroll
-          for (int j = 0; j < S::kOut; ++j) o[j] *= shrink;
-        }
-      }
-      // 1 / vnorm: for a power of two the two exponents add up to twice that of 1.
-      const _Float16 inv =
-          (_Float16)__builtin_bit_cast(float, 0x7F000000u - __builtin_bit_cast(uint32_t, vnorm));
-#pragma unroll
-      for (int u = 0; u < S::kBlocks / 2; ++u)
-        vscale[u] = __builtin_bit_cast(
-            v4u, __builtin_bit_cast(v8h, vscale[u]) * v8h{inv, inv, inv, inv, inv, inv, inv, inv});
-    }
     const float base = m == -INFINITY ? 0.0f : m;
     _Float16 p[S::kBlocks * 4];
+    float most = 0.0f;  // INT4: the lane's largest product
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
         sum += x;
-        if constexpr (kInt4)  // as a mixed fma, which takes the float16 factor as it is
-          p[4 * u + r] = (_Float16)__builtin_fmaf(
+        if constexpr (kInt4) {  // as a mixed fma, which takes the float16 factor as it is
+          l[u][r] = __builtin_fmaf(
               x, (float)__builtin_bit_cast(v8h, vscale[u / 2])[4 * (u & 1) + r], 0.0f);
-        else
+          most = larger(most, l[u][r]);
+        } else {
           p[4 * u + r] = (_Float16)x;
+        }
       }
+    if constexpr (kInt4) {
+      if (__any(fresh || most > 0x1p15f)) {
+        const float all = column_max(most);
+        int e = 0;
+        if (fresh || all > 0x1p15f)
+          e = all > 0.0f ? max(__builtin_amdgcn_frexp_expf(all) - kLift, -kDeepest) : -kDeepest;
+        const float turn = __builtin_amdgcn_ldexpf(1.0f, -e);
+        m += (float)e;
+        sum *= turn;
+#pragma unroll
+        for (int j = 0; j < S::kOut; ++j) o[j] *= turn;
+#pragma unroll
+        for (int u = 0; u < S::kBlocks; ++u)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) l[u][r] *= turn;
+      }
+#pragma unroll
+      for (int u = 0; u < S::kBlocks; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[4 * u + r] = (_Float16)l[u][r];
+    }
 
     if constexpr (!kInt4) {
 #pragma unroll
@@ -615,12 +632,12 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     __builtin_amdgcn_wave_barrier();
   }
 
-  // The waves' sums meet in LDS. o is put in proportion to sum: in units of vnorm (INT4), or from
-  // the sum of the rounded p, so that what rounding did to a weight it also did to the sum
-  // that divides it (one weight that outgrows all others is then exact).
+  // The waves' sums meet in LDS. Float16 values: o is put in proportion to sum from the sum of the
+  // rounded p, so that what rounding did to a weight it also did to the sum that divides it (one
+  // weight that outgrows all others is then exact).
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
-  float unit_o = vnorm;
+  float unit_o = 1.0f;
   if constexpr (!kInt4) {
     rounded += __shfl_xor(rounded, 16);
     rounded += __shfl_xor(rounded, 32);
@@ -637,8 +654,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
             v4h{(_Float16)x[0], (_Float16)x[1], (_Float16)x[2], (_Float16)x[3]};
       }
       if (quarter == 0) {
-        if (a.lse)
-          a.lse[bh] = sum != 0.0f ? (m + __builtin_amdgcn_logf(sum)) / kLog2e : -INFINITY;
+        if (a.lse) a.lse[bh] = log_sum(m, sum);
         if (plan.stats)
           plan.stats[(size_t)piece.index * a.heads + head0 + col] = make_float2(m, sum);
       }
@@ -673,8 +689,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     row_stats[0][col] = weight_row(top, total);
   if (threadIdx.x < rows) {
     const size_t bh = (size_t)b * a.heads + head0 + threadIdx.x;
-    if (whole && a.lse)
-      a.lse[bh] = total != 0.0f ? (top + __builtin_amdgcn_logf(total)) / kLog2e : -INFINITY;
+    if (whole && a.lse) a.lse[bh] = log_sum(top, total);
     if (plan.stats)
       plan.stats[(size_t)piece.index * a.heads + head0 + threadIdx.x] = make_float2(top, total);
   }
@@ -780,8 +795,7 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = (_Float16)(some ? v[i] / all.y : 0.0f);
     *reinterpret_cast<v4h*>(a.out + (size_t)bh * D + 4 * d4) = y;
-    if (d4 == 0 && a.lse)
-      a.lse[bh] = some ? (all.x + __builtin_amdgcn_logf(all.y)) / kLog2e : -INFINITY;
+    if (d4 == 0 && a.lse) a.lse[bh] = log_sum(all.x, all.y);
     return;
   }
   const int id = blockIdx.x - joins;
