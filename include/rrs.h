@@ -650,7 +650,9 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
  *                 a context are joined.
  *   workspace   : at least rrs_paged_attention_workspace_bytes; contents ignored.
  *   scale       : finite, else RRS_ERR_FLAGS.
- * Logits, softmax and sums in float32; weights are rounded to float16 for the product with V. A
+ * Logits, softmax and sums in float32; for the product with V the weights (RRS_KV_INT4: times the
+ * value's scale) are rounded to float16 in units of their own: off by 2^-11 relative, or by 2^-36 of the
+ * head's largest one where that is more. A
  * sequence's result depends on the other sequences only through their lengths, which decide where the
  * sums are cut; it repeats bit for bit for the same lengths and max_length.
  */

@@ -24,8 +24,10 @@
 // the largest of these products, not the largest p or scale: a slot whose values are large and
 // whose weight is next to nothing, or the other way round, takes no bits from the others.
 //
-// p is rounded to float16 (as the matrix instruction needs it): 2^-11 relative per term, no
-// more than the rounding of the output itself. Everything else is float32.
+// p is rounded to float16 (as the matrix instruction needs it), in units that leave the largest
+// weight 2^12 or more: off by 2^-11 relative, or by 2^-37 of the largest weight where that is more
+// (INT4, with the value's scale: 2^-36 of the largest product). The matrix instruction and the sum of
+// the rounded p keep float16's subnormals. Everything else is float32.
 //
 // Measured (kernel time; bytes of K, V and scales read): 256 sequences of 1 to 4096 slots, 8 KV
 // heads of 128, float16, 383 us (5.6 TB/s); one of 131071 slots 94 us (5.7 TB/s); 49 sequences of
@@ -253,17 +255,19 @@ __device__ __forceinline__ float column_max(float x) {
                __builtin_bit_cast(float, (uint32_t)b[1]));
 }
 
-// p may grow to 2^kSlack before the sums are rescaled to a new maximum: few tiles then do it,
-// and float16 holds such p with the same relative precision.
-constexpr float kSlack = 8.0f;
-
-// INT4: the products of p and value scales are float16 of up to 2^15. A column's m is set so that
-// its largest product lies in [2^(kLift - 1), 2^kLift), and again where one outgrows 2^15;
+// float16 values: p is taken into the products as float16 of up to 2^15. A column's m is set kLift
+// below its largest logit, and again where p would outgrow 2^kRoom: few tiles do that, and the largest
+// p is 2^kLift at least, so that smaller ones are off by 2^-11 relative or half a subnormal
+// step, 2^-25, at most: 2^-37 of the largest.
+//
+// INT4: the products of p and value scales are such float16 numbers. m is set so that
+// the largest product lies in [2^(kLift - 1), 2^kLift), and again where one outgrows 2^15;
 // smaller ones are off by 2^-11 relative or half a subnormal step, 2^-25, at most: 2^-36 of the largest.
 // Where all products are small m is kDeepest below the largest logit, and what a product loses
 // is at most 2^-25 2^-kDeepest of a weight of 1, times a code: 7 x 2^-45 of the output, which
 // is float16. p itself stays below 2^kFar; its sum and that of the products are float32.
 constexpr int kLift = 12;
+constexpr float kRoom = 15.0f;
 constexpr int kDeepest = 20;
 constexpr float kFar = 24.0f;
 
@@ -509,9 +513,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     for (int u = 0; u < S::kBlocks; ++u)
       top = larger(larger(larger(larger(top, l[u][0]), l[u][1]), l[u][2]), l[u][3]);
     bool fresh = false;  // INT4: m is to be set from the products
-    if (__any(top * scale > m + (kInt4 ? kFar : kSlack))) {
+    if (__any(top * scale > m + (kInt4 ? kFar : kRoom))) {
       top = column_max(top) * scale;
-      float up = fmaxf(m, top);
+      float up = fmaxf(m, top - kLift);
       if constexpr (kInt4) {
         fresh = top > m + kFar;
         up = fresh ? top : m;

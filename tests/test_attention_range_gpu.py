@@ -76,3 +76,9 @@ def _sink(B, heads, hk, n, octaves, fmt):
 @pytest.mark.parametrize("B,heads,hk,n", WAYS)
 def test_int4_sink_without_a_value(B, heads, hk, n, octaves):
     _sink(B, heads, hk, n, octaves, "int4")
+
+
+@pytest.mark.parametrize("octaves", OCTAVES)
+@pytest.mark.parametrize("B,heads,hk,n", WAYS)
+def test_f16_sink_without_a_value(B, heads, hk, n, octaves):
+    _sink(B, heads, hk, n, octaves, "f16")
