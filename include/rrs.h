@@ -566,7 +566,8 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *  - k_scale, v_scale (RRS_KV_INT4; else NULL): pages x kv_heads x page_size float16,
  *    one per row: s = fp16(max |x| / 7), q = clamp(rint(x / s), -7, 7) of the
  *    float16 values x (codes 0 where s = 0); the row stands for q s. The scale is rounded
- *    before it divides, so codes and scale are exact functions of x.
+ *    before it divides, so codes and scale are exact functions of x. Of a row with a
+ *    value that is not finite the scale is not either and the codes are 0: the row stands for NaN.
  *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
  *    read. No page belongs to two rows of the table in a call that writes the cache.
  * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,

@@ -41,18 +41,23 @@ __device__ __forceinline__ void unpack_halves(const uint4& w, float (&v)[8]) {
   }
 }
 
+// NaN if one of them is: it has to reach the row's scale.
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+
 __device__ __forceinline__ float max_abs(const float (&v)[8]) {
   float m = 0.0f;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]));
+  for (int e = 0; e < 8; ++e) m = larger(m, fabsf(v[e]));
   return m;
 }
 
 // q = clamp(rint(x / s), -7, 7), eight codes of 4 bits. The division is the IEEE one: s has 11
 // bits, so no quotient is close to a half integer without being one, and the code is
-// that of the real quotient.
+// that of the real quotient. Codes of 0 under a scale that is not finite: the row reads as NaN.
 __device__ __forceinline__ uint32_t codes8(const float (&v)[8], float s) {
-  if (s == 0.0f) return 0u;
+  if (!(s > 0.0f && s < INFINITY)) return 0u;
   uint32_t w = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
@@ -190,9 +195,9 @@ __global__ void __launch_bounds__(kThreads) rope_kv_append_kernel(RopeArgs a, Kv
         x[e] = (float)(_Float16)x[e];
         y[e] = (float)(_Float16)y[e];
       }
-      float top = fmaxf(max_abs(x), max_abs(y));
+      float top = larger(max_abs(x), max_abs(y));
 #pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+      for (int d = 1; d < kLanes; d <<= 1) top = larger(top, __shfl_xor(top, d));
       const _Float16 scale = (_Float16)__fdiv_rn(top, 7.0f);
       uint8_t* dst = (value ? c.v : c.k) + row * (D / 2);
       *reinterpret_cast<uint32_t*>(dst + o0 / 2) = codes8(x, (float)scale);
