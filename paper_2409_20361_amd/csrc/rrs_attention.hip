@@ -285,6 +285,21 @@ __device__ __forceinline__ float4 slot_weights(const float* logits, int ld, int 
     w.z += __builtin_amdgcn_exp2f(l.z - r.x) * r.y;
     w.w += __builtin_amdgcn_exp2f(l.w - r.x) * r.y;
   }
+  // Of a row with an inv of NaN the slots that take part get NaN; those under the mask (a logit of
+  // -inf) got it, too. Summed again without them, since a condition in the loop above keeps its loads from
+  // running ahead (40 heads over 6 x 1057 slots: 14.5 -> 22.5 us).
+  if (w.x != w.x || w.y != w.y || w.z != w.z || w.w != w.w) {
+    float x[4] = {};
+    for (int g = 0; g < rows; ++g) {
+      const float2 r = at(g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float l = logits[(size_t)g * ld + i];
+        if (l != -INFINITY) x[i] += __builtin_amdgcn_exp2f(l - r.x) * r.y;
+      }
+    }
+    w = make_float4(x[0], x[1], x[2], x[3]);
+  }
   return w;
 }
 
@@ -304,9 +319,10 @@ __device__ __forceinline__ float log_sum(float m, float sum) {
   return (e + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(sum))) / kLog2e;
 }
 
-// top and inv of a row for slot_weights; a row without slots has logits of -inf only.
+// top and inv of a row for slot_weights; a row without slots has logits of -inf only, one whose sum is
+// NaN an inv of NaN.
 __device__ __forceinline__ float2 weight_row(float top, float total) {
-  return total > 0.0f ? make_float2(top, 1.0f / total) : make_float2(0.0f, 0.0f);
+  return total != 0.0f ? make_float2(top, 1.0f / total) : make_float2(0.0f, 0.0f);
 }
 
 // Grid: pieces x KV heads x row blocks. The row blocks of a piece and head read the same rows: they

@@ -43,3 +43,30 @@ def test_int4_append_keeps_rows_that_are_not_finite(D, bad):
         assert torch.equal(b[0][~nan.cuda()], a[0][~nan.cuda()]), name
     out = rrs.paged_attention(want[M - 1:, :hk].contiguous().cuda(), cache, n, M)
     assert out.isnan().all()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4"])
+@pytest.mark.parametrize("B,lengths", [(2, [40, 33]), (2, [9000, 7000]), (200, [40, 33])])
+def test_not_a_number_reaches_the_weights(B, lengths, fmt):
+    """A head whose softmax is NaN: the slots that take part get a NaN weight, no others do."""
+    gen = torch.Generator().manual_seed(18)
+    hk, D, page = 8, 128, 16
+    lengths = [lengths[b % 2] for b in range(B)]
+    top = max(lengths)
+    cache = make_cache(gen, B, top, hk, D, page, fmt)
+    Q = torch.randn((B, 2 * hk, D), generator=gen).half().cuda()
+    mask = (torch.rand((B, cache.capacity), generator=gen) < 0.8).cuda()
+    t = lengths[1] - 2   # of sequence 1, KV head 3
+    mask[1, t] = True
+    where = (cache.table[1, t // page].long(), 3, t % page)
+    (cache.k if fmt == "f16" else cache.k_scale)[where] = math.nan
+    w = torch.rand((B, hk, cache.capacity), generator=gen).cuda()
+    w0 = w.clone()
+    rrs.paged_attention(Q, cache, torch.tensor(lengths, dtype=torch.int32).cuda(), top, mask=mask,
+                        weights=w)
+    live = mask & (torch.arange(cache.capacity).cuda() < torch.tensor(lengths).cuda()[:, None])
+    hit = torch.zeros((B, hk, 1), dtype=torch.bool, device="cuda")
+    hit[1, 3] = True
+    assert torch.equal(w.isnan(), live[:, None] & hit)
+    dead = (~live)[:, None].expand_as(w)
+    assert torch.equal(w[dead], w0[dead])
