@@ -51,28 +51,39 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
   return THPVariable_Unpack(o);
 }
 
-const at::Tensor& gpu_tensor(PyObject* o, const char* name, at::ScalarType dtype) {
+// The GPU that a call is for: that of the tensor which says so.
+at::Device gpu_of(PyObject* o, const char* name) {
   const at::Tensor& t = tensor(o, name);
   if (!t.is_cuda())
     raise(PyExc_ValueError,
           std::string(name) + " must be a GPU tensor, got " + t.device().str());
+  return t.device();
+}
+
+const at::Tensor& gpu_tensor(PyObject* o, const char* name, at::ScalarType dtype, at::Device on) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.device() != on)
+    raise(PyExc_ValueError,
+          std::string(name) + " must be on " + on.str() + ", got " + t.device().str());
   if (t.scalar_type() != dtype)
     raise(PyExc_TypeError, std::string(name) + " must be " + text(dtype) + ", got " +
                                text(t.scalar_type()));
   return t;
 }
 
-// The device pointer of a contiguous GPU tensor of this type and shape.
-void* dev(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape) {
-  const at::Tensor& t = gpu_tensor(o, name, dtype);
+// The device pointer of a contiguous tensor of this type and shape on this GPU.
+void* dev(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape,
+          at::Device on) {
+  const at::Tensor& t = gpu_tensor(o, name, dtype, on);
   if (t.sizes() != shape)
     raise(PyExc_ValueError, std::string(name) + " must have shape " + text(shape) + ", got " +
                                 text(t.sizes()));
   if (!t.is_contiguous()) raise(PyExc_ValueError, std::string(name) + " must be contiguous");
   return t.data_ptr();
 }
-void* dev_or_null(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape) {
-  return o == Py_None ? nullptr : dev(o, name, dtype, shape);
+void* dev_or_null(PyObject* o, const char* name, at::ScalarType dtype, at::IntArrayRef shape,
+                  at::Device on) {
+  return o == Py_None ? nullptr : dev(o, name, dtype, shape, on);
 }
 
 int to_int(PyObject* o, const char* name) {
@@ -103,12 +114,12 @@ PyObject* check(rrs_status s, const char* where, PyObject* result) {
   return nullptr;
 }
 
-// The tensor's device made current for the call, and its current stream.
+// The call's device made current, and its current stream.
 struct Launch {
   c10::DeviceGuard guard;
   void* stream;
-  explicit Launch(const at::Tensor& t)
-      : guard(t.device()), stream(c10::hip::getCurrentHIPStream(t.get_device()).stream()) {}
+  explicit Launch(at::Device on)
+      : guard(on), stream(c10::hip::getCurrentHIPStream(on.index()).stream()) {}
 };
 
 struct Cache {
@@ -116,20 +127,20 @@ struct Cache {
   int64_t heads, dim, sequences, capacity;
 
   // a: k, v, table, k_scale, v_scale
-  explicit Cache(PyObject* const* a) {
+  Cache(PyObject* const* a, at::Device on) {
     const at::Tensor& k = tensor(a[0], "k");
     const at::Tensor& table = tensor(a[2], "table");
     if (k.dim() != 4 || table.dim() != 2)
       raise(PyExc_ValueError, "cache: k must have 4 dimensions and table 2");
     const auto s = k.sizes();
-    c.table = static_cast<const int32_t*>(dev(a[2], "table", at::kInt, table.sizes()));
+    c.table = static_cast<const int32_t*>(dev(a[2], "table", at::kInt, table.sizes(), on));
     const bool int4 = a[3] != Py_None || a[4] != Py_None;
     const auto type = int4 ? at::kByte : at::kHalf;
-    c.k = dev(a[0], "k", type, s);
-    c.v = dev(a[1], "v", type, s);
+    c.k = dev(a[0], "k", type, s, on);
+    c.v = dev(a[1], "v", type, s, on);
     if (int4) {
-      c.k_scale = dev(a[3], "k_scale", at::kHalf, s.slice(0, 3));
-      c.v_scale = dev(a[4], "v_scale", at::kHalf, s.slice(0, 3));
+      c.k_scale = dev(a[3], "k_scale", at::kHalf, s.slice(0, 3), on);
+      c.v_scale = dev(a[4], "v_scale", at::kHalf, s.slice(0, 3), on);
     }
     for (const int64_t x : {s[0], s[1], s[2], 2 * s[3], table.size(0), table.size(1)})
       if (x > INT32_MAX) raise(PyExc_ValueError, "cache: a size is out of range");
@@ -158,15 +169,15 @@ struct Workspace {
   at::Tensor keep;
   void* p = nullptr;
   size_t bytes = 0;
-  Workspace(PyObject* o, size_t need, const at::Tensor& like) {
+  Workspace(PyObject* o, size_t need, at::Device on) {
     if (o != Py_None) {
       const at::Tensor& t = tensor(o, "workspace");
-      if (t.device() != like.device() || !t.is_contiguous())
-        raise(PyExc_ValueError, "workspace must be contiguous and on " + like.device().str());
+      if (t.device() != on || !t.is_contiguous())
+        raise(PyExc_ValueError, "workspace must be contiguous and on " + on.str());
       p = t.data_ptr();
       bytes = t.nbytes();
     } else if (need > 0) {
-      keep = at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+      keep = at::empty({(int64_t)need}, at::TensorOptions().device(on).dtype(at::kByte));
       p = keep.data_ptr();
       bytes = need;
     }
@@ -191,11 +202,12 @@ PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 // qkv, positions, rope, cache (5), seq, slot, heads, sections, interleaved, weights, slot_pos, out
 RRS_CALL(rope_kv_append) {
   arguments(n, 16, "rope_kv_append");
-  const Cache cache(a + 3);
+  const at::Device on = gpu_of(a[0], "qkv");
+  const Cache cache(a + 3, on);
   const int heads = to_int(a[10], "heads");
   const int64_t width = (heads + 2 * cache.heads) * cache.dim;
   const at::Tensor& qkv = tensor(a[0], "qkv");
-  if (!qkv.is_cuda() || qkv.scalar_type() != at::kHalf || qkv.dim() != 2 ||
+  if (qkv.scalar_type() != at::kHalf || qkv.dim() != 2 ||
       qkv.size(1) != width || qkv.stride(1) != 1)
     raise(PyExc_ValueError, "qkv must be a float16 GPU tensor (M, " + std::to_string(width) +
                                 ") with unit column stride");
@@ -203,11 +215,11 @@ RRS_CALL(rope_kv_append) {
   if (M > INT32_MAX) raise(PyExc_ValueError, "qkv has too many rows");
   const at::Tensor& positions = tensor(a[1], "positions");
   const int64_t axes = positions.dim() == 2 ? positions.size(1) : 0;
-  const void* pp = dev(a[1], "positions", at::kInt, {M, axes});
-  const at::Tensor& rope = gpu_tensor(a[2], "rope", at::kFloat);
+  const void* pp = dev(a[1], "positions", at::kInt, {M, axes}, on);
+  const at::Tensor& rope = gpu_tensor(a[2], "rope", at::kFloat, on);
   if (rope.dim() != 2 || rope.size(0) > INT32_MAX || rope.size(1) > INT32_MAX)
     raise(PyExc_ValueError, "rope must have shape (positions, rotary dim)");
-  dev(a[2], "rope", at::kFloat, rope.sizes());
+  dev(a[2], "rope", at::kFloat, rope.sizes(), on);
   int32_t sections[4] = {};
   if (a[11] == Py_None) {
     if (axes != 1)
@@ -228,11 +240,11 @@ RRS_CALL(rope_kv_append) {
     if (!good)
       raise(PyExc_ValueError, "sections must name " + std::to_string(axes) + " axes, at most 4");
   }
-  const void* sp = dev(a[8], "seq", at::kInt, {M});
-  const void* tp = dev(a[9], "slot", at::kInt, {M});
+  const void* sp = dev(a[8], "seq", at::kInt, {M}, on);
+  const void* tp = dev(a[9], "slot", at::kInt, {M}, on);
   const int64_t slots[3] = {cache.sequences, cache.heads, cache.capacity};
-  void* wp = dev_or_null(a[13], "weights", at::kFloat, slots);
-  void* op = dev_or_null(a[14], "slot_pos", at::kInt, slots);
+  void* wp = dev_or_null(a[13], "weights", at::kFloat, slots, on);
+  void* op = dev_or_null(a[14], "slot_pos", at::kInt, slots, on);
   at::Tensor made;
   void* qp;
   if (a[15] == Py_None) {
@@ -240,9 +252,9 @@ RRS_CALL(rope_kv_append) {
     made = at::empty({M, heads, cache.dim}, qkv.options());
     qp = made.data_ptr();
   } else {
-    qp = dev(a[15], "out", at::kHalf, {M, heads, cache.dim});
+    qp = dev(a[15], "out", at::kHalf, {M, heads, cache.dim}, on);
   }
-  const Launch launch(qkv);
+  const Launch launch(on);
   const rrs_status s = rrs_rope_kv_append(
       qkv.data_ptr(), M > 1 ? qkv.stride(0) : width, (int)M, heads,
       static_cast<const int32_t*>(pp), (int)axes, sections,
@@ -257,21 +269,22 @@ RRS_CALL(rope_kv_append) {
 // Q, cache (5), lengths, max_length, scale, mask, weights, return_lse, workspace, out
 RRS_CALL(paged_attention) {
   arguments(n, 14, "paged_attention");
-  const Cache cache(a + 1);
+  const at::Device on = gpu_of(a[0], "Q");
+  const Cache cache(a + 1, on);
   const at::Tensor& Q = tensor(a[0], "Q");
   const int64_t B = cache.sequences, heads = Q.dim() == 3 ? Q.size(1) : 0;
   if (heads > INT32_MAX) raise(PyExc_ValueError, "Q has too many heads");
   const int64_t shape[3] = {B, heads, cache.dim};
-  const void* qp = dev(a[0], "Q", at::kHalf, shape);
-  const void* lp = dev(a[6], "lengths", at::kInt, {B});
+  const void* qp = dev(a[0], "Q", at::kHalf, shape, on);
+  const void* lp = dev(a[6], "lengths", at::kInt, {B}, on);
   const int top = cache.bound(a[7]);
   double scale = 1.0 / std::sqrt((double)cache.dim);
   if (a[8] != Py_None) {
     scale = PyFloat_AsDouble(a[8]);
     if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
   }
-  const void* mp = dev_or_null(a[9], "mask", at::kBool, {B, cache.capacity});
-  void* wp = dev_or_null(a[10], "weights", at::kFloat, {B, cache.heads, cache.capacity});
+  const void* mp = dev_or_null(a[9], "mask", at::kBool, {B, cache.capacity}, on);
+  void* wp = dev_or_null(a[10], "weights", at::kFloat, {B, cache.heads, cache.capacity}, on);
   const bool want_lse = to_bool(a[11]);
   at::Tensor made, lse;
   void* yp;
@@ -279,15 +292,15 @@ RRS_CALL(paged_attention) {
     made = at::empty(shape, Q.options());
     yp = made.data_ptr();
   } else {
-    yp = dev(a[13], "out", at::kHalf, shape);
+    yp = dev(a[13], "out", at::kHalf, shape, on);
   }
   if (want_lse) lse = at::empty({B, heads}, Q.options().dtype(at::kFloat));
   const size_t need =
       a[12] == Py_None
           ? rrs_paged_attention_workspace_bytes(&cache.c, (int)heads, top, wp != nullptr)
           : 0;
-  const Workspace ws(a[12], need, Q);
-  const Launch launch(Q);
+  const Workspace ws(a[12], need, on);
+  const Launch launch(on);
   const rrs_status s = rrs_paged_attention(
       qp, (int)heads, &cache.c, static_cast<const int32_t*>(lp), top, (float)scale,
       static_cast<const uint8_t*>(mp), static_cast<float*>(wp), yp,
@@ -305,7 +318,7 @@ RRS_CALL(paged_attention) {
 // cache (5), heads, max_length, with_weights
 RRS_CALL(paged_attention_workspace_bytes) {
   arguments(n, 8, "paged_attention_workspace_bytes");
-  const Cache cache(a);
+  const Cache cache(a, gpu_of(a[0], "k"));
   return PyLong_FromSize_t(rrs_paged_attention_workspace_bytes(
       &cache.c, to_int(a[5], "heads"), to_int(a[6], "max_length"), to_bool(a[7])));
 }
@@ -313,17 +326,21 @@ RRS_CALL(paged_attention_workspace_bytes) {
 // cache (5), lengths, weights, slot_pos, keep_from, budget, max_length, out, workspace
 RRS_CALL(kv_evict) {
   arguments(n, 13, "kv_evict");
-  const Cache cache(a);
+  const at::Device on = gpu_of(a[5], "lengths");
+  const Cache cache(a, on);
   const int64_t B = cache.sequences, h = cache.heads, cap = cache.capacity;
-  const void* lp = dev(a[5], "lengths", at::kInt, {B});
-  const void* wp = dev(a[6], "weights", at::kFloat, {B, h, cap});
-  const void* pp = dev(a[7], "slot_pos", at::kInt, {B, h, cap});
-  const void* fp = dev(a[8], "keep_from", at::kInt, {B});
+  const void* lp = dev(a[5], "lengths", at::kInt, {B}, on);
+  const void* wp = dev(a[6], "weights", at::kFloat, {B, h, cap}, on);
+  const void* pp = dev(a[7], "slot_pos", at::kInt, {B, h, cap}, on);
+  const void* fp = dev(a[8], "keep_from", at::kInt, {B}, on);
   const int budget = to_int(a[9], "budget"), top = cache.bound(a[10]);
   if (budget < 1 || budget > cap)
     raise(PyExc_ValueError, "budget must be in [1, " + std::to_string(cap) + "], got " +
                                 std::to_string(budget));
   const at::Tensor& lengths = THPVariable_Unpack(a[5]);
+  const size_t need =
+      a[12] == Py_None ? rrs_kv_evict_workspace_bytes(&cache.c, top, budget) : 0;
+  const Workspace ws(a[12], need, on);
   at::Tensor made[4];
   void* out[4];
   if (a[11] == Py_None) {
@@ -335,17 +352,14 @@ RRS_CALL(kv_evict) {
   } else {
     if (!PyTuple_Check(a[11]) || PyTuple_GET_SIZE(a[11]) != 4)
       raise(PyExc_TypeError, "out must be a tuple (kept, lengths, weights, slot_pos)");
-    out[0] = dev(PyTuple_GET_ITEM(a[11], 0), "kept", at::kInt, {B, h, budget});
-    out[1] = dev(PyTuple_GET_ITEM(a[11], 1), "new_lengths", at::kInt, {B});
-    out[2] = dev(PyTuple_GET_ITEM(a[11], 2), "weights_out", at::kFloat, {B, h, cap});
-    out[3] = dev(PyTuple_GET_ITEM(a[11], 3), "pos_out", at::kInt, {B, h, cap});
+    out[0] = dev(PyTuple_GET_ITEM(a[11], 0), "kept", at::kInt, {B, h, budget}, on);
+    out[1] = dev(PyTuple_GET_ITEM(a[11], 1), "new_lengths", at::kInt, {B}, on);
+    out[2] = dev(PyTuple_GET_ITEM(a[11], 2), "weights_out", at::kFloat, {B, h, cap}, on);
+    out[3] = dev(PyTuple_GET_ITEM(a[11], 3), "pos_out", at::kInt, {B, h, cap}, on);
     if (out[1] == lp || out[2] == wp || out[3] == pp)
       raise(PyExc_ValueError, "kv_evict: outputs must not be inputs");
   }
-  const size_t need =
-      a[12] == Py_None ? rrs_kv_evict_workspace_bytes(&cache.c, top, budget) : 0;
-  const Workspace ws(a[12], need, lengths);
-  const Launch launch(lengths);
+  const Launch launch(on);
   const rrs_status s = rrs_kv_evict(
       &cache.c, static_cast<const int32_t*>(lp), top, static_cast<const float*>(wp),
       static_cast<const int32_t*>(pp), static_cast<const int32_t*>(fp), budget,
@@ -368,7 +382,7 @@ RRS_CALL(kv_evict) {
 // cache (5), max_length, budget
 RRS_CALL(kv_evict_workspace_bytes) {
   arguments(n, 7, "kv_evict_workspace_bytes");
-  const Cache cache(a);
+  const Cache cache(a, gpu_of(a[0], "k"));
   return PyLong_FromSize_t(rrs_kv_evict_workspace_bytes(&cache.c, to_int(a[5], "max_length"),
                                                         to_int(a[6], "budget")));
 }
@@ -376,9 +390,10 @@ RRS_CALL(kv_evict_workspace_bytes) {
 // cache (5), lengths, max_length, out
 RRS_CALL(kv_read) {
   arguments(n, 8, "kv_read");
-  const Cache cache(a);
+  const at::Device on = gpu_of(a[5], "lengths");
+  const Cache cache(a, on);
   const int64_t B = cache.sequences;
-  const void* lp = dev(a[5], "lengths", at::kInt, {B});
+  const void* lp = dev(a[5], "lengths", at::kInt, {B}, on);
   const at::Tensor& lengths = THPVariable_Unpack(a[5]);
   const int top = cache.bound(a[6]);
   if (top < 1 || top > cache.capacity)
@@ -395,10 +410,10 @@ RRS_CALL(kv_read) {
   } else {
     if (!PyTuple_Check(a[7]) || PyTuple_GET_SIZE(a[7]) != 2)
       raise(PyExc_TypeError, "out must be a tuple (K, V)");
-    out[0] = dev(PyTuple_GET_ITEM(a[7], 0), "K", at::kHalf, shape);
-    out[1] = dev(PyTuple_GET_ITEM(a[7], 1), "V", at::kHalf, shape);
+    out[0] = dev(PyTuple_GET_ITEM(a[7], 0), "K", at::kHalf, shape, on);
+    out[1] = dev(PyTuple_GET_ITEM(a[7], 1), "V", at::kHalf, shape, on);
   }
-  const Launch launch(lengths);
+  const Launch launch(on);
   const rrs_status s = rrs_kv_read(&cache.c, static_cast<const int32_t*>(lp), top, out[0], out[1],
                                    launch.stream);
   if (s != RRS_OK) return check(s, "rrs_kv_read", nullptr);
