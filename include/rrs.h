@@ -679,9 +679,11 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
  *                               j's token came from; -1 from min(n, budget) on.
  *   new_lengths           out : sequences int32, min(n, budget).
  *   weights_out, pos_out  out : as weights and slot_pos, of the moved slots; 0 and -1 from
- *                               new_lengths[b] on. They must not overlap the inputs.
+ *                               new_lengths[b] on.
  *   workspace                 : at least rrs_kv_evict_workspace_bytes (0 up to 16384 slots: may
  *                               be NULL); contents ignored.
+ * The four outputs and the workspace must overlap neither an input (any of them: keep_from is read
+ * while new_lengths is written) nor the cache nor each other.
  * k, v and the scales are moved in place. Pages past the new length are the caller's to reuse.
  */
 size_t rrs_kv_evict_workspace_bytes(const rrs_kv_cache* cache, int max_length, int budget);

@@ -137,7 +137,7 @@ def kv_evict(cache: KVCache, lengths: torch.Tensor, weights: torch.Tensor, slot_
     weights, slot_pos: (sequences, KV heads, capacity) float32 / int32; keep_from: (sequences,)
     int32, tokens at positions from it on are kept first. Returns (kept, lengths, weights,
     slot_pos) of the cache after the move (include/rrs.h, rrs_kv_evict), new tensors or `out`;
-    none of them may be an input."""
+    none of them may overlap an input, the cache, the workspace or another."""
     return (_module or _load()).kv_evict(*cache, lengths, weights, slot_pos, keep_from, budget,
                                          max_length, out, workspace)
 

@@ -184,6 +184,17 @@ struct Workspace {
   }
 };
 
+// The memory of an argument, for calls whose outputs may not share any with what they still read.
+struct Span {
+  const char* name;
+  const void* p;
+  size_t bytes;
+  bool meets(const Span& o) const {
+    const char *a = static_cast<const char*>(p), *b = static_cast<const char*>(o.p);
+    return bytes > 0 && o.bytes > 0 && a < b + o.bytes && b < a + bytes;
+  }
+};
+
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 
 #define RRS_CALL(name)                                                              \
@@ -338,8 +349,7 @@ RRS_CALL(kv_evict) {
     raise(PyExc_ValueError, "budget must be in [1, " + std::to_string(cap) + "], got " +
                                 std::to_string(budget));
   const at::Tensor& lengths = THPVariable_Unpack(a[5]);
-  const size_t need =
-      a[12] == Py_None ? rrs_kv_evict_workspace_bytes(&cache.c, top, budget) : 0;
+  const size_t need = rrs_kv_evict_workspace_bytes(&cache.c, top, budget);
   const Workspace ws(a[12], need, on);
   at::Tensor made[4];
   void* out[4];
@@ -356,8 +366,31 @@ RRS_CALL(kv_evict) {
     out[1] = dev(PyTuple_GET_ITEM(a[11], 1), "new_lengths", at::kInt, {B}, on);
     out[2] = dev(PyTuple_GET_ITEM(a[11], 2), "weights_out", at::kFloat, {B, h, cap}, on);
     out[3] = dev(PyTuple_GET_ITEM(a[11], 3), "pos_out", at::kInt, {B, h, cap}, on);
-    if (out[1] == lp || out[2] == wp || out[3] == pp)
-      raise(PyExc_ValueError, "kv_evict: outputs must not be inputs");
+  }
+  // The kernels read the inputs and the cache while they write, in any order.
+  if (a[11] != Py_None || a[12] != Py_None) {
+    const size_t row = (size_t)B * h, all = row * cap * 4, pool = THPVariable_Unpack(a[0]).nbytes();
+    const size_t scales = a[3] == Py_None ? 0 : THPVariable_Unpack(a[3]).nbytes();
+    const Span spans[] = {{"workspace", ws.p, need},
+                          {"kept", out[0], row * budget * 4},
+                          {"new_lengths", out[1], (size_t)B * 4},
+                          {"weights_out", out[2], all},
+                          {"pos_out", out[3], all},
+                          {"lengths", lp, (size_t)B * 4},
+                          {"weights", wp, all},
+                          {"slot_pos", pp, all},
+                          {"keep_from", fp, (size_t)B * 4},
+                          {"table", cache.c.table, (size_t)B * cache.c.max_pages * 4},
+                          {"k", cache.c.k, pool},
+                          {"v", cache.c.v, pool},
+                          {"k_scale", cache.c.k_scale, scales},
+                          {"v_scale", cache.c.v_scale, scales}};
+    const size_t count = sizeof(spans) / sizeof(spans[0]);
+    for (size_t i = 0; i < 5; ++i)
+      for (size_t j = i + 1; j < count; ++j)
+        if (spans[i].meets(spans[j]))
+          raise(PyExc_ValueError, std::string("kv_evict: ") + spans[i].name + " and " +
+                                      spans[j].name + " must not overlap");
   }
   const Launch launch(on);
   const rrs_status s = rrs_kv_evict(
