@@ -572,7 +572,16 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *    read. No page belongs to two rows of the table in a call that writes the cache.
  * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,
  * sequences, max_pages, pages >= 1; sequences * kv_heads < 2^23; max_pages * page_size
- * <= 2^30. The struct is read on the host during the call only.
+ * <= 2^30. The struct is read on the host during the call only. A launch holds fewer than 2^32
+ * threads, of 256 or (kv_evict's selection) 1024 per workgroup: larger calls are RRS_ERR_SHAPE, with
+ * nothing enqueued. These are, with r = sequences * kv_heads and all quotients rounded up,
+ *  - rrs_rope_kv_append: M >= 2^24;
+ *  - rrs_paged_attention with weights, where they take a second launch (more than 16 query
+ *    heads per KV head, or sequences that are cut): r * max_length / 1024, and sequences * heads
+ *    if they are cut, >= 2^24;
+ *  - rrs_kv_evict: r >= 2^22 up to 16384 slots, r * max_length / 8192 >= 2^22 above; or 2^24 or more
+ *    workgroups of 4096 bytes of k for rows that may move;
+ *  - rrs_kv_read: r * max_length / (2048 / head_dim) >= 2^24.
  *
  * The calls below follow the conventions at the top of this file; wrong sizes are
  * RRS_ERR_SHAPE, an unknown format or flag RRS_ERR_FLAGS. Every device array is 16-byte

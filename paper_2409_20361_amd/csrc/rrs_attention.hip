@@ -918,13 +918,29 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
   return p;
 }
 
+// Workgroups of the first launch.
+long long first_grid(const Plan& p, const KvView& c, int max_length) {
+  const long long units = max_pieces(p, c, max_length) * c.heads;
+  const long long grid = p.row_blocks == 1 ? units : (units + 7) / 8 * 8 * p.row_blocks;
+  return p.team == 1 ? (grid + kWaves - 1) / kWaves : grid;
+}
+
+// Of the second those that join, and those per (sequence, KV head) that add the weights.
+struct Second {
+  int joins, blocks;
+  long long grid;
+};
+Second second_grid(const Plan& p, const KvView& c, int heads, int max_length, bool with_weights) {
+  Second s;
+  s.joins = max_pieces(p, c, max_length) > c.sequences ? c.sequences * heads : 0;
+  s.blocks = with_weights && !p.adds_weights ? (max_length - 1) / (4 * kThreads) + 1 : 0;
+  s.grid = s.joins + (long long)s.blocks * c.sequences * c.heads;
+  return s;
+}
+
 template <int D>
 hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
-  const long long pieces = max_pieces(p, c, a.max_length);
-  const long long units = pieces * c.heads;
-  long long grid = p.row_blocks == 1 ? units : (units + 7) / 8 * 8 * p.row_blocks;
-  if (p.team == 1) grid = (grid + kWaves - 1) / kWaves;
-  if (!fits_grid(grid, kThreads)) return hipErrorInvalidValue;
+  const long long grid = first_grid(p, c, a.max_length);
   const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p); };
   if (p.team == 1) {
     if (c.int4())
@@ -940,16 +956,20 @@ hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStr
              : run(attention_kernel<D, false, false, kWaves>);
   }
   if (hipError_t e = hipGetLastError()) return e;
-  const int blocks = p.logits && !p.adds_weights ? (a.max_length - 1) / (4 * kThreads) + 1 : 0;
-  const int joins = p.part ? c.sequences * a.heads : 0;
-  const long long wgs = joins + (long long)blocks * c.sequences * c.heads;
-  if (!fits_grid(wgs, kThreads)) return hipErrorInvalidValue;
-  if (wgs > 0)
-    attention_join_kernel<D><<<(unsigned)wgs, kThreads, 0, stream>>>(a, c, p, joins, blocks);
+  const Second s = second_grid(p, c, a.heads, a.max_length, a.weights != nullptr);
+  if (s.grid > 0)
+    attention_join_kernel<D><<<(unsigned)s.grid, kThreads, 0, stream>>>(a, c, p, s.joins, s.blocks);
   return hipGetLastError();
 }
 
 }  // namespace
+
+bool attention_fits(const KvView& c, int heads, int max_length, bool with_weights) {
+  size_t bytes;
+  const Plan p = make_plan(c, heads, max_length, with_weights, nullptr, &bytes);
+  return fits_grid(first_grid(p, c, max_length), kThreads) &&
+         fits_grid(second_grid(p, c, heads, max_length, with_weights).grid, kThreads);
+}
 
 size_t attention_workspace_bytes(const KvView& c, int heads, int max_length, bool with_weights) {
   size_t bytes;

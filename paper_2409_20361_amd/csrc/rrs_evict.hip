@@ -611,43 +611,55 @@ __global__ void __launch_bounds__(kMoveThreads)
 
 constexpr int kMostInRegisters = 16 * kThreads;
 
-int most_moves(const EvictArgs& a) {
-  const int over = a.max_length - a.budget;
-  return over <= 0 ? 0 : over < a.budget ? over : a.budget;
+int most_moves(int max_length, int budget) {
+  const int over = max_length - budget;
+  return over <= 0 ? 0 : over < budget ? over : budget;
 }
 
 LongPlan long_plan(int max_length, int budget, void* workspace) {
-  const int over = max_length - budget;
-  return LongPlan{(max_length - 1) / kSegment + 1,
-                  over <= 0 ? 0 : over < budget ? over : budget, static_cast<int*>(workspace)};
+  return LongPlan{(max_length - 1) / kSegment + 1, most_moves(max_length, budget),
+                  static_cast<int*>(workspace)};
+}
+
+// The launches' workgroups: of the selection, and of the moves where they are a launch of their own.
+struct Grids {
+  long long select, move;
+  int move_blocks;  // per (sequence, KV head)
+};
+Grids grids(const KvView& c, int max_length, int budget) {
+  const int row = c.int4() ? c.dim / 2 : 2 * c.dim, per_block = kMoveThreads / (row / 16);
+  const long long rows = (long long)c.sequences * c.heads;
+  const int moves = most_moves(max_length, budget);
+  const bool longer = max_length > kMostInRegisters;
+  // One round of a workgroup's lanes moves so many rows; with no more, they are moved right there.
+  const bool moves_too = !longer && moves <= 16 * kThreads / row;
+  const int of = moves_too ? 0 : longer ? moves : budget;
+  Grids g;
+  g.move_blocks = (of + per_block - 1) / per_block;
+  g.select = longer ? rows * ((max_length - 1) / kSegment + 1) : rows;
+  g.move = rows * g.move_blocks;
+  return g;
 }
 
 template <int kRow>
 hipError_t launch(const EvictArgs& a, const KvView& c, void* workspace, hipStream_t stream) {
-  constexpr int kMoveRows = kMoveThreads / (kRow / 16);
-  const int rows = c.sequences * c.heads;
-  const int moves = most_moves(a);
+  const Grids g = grids(c, a.max_length, a.budget);
+  const unsigned select = (unsigned)g.select, move = (unsigned)g.move;
   if (a.max_length > kMostInRegisters) {
     const LongPlan plan = long_plan(a.max_length, a.budget, workspace);
-    const long long grid = (long long)rows * plan.segments;
-    const int blocks = (moves + kMoveRows - 1) / kMoveRows;
-    if (!fits_grid(grid, kThreads) || !fits_grid((long long)rows * blocks, kMoveThreads))
-      return hipErrorInvalidValue;
-    if (moves > 0) {
-      evict_digit_kernel<0><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, plan);
-      evict_digit_kernel<1><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, plan);
-      evict_digit_kernel<2><<<(unsigned)grid, kThreads, 0, stream>>>(a, c, plan);
+    if (move > 0) {
+      evict_digit_kernel<0><<<select, kThreads, 0, stream>>>(a, c, plan);
+      evict_digit_kernel<1><<<select, kThreads, 0, stream>>>(a, c, plan);
+      evict_digit_kernel<2><<<select, kThreads, 0, stream>>>(a, c, plan);
     }
-    evict_list_kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, plan);
-    if (moves > 0)
+    evict_list_kernel<<<select, kThreads, 0, stream>>>(a, c, plan);
+    if (move > 0)
       evict_long_move_kernel<kRow>
-          <<<(unsigned)(rows * blocks), kMoveThreads, 0, stream>>>(a, c, plan, blocks);
+          <<<move, kMoveThreads, 0, stream>>>(a, c, plan, g.move_blocks);
     return hipGetLastError();
   }
-  if (!fits_grid(rows, kThreads)) return hipErrorInvalidValue;
-  // One round of a workgroup's lanes moves so many rows; with no more, they are moved right there.
-  const bool moves_too = moves <= 16 * kThreads / kRow;
-  const auto run = [&](auto kernel) { kernel<<<rows, kThreads, 0, stream>>>(a, c); };
+  const bool moves_too = move == 0;
+  const auto run = [&](auto kernel) { kernel<<<select, kThreads, 0, stream>>>(a, c); };
   if (a.max_length <= kThreads)
     moves_too ? run(evict_kernel<1, kRow>) : run(evict_kernel<1, 0>);
   else if (a.max_length <= 4 * kThreads)
@@ -658,14 +670,17 @@ hipError_t launch(const EvictArgs& a, const KvView& c, void* workspace, hipStrea
     moves_too ? run(evict_kernel<16, kRow>) : run(evict_kernel<16, 0>);
   if (hipError_t e = hipGetLastError()) return e;
   if (moves_too) return hipSuccess;
-  const int blocks = (a.budget + kMoveRows - 1) / kMoveRows;
-  const long long grid = (long long)blocks * rows;
-  if (!fits_grid(grid, kMoveThreads)) return hipErrorInvalidValue;
-  evict_move_kernel<kRow><<<(unsigned)grid, kMoveThreads, 0, stream>>>(a.kept, a.budget, blocks, c);
+  evict_move_kernel<kRow>
+      <<<move, kMoveThreads, 0, stream>>>(a.kept, a.budget, g.move_blocks, c);
   return hipGetLastError();
 }
 
 }  // namespace
+
+bool evict_fits(const KvView& c, int max_length, int budget) {
+  const Grids g = grids(c, max_length, budget);
+  return fits_grid(g.select, kThreads) && fits_grid(g.move, kMoveThreads);
+}
 
 size_t evict_workspace_bytes(const KvView& c, int max_length, int budget) {
   if (max_length <= kMostInRegisters) return 0;

@@ -68,8 +68,10 @@ struct RopeArgs {
   float* weights;
   int32_t* slot_pos;
 };
+bool append_fits(int M);  // ..._fits: the call's launches are within fits_grid
 hipError_t launch_rope_kv_append(const RopeArgs& a, const KvView& c, hipStream_t stream);
 
+bool read_fits(const KvView& c, int max_length);
 hipError_t launch_kv_read(const KvView& c, const int32_t* lengths, int max_length, uint16_t* K,
                           uint16_t* V, hipStream_t stream);
 
@@ -85,6 +87,7 @@ struct AttentionArgs {
   float* lse;  // or nullptr
   void* workspace;
 };
+bool attention_fits(const KvView& c, int heads, int max_length, bool with_weights);
 size_t attention_workspace_bytes(const KvView& c, int heads, int max_length, bool with_weights);
 hipError_t launch_paged_attention(const AttentionArgs& a, const KvView& c, hipStream_t stream);
 
@@ -100,6 +103,7 @@ struct EvictArgs {
   float* weights_out;
   int32_t* pos_out;
 };
+bool evict_fits(const KvView& c, int max_length, int budget);
 size_t evict_workspace_bytes(const KvView& c, int max_length, int budget);
 hipError_t launch_kv_evict(const EvictArgs& a, const KvView& c, void* workspace,
                            hipStream_t stream);

@@ -165,7 +165,7 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
   if (!qkv || !positions || !sections || !rope || !seq || !slot || !Q || any_null(cache))
     return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
-  if (!valid_shape(c) || heads < 1 || M < 1 || axes < 1 || axes > 4 || rope_rows < 1 ||
+  if (!valid_shape(c) || heads < 1 || M < 1 || !rrs::append_fits(M) || axes < 1 || axes > 4 || rope_rows < 1 ||
       rotary_dim < 16 || rotary_dim % 16 != 0 || rotary_dim > c.head_dim)
     return RRS_ERR_SHAPE;
   const int64_t width = ((int64_t)heads + 2 * (int64_t)c.kv_heads) * c.head_dim;
@@ -219,7 +219,8 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
 size_t rrs_paged_attention_workspace_bytes(const rrs_kv_cache* cache, int heads, int max_length,
                                            int with_weights) {
   if (!cache || !valid_shape(*cache) || !valid_format(*cache) || !valid_heads(*cache, heads) ||
-      max_length < 1 || max_length > capacity(*cache))
+      max_length < 1 || max_length > capacity(*cache) ||
+      !rrs::attention_fits(view(*cache), heads, max_length, with_weights != 0))
     return 0;
   return rrs::attention_workspace_bytes(view(*cache), heads, max_length, with_weights != 0);
 }
@@ -232,7 +233,8 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
   if (debug) debug_print("paged_attention", cache);
   if (!Q || !lengths || !out || any_null(cache)) return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
-  if (!valid_shape(c) || !valid_heads(c, heads) || max_length < 1 || max_length > capacity(c))
+  if (!valid_shape(c) || !valid_heads(c, heads) || max_length < 1 || max_length > capacity(c) ||
+      !rrs::attention_fits(view(c), heads, max_length, weights != nullptr))
     return RRS_ERR_SHAPE;
   if (!valid_format(c) || !std::isfinite(scale)) return RRS_ERR_FLAGS;
   const size_t need =
@@ -256,7 +258,8 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
 
 size_t rrs_kv_evict_workspace_bytes(const rrs_kv_cache* cache, int max_length, int budget) {
   if (!cache || !valid_shape(*cache) || !valid_format(*cache) || max_length < 1 ||
-      max_length > capacity(*cache) || budget < 1 || budget > capacity(*cache))
+      max_length > capacity(*cache) || budget < 1 || budget > capacity(*cache) ||
+      !rrs::evict_fits(view(*cache), max_length, budget))
     return 0;
   return rrs::evict_workspace_bytes(view(*cache), max_length, budget);
 }
@@ -272,7 +275,7 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
     return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
   if (!valid_shape(c) || max_length < 1 || max_length > capacity(c) || budget < 1 ||
-      budget > capacity(c))
+      budget > capacity(c) || !rrs::evict_fits(view(c), max_length, budget))
     return RRS_ERR_SHAPE;
   if (!valid_format(c)) return RRS_ERR_FLAGS;
   const size_t need = rrs::evict_workspace_bytes(view(c), max_length, budget);
@@ -296,7 +299,9 @@ rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int ma
   if (debug) debug_print("kv_read", cache);
   if (!lengths || !K || !V || any_null(cache)) return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
-  if (!valid_shape(c) || max_length < 1 || max_length > capacity(c)) return RRS_ERR_SHAPE;
+  if (!valid_shape(c) || max_length < 1 || max_length > capacity(c) ||
+      !rrs::read_fits(view(c), max_length))
+    return RRS_ERR_SHAPE;
   if (!valid_format(c)) return RRS_ERR_FLAGS;
   if (!aligned(c) || !is_aligned(lengths) || !is_aligned(K) || !is_aligned(V))
     return RRS_ERR_ALIGN;

@@ -239,7 +239,6 @@ template <int D>
 hipError_t append(const RopeArgs& a, const KvView& c, hipStream_t stream) {
   const int per_pass = kThreads / (D / 16);
   const int passes = (a.heads + 2 * c.heads + per_pass - 1) / per_pass;
-  if (!fits_grid(a.M, kThreads)) return hipErrorInvalidValue;
   // Few tokens: a workgroup per pass, so that all rows are in flight at once.
   const dim3 grid(a.M, a.M < 2048 && passes <= 65535 ? passes : 1);
   if (c.int4())
@@ -249,13 +248,15 @@ hipError_t append(const RopeArgs& a, const KvView& c, hipStream_t stream) {
   return hipGetLastError();
 }
 
+int read_blocks(int dim, int max_length) {  // of a (sequence, KV head)
+  return (max_length - 1) / (kThreads / (dim / 8)) + 1;
+}
+
 template <int D>
 hipError_t read(const KvView& c, const int32_t* lengths, int max_length, uint16_t* K, uint16_t* V,
                 hipStream_t stream) {
-  const int rows = kThreads / (D / 8);
-  const int blocks = (max_length - 1) / rows + 1;
+  const int blocks = read_blocks(D, max_length);
   const long long grid = (long long)blocks * c.sequences * c.heads;
-  if (!fits_grid(grid, kThreads)) return hipErrorInvalidValue;
   if (c.int4())
     kv_read_kernel<D, true>
         <<<(unsigned)grid, kThreads, 0, stream>>>(c, lengths, max_length, blocks, K, V);
@@ -266,6 +267,12 @@ hipError_t read(const KvView& c, const int32_t* lengths, int max_length, uint16_
 }
 
 }  // namespace
+
+bool append_fits(int M) { return fits_grid(M, kThreads); }
+
+bool read_fits(const KvView& c, int max_length) {
+  return fits_grid((long long)read_blocks(c.dim, max_length) * c.sequences * c.heads, kThreads);
+}
 
 hipError_t launch_rope_kv_append(const RopeArgs& a, const KvView& c, hipStream_t stream) {
   switch (c.dim) {
