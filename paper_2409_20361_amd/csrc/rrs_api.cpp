@@ -8,7 +8,6 @@
 #include <cstdlib>
 #include <cmath>
 #include <cstring>
-#include <vector>
 
 #include "rrs.h"
 #include "rrs_check.h"
@@ -17,7 +16,7 @@
 using rrs::check_device;
 using rrs::debug_check_finite_f16;
 using rrs::debug_enabled;
-using rrs::debug_fetch;
+using rrs::debug_fetch_new;
 using rrs::from_hip;
 using rrs::is_aligned;
 
@@ -51,8 +50,8 @@ rrs_status debug_fetch(void* host, const void* dev, size_t bytes, void* stream) 
 
 // Every float16 of the count at `p` is finite (exponent field not all ones).
 rrs_status debug_check_finite_f16(const void* p, size_t count, const char* what, void* stream) {
-  std::vector<uint16_t> h(count);
-  if (rrs_status e = debug_fetch(h.data(), p, count * 2, stream)) return e;
+  std::unique_ptr<uint16_t[]> h;
+  if (rrs_status e = debug_fetch_new(&h, p, count, stream)) return e;
   for (size_t i = 0; i < count; ++i) {
     if ((h[i] & 0x7C00u) == 0x7C00u) {
       std::fprintf(stderr, "[rrs] RRS_DEBUG: %s[%zu] is not finite (bits 0x%04x)\n", what, i,
@@ -127,9 +126,10 @@ float out_scale(int K, int flags) {
 // `perm` (n entries) holds every value of 0..n-1 exactly once.
 rrs_status debug_check_perm(const int32_t* perm, int n, const char* what, void* stream) {
   if (!perm) return RRS_OK;
-  std::vector<int32_t> h((size_t)n);
-  if (rrs_status e = debug_fetch(h.data(), perm, (size_t)n * 4, stream)) return e;
-  std::vector<unsigned char> seen((size_t)n, 0);
+  std::unique_ptr<int32_t[]> h;
+  if (rrs_status e = debug_fetch_new(&h, perm, (size_t)n, stream)) return e;
+  std::unique_ptr<unsigned char[]> seen(new (std::nothrow) unsigned char[(size_t)n]());
+  if (!seen) return RRS_ERR_HIP;
   for (int j = 0; j < n; ++j) {
     const int32_t v = h[(size_t)j];
     if (v < 0 || v >= n || seen[(size_t)v]) {
@@ -182,8 +182,8 @@ rrs_status debug_check_reorder_wait(int M, int K, const void* workspace, void* s
 // Every float32 of the count at `p` is finite.
 rrs_status debug_check_finite_f32(const float* p, size_t count, const char* what,
                                   void* stream) {
-  std::vector<float> h(count);
-  if (rrs_status e = debug_fetch(h.data(), p, count * 4, stream)) return e;
+  std::unique_ptr<float[]> h;
+  if (rrs_status e = debug_fetch_new(&h, p, count, stream)) return e;
   for (size_t i = 0; i < count; ++i) {
     if (!std::isfinite(h[i])) {
       std::fprintf(stderr, "[rrs] RRS_DEBUG: %s[%zu] is not finite (%g)\n", what, i,

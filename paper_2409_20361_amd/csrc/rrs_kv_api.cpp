@@ -5,7 +5,6 @@
 #include <cmath>
 #include <cstdio>
 #include <memory>
-#include <new>
 
 #include "rrs.h"
 #include "rrs_check.h"
@@ -14,7 +13,7 @@
 using rrs::check_device;
 using rrs::debug_check_finite_f16;
 using rrs::debug_enabled;
-using rrs::debug_fetch;
+using rrs::debug_fetch_new;
 using rrs::from_hip;
 using rrs::is_aligned;
 
@@ -72,18 +71,11 @@ rrs::KvView view(const rrs_kv_cache& c) {
 // to host memory on the caller's stream and wait.
 // ---------------------------------------------------------------------------
 
-rrs_status debug_fetch_i32(std::unique_ptr<int32_t[]>* h, const int32_t* p, size_t count,
-                           void* stream) {
-  h->reset(new (std::nothrow) int32_t[count]);
-  if (!*h) return RRS_ERR_HIP;
-  return debug_fetch(h->get(), p, count * 4, stream);
-}
-
 // lo <= every entry < hi.
 rrs_status debug_check_range(const int32_t* p, size_t count, int64_t lo, int64_t hi,
                              const char* what, void* stream) {
   std::unique_ptr<int32_t[]> h;
-  if (rrs_status e = debug_fetch_i32(&h, p, count, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&h, p, count, stream)) return e;
   for (size_t i = 0; i < count; ++i)
     if (h[i] < lo || h[i] >= hi) {
       std::fprintf(stderr, "[rrs] RRS_DEBUG: %s[%zu] = %d is outside [%lld, %lld)\n", what, i,
@@ -100,9 +92,9 @@ rrs_status debug_check_lengths(const rrs_kv_cache& c, const int32_t* lengths, in
                                        "lengths", stream))
     return e;
   std::unique_ptr<int32_t[]> n, t;
-  if (rrs_status e = debug_fetch_i32(&n, lengths, (size_t)c.sequences, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&n, lengths, (size_t)c.sequences, stream)) return e;
   if (rrs_status e =
-          debug_fetch_i32(&t, c.table, (size_t)c.sequences * (size_t)c.max_pages, stream))
+          debug_fetch_new(&t, c.table, (size_t)c.sequences * (size_t)c.max_pages, stream))
     return e;
   for (int b = 0; b < c.sequences; ++b)
     for (int i = 0; (int64_t)i * c.page_size < n[(size_t)b]; ++i) {
@@ -120,10 +112,10 @@ rrs_status debug_check_lengths(const rrs_kv_cache& c, const int32_t* lengths, in
 rrs_status debug_check_places(const rrs_kv_cache& c, const int32_t* seq, const int32_t* slot,
                               int M, void* stream) {
   std::unique_ptr<int32_t[]> b, s, t;
-  if (rrs_status e = debug_fetch_i32(&b, seq, (size_t)M, stream)) return e;
-  if (rrs_status e = debug_fetch_i32(&s, slot, (size_t)M, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&b, seq, (size_t)M, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&s, slot, (size_t)M, stream)) return e;
   if (rrs_status e =
-          debug_fetch_i32(&t, c.table, (size_t)c.sequences * (size_t)c.max_pages, stream))
+          debug_fetch_new(&t, c.table, (size_t)c.sequences * (size_t)c.max_pages, stream))
     return e;
   for (int m = 0; m < M; ++m) {
     const int32_t bm = b[(size_t)m], sm = s[(size_t)m];
