@@ -648,7 +648,10 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
  *   Q        in : sequences x heads x head_dim float16; heads a multiple of kv_heads, query
  *                 head h reads KV head h / (heads / kv_heads).
  *   lengths  in : sequences int32; max_length >= every length, 1 <= max_length <=
- *                 max_pages * page_size (it sizes the launch and the workspace).
+ *                 max_pages * page_size. The launches and the workspace follow from it, not from
+ *                 the lengths: short sequences under a large bound are not taken in the forms
+ *                 made for them, and with weights the workspace holds sequences * heads *
+ *                 max_length floats.
  *   mask     in : NULL, or sequences x (max_pages * page_size) bytes; slots with 0 take no
  *                 part.
  *   weights     : NULL, or sequences x kv_heads x (max_pages * page_size) float32, in
@@ -682,6 +685,7 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
  * positions, so the order of slots means nothing to attention. Nothing moves where
  * n <= budget.
  *   weights, slot_pos      in : sequences x kv_heads x (max_pages * page_size) float32 / int32.
+ *   lengths, max_length       : as above; max_length above 16384 takes the launches for long rows.
  *   keep_from              in : sequences int32.
  *   budget                    : 1 <= budget <= max_pages * page_size.
  *   kept                  out : sequences x kv_heads x budget int32: the slot that slot

@@ -116,7 +116,8 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, lengths: torch.Tensor,
     """Attention of one new token per sequence over its cache.
 
     Q: sequences x heads x head dim fp16; lengths: (sequences,) int32, the new token included;
-    max_length: a bound on them (None: the cache's capacity); scale: of the logits (None:
+    max_length: a bound on them (None: the cache's capacity), by which the launches and the workspace are
+    chosen, so best a tight one; scale: of the logits (None:
     head dim^-1/2); mask: (sequences, capacity) bool, False slots take no part; weights:
     (sequences, KV heads, capacity) float32, gains every slot's attention weight. Returns
     the output (as Q), or (output, lse) with lse (sequences, heads) float32."""
@@ -135,7 +136,8 @@ def kv_evict(cache: KVCache, lengths: torch.Tensor, weights: torch.Tensor, slot_
     """Brings every sequence down to its `budget` slots of largest weight, in place.
 
     weights, slot_pos: (sequences, KV heads, capacity) float32 / int32; keep_from: (sequences,)
-    int32, tokens at positions from it on are kept first. Returns (kept, lengths, weights,
+    int32, tokens at positions from it on are kept first; max_length: a bound on the lengths (None: the
+    cache's capacity), above 16384 with the launches for long rows. Returns (kept, lengths, weights,
     slot_pos) of the cache after the move (include/rrs.h, rrs_kv_evict), new tensors or `out`;
     none of them may overlap an input, the cache, the workspace or another."""
     return (_module or _load()).kv_evict(*cache, lengths, weights, slot_pos, keep_from, budget,

@@ -30,10 +30,10 @@
 // the rounded p keep float16's subnormals. Everything else is float32.
 //
 // Measured (kernel time; bytes of K, V and scales read): 256 sequences of 1 to 4096 slots, 8 KV
-// heads of 128, float16, 383 us (5.6 TB/s); one of 131071 slots 94 us (5.7 TB/s); 49 sequences of
-// 1 to 4096, INT4, 33.7 us (3.5 TB/s: half of the cycles issue vector instructions, half of them
-// the codes' way to float16, at three waves per SIMD; 64 of 1 to 8192 with 16 KV heads
-// 123 us, 4.6 TB/s); 8 x 40 heads over one KV head of 256 with a mask, 19 us (2.0 TB/s: latency of three or
+// heads of 128, float16, 383 us (5.7 TB/s); one of 131071 slots 94 us (5.7 TB/s); 49 sequences of
+// 1 to 4096, INT4, 33.4 us (3.6 TB/s: half of the cycles issue vector instructions, two fifths of them the
+// codes' way to float16, at three waves per SIMD; 64 of 1 to 8192 with 16 KV heads
+// 127 us with the join, 4.4 TB/s); 8 x 40 heads over one KV head of 256 with a mask, 19 us (2.0 TB/s: latency of three or
 // four tiles per wave, the rows read by three row blocks); one sequence of 117 slots, 32 heads, 5
 // us (latency); 179 x 64 heads of up to 5 slots 14 us.
 #include "rrs_device.h"
@@ -55,7 +55,12 @@ typedef __attribute__((address_space(3))) v2i* lds_v2i;
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 constexpr int kRows = 16;  // query heads per workgroup: columns of the products
-constexpr int kWidest = 256;  // sequences up to which pieces follow the lengths
+// Sequences up to which pieces follow the lengths: four lengths per lane of find_piece. Above it, as
+// below, pieces of one size for all: 100 sequences of 1 to 8192 slots, one KV head of 128, 60.3 against
+// 49.7 us; 256 of 1 to 4096 with eight 417 against 401; 65 of them 113 against 115. With eight lengths per
+// lane 300 sequences of 1 to 4096 and eight KV heads take 474 instead of 513 us, but 512 with one
+// KV head 124 instead of 115.
+constexpr int kWidest = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Sizes of a launch, and where its pieces lie in the workspace. A piece is a run of one sequence's

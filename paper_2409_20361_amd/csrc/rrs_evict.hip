@@ -5,7 +5,7 @@
 // budget-th slot is found digit by digit (histograms in LDS, 11 + 11 + 10 bits): slots above T are
 // kept, and of those at T the first ones.
 //
-// Up to 16384 slots (one_kernel) a workgroup takes a (sequence, KV head) and keeps its keys in
+// Up to 16384 slots (evict_kernel) a workgroup takes a (sequence, KV head) and keeps its keys in
 // registers: item k of lane l of wave w is slot (w items + k) 64 + l, so that ranks in slot order
 // are ballots within a wave and one sum over the waves. The weights and positions are read once, from HBM;
 // what is left is the time of a few passes over registers (latency, not bandwidth).
@@ -13,8 +13,9 @@
 // that meet in the workspace.
 //
 // Measured: 64 rows of 2049 slots to 2048, 5.9 us; 128 rows of up to 8192 to 2048, 13.8 us, their moves
-// (INT4 rows of 64 bytes) 12.4 us; 16 rows of 131072 to 16384, three digits 7.7 us each, lists 15.6 us,
-// moves 52 us (4.5 TB/s).
+// (INT4 rows of 64 bytes) 14.7 us, or 12.4 where two sets of inputs in turn leave a part of them in the last
+// cache; 16 rows of 131072 to 16384, three digits 8.6, 7.5 and 7.9 us, lists 15.0 us, moves 52 us
+// (4.5 TB/s).
 //
 // Moves. The evicted slots below the budget (holes) take the kept slots above it, in order. No slot is
 // both, so rows are copied in any order, 16 bytes per lane, bound by HBM: in the same kernel

@@ -7,8 +7,8 @@
 // rotation needs no other lane. A lane's channels are the same in every head: its eight
 // cosines and sines are loaded once per token and used for all heads. Bound by HBM: every
 // byte of qkv is read once, 16 bytes per lane, and every result written once. Measured: 8192 tokens
-// of 32 + 32 + 32 heads of 128, float16, 78.5 us (5.2 TB/s read and written); 1117 tokens of
-// 32 + 8 + 8 into INT4, 9.6 us, one token 2.4 us (latency).
+// of 32 + 32 + 32 heads of 128, float16, 78.0 us (5.2 TB/s read and written; a copy of 400 MiB reaches
+// 5.4); 1117 tokens of 32 + 8 + 8 into INT4, 9.0 to 10.4 us, one token 2.3 to 2.7 us (latency).
 //
 // Read-back. One row of K and V per D / 8 lanes; bound by the writes, which go past the caches
 // (134 MB from 2048 slots of 4 x 32 INT4 heads: 25.7 us, 40.8 with ordinary stores;
