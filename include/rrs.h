@@ -568,6 +568,11 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *    float16 values x (codes 0 where s = 0); the row stands for q s. The scale is rounded
  *    before it divides, so codes and scale are exact functions of x. Of a row with a
  *    value that is not finite the scale is not either and the codes are 0: the row stands for NaN.
+ *  - RRS_KV_FP8: k, v hold head_dim bytes per row, 8-bit floats of 4 exponent and 3 mantissa bits (bias
+ *    7, no infinities, 0x7F and 0xFF are NaN, largest 448). k_scale, v_scale: pages x kv_heads x
+ *    page_size / 16 float16, one for each block of 16 slots of a page and head: a power of two s
+ *    in [2^-15, 2^8]. A row stands for q s, which is a float16 number exactly. What an append makes of it
+ *    is stated at rrs_rope_kv_append. rrs_kv_evict moves single rows and refuses this format.
  *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
  *    read. No page belongs to two rows of the table in a call that writes the cache.
  * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,
@@ -575,7 +580,8 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  * <= 2^30. The struct is read on the host during the call only. A launch holds fewer than 2^32
  * threads, of 256 or (kv_evict's selection) 1024 per workgroup: larger calls are RRS_ERR_SHAPE, with
  * nothing enqueued. These are, with r = sequences * kv_heads and all quotients rounded up,
- *  - rrs_rope_kv_append: M >= 2^24;
+ *  - rrs_rope_kv_append: M >= 2^24; into RRS_KV_FP8 M + M / 16 >= 2^24 or, for M < 768,
+ *    M (kv_heads / 2 + heads * head_dim / 4096) >= 2^24;
  *  - rrs_paged_attention with weights, where they take a second launch (more than 16 query
  *    heads per KV head, or sequences that are cut): r * max_length / 1024, and sequences * heads
  *    if they are cut, >= 2^24;
@@ -591,7 +597,7 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  * sequence's length are never used, whatever they hold.
  * ------------------------------------------------------------------------
  */
-enum { RRS_KV_F16 = 0, RRS_KV_INT4 = 1 };
+enum { RRS_KV_F16 = 0, RRS_KV_INT4 = 1, RRS_KV_FP8 = 8 };
 
 typedef struct rrs_kv_cache {
   void* k;
@@ -599,7 +605,7 @@ typedef struct rrs_kv_cache {
   void* k_scale;        /* NULL for RRS_KV_F16 */
   void* v_scale;        /* NULL for RRS_KV_F16 */
   const int32_t* table; /* sequences x max_pages */
-  int32_t format;       /* RRS_KV_F16 or RRS_KV_INT4 */
+  int32_t format;       /* RRS_KV_F16, RRS_KV_INT4 or RRS_KV_FP8 */
   int32_t pages;        /* pages of k and v */
   int32_t kv_heads;
   int32_t page_size;
@@ -634,6 +640,16 @@ enum { RRS_ROPE_INTERLEAVED = 1 };
  *   weights, slot_pos: NULL, or the arrays of rrs_kv_evict (sequences x kv_heads x
  *                  max_pages * page_size): a stored token's entries become 0 and its
  *                  position on axis 0.
+ * RRS_KV_FP8: the tokens that a call puts into a block of 16 slots stand in consecutive rows, in the order of
+ * their slots and without gaps (as prompts and single tokens do; RRS_DEBUG: else RRS_ERR_PRECONDITION; without
+ * it such a block's codes and scale are undefined, nothing else). The
+ * block's scale becomes the smallest power of two, 2^-15 or more, that is not below its scale so far and
+ * brings the tokens' largest finite |x| to 448 at most; a call that writes the block's first slot
+ * begins it anew, as if its scale so far were 2^-15. Codes are q = x / s to nearest (ties to even; cut to
+ * +-240 where s = 2^8, so that q s <= 61440), NaN where x is not finite. Where the scale grows, the block's
+ * other rows get the codes of their q s in the new scale: the same numbers, but for those below 2^-6 s,
+ * which are rounded to multiples of 2^-9 s. A value is off by at most 2^-4 of itself or half of 2^-9 s,
+ * and by that half once more, in smaller scales, for every time that its scale has grown.
  */
 rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int heads,
                               const int32_t* positions, int axes, const int32_t* sections,
@@ -665,7 +681,7 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
  *   scale       : finite, else RRS_ERR_FLAGS.
  * Logits, softmax and sums in float32; for the product with V the weights (RRS_KV_INT4: times the
  * value's scale) are rounded to float16 in units of their own: off by 2^-11 relative, or by 2^-36 of the
- * head's largest one where that is more. A
+ * head's largest one where that is more (RRS_KV_F16 and RRS_KV_FP8: 2^-37). A
  * sequence's result depends on the other sequences only through their lengths, which decide where the
  * sums are cut; it repeats bit for bit for the same lengths and max_length.
  */
@@ -708,7 +724,7 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
 /*
  * The cached values as float16: K and V, each sequences x kv_heads x max_length x
  * head_dim, zeros from a sequence's length on (for the attention of a prompt's tokens, and
- * to look at what an INT4 cache stands for: fp16(q s)).
+ * to look at what a cache of codes stands for: fp16(q s)).
  */
 rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int max_length, void* K,
                        void* V, void* stream);

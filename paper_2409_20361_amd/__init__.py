@@ -49,6 +49,7 @@ from ._binding import (  # noqa: F401
 )
 from ._kv import (  # noqa: F401
     KV_F16,
+    KV_FP8,
     KV_INT4,
     KVCache,
     kv_cache,
@@ -62,7 +63,7 @@ from ._kv import (  # noqa: F401
 )
 
 __all__ = [
-    "KV_F16", "KV_INT4", "KVCache", "kv_cache", "kv_evict", "kv_evict_workspace_bytes",
+    "KV_F16", "KV_FP8", "KV_INT4", "KVCache", "kv_cache", "kv_evict", "kv_evict_workspace_bytes",
     "kv_read", "paged_attention",
     "paged_attention_workspace_bytes", "rope_kv_append", "rope_table",
     "REORDER_BLOCK", "SCHEME_PER_CHANNEL", "SCHEME_RUNTIME_SMOOTH", "SCHEME_SUB_CHANNEL",

@@ -21,6 +21,7 @@ from ._binding import RRSError, lib
 # Formats of the cached values (include/rrs.h, RRS_KV_*).
 KV_F16 = 0
 KV_INT4 = 1
+KV_FP8 = 8
 
 _module = None
 
@@ -42,7 +43,8 @@ def _load():
 class KVCache(NamedTuple):
     """One layer's cache. k, v: (pages, KV heads, page size, head dim) float16, or (..., head dim
     / 2) uint8 of packed INT4 codes with k_scale, v_scale (pages, KV heads, page size)
-    float16; table: (sequences, pages per sequence) int32, sequence b's slot t being slot
+    float16, or float8_e4m3fn with k_scale, v_scale (pages, KV heads, page size / 16) float16, powers of
+    two for blocks of 16 slots; table: (sequences, pages per sequence) int32, sequence b's slot t being slot
     t % page size of page table[b, t // page size]."""
     k: torch.Tensor
     v: torch.Tensor
@@ -64,8 +66,14 @@ def kv_cache(pages: int, kv_heads: int, page_size: int, head_dim: int, table: to
         k, v = (torch.empty((pages, kv_heads, page_size, head_dim), dtype=torch.float16,
                             device=dev) for _ in range(2))
         return KVCache(k, v, table)
+    if format == KV_FP8:
+        k, v = (torch.empty((pages, kv_heads, page_size, head_dim), dtype=torch.float8_e4m3fn,
+                            device=dev) for _ in range(2))
+        ks, vs = (torch.zeros((pages, kv_heads, page_size // 16), dtype=torch.float16, device=dev)
+                  for _ in range(2))
+        return KVCache(k, v, table, ks, vs)
     if format != KV_INT4:
-        raise ValueError("format must be KV_F16 or KV_INT4")
+        raise ValueError("format must be KV_F16, KV_INT4 or KV_FP8")
     k, v = (torch.empty((pages, kv_heads, page_size, head_dim // 2), dtype=torch.uint8, device=dev)
             for _ in range(2))
     ks, vs = (torch.empty((pages, kv_heads, page_size), dtype=torch.float16, device=dev)
@@ -95,7 +103,8 @@ def rope_kv_append(qkv: torch.Tensor, positions: torch.Tensor, rope: torch.Tenso
     qkv: M x (heads + 2 KV heads) head dim fp16, as the QKV projection writes it (its rows may
     lie apart); positions: (M, axes) int32; rope: (positions, rotary dim) float32 (rope_table);
     sections: frequencies of each axis (None: all on the one axis); seq, slot: (M,) int32, the
-    place of each token (out of range: not stored). weights, slot_pos: kv_evict's arrays;
+    place of each token (out of range: not stored; KV_FP8: tokens of one block of 16 slots in consecutive
+    rows, as their slots). weights, slot_pos: kv_evict's arrays;
     a stored token's entries become 0 and its position on axis 0. Returns the rotated queries,
     M x heads x head dim."""
     return (_module or _load()).rope_kv_append(qkv, positions, rope, *cache, seq, slot, heads,

@@ -36,13 +36,14 @@
 // 127 us with the join, 4.4 TB/s); 8 x 40 heads over one KV head of 256 with a mask, 19 us (2.0 TB/s: latency of three or
 // four tiles per wave, the rows read by three row blocks); one sequence of 117 slots, 32 heads, 5
 // us (latency); 179 x 64 heads of up to 5 slots 14 us.
+#include <type_traits>
+
 #include "rrs_device.h"
 #include "rrs_kv.h"
 
 namespace rrs {
 namespace {
 
-typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -163,14 +164,22 @@ __device__ __forceinline__ bool find_piece(const AttentionArgs& a, const KvView&
   return true;
 }
 
-template <int D, bool kInt4, int kTeam = kWaves>
+// Slots per wave and step.
+constexpr int tile_slots(int dim, int format, bool alone) {
+  if (format == kCacheInt4) return 64;
+  const int n = dim == 256 || alone ? 16 : 32;
+  return format == kCacheFp8 ? 2 * n : n;
+}
+
+template <int D, int kFormat, int kTeam = kWaves>
 struct Shape {
+  static constexpr bool kInt4 = kFormat == kCacheInt4, kFp8 = kFormat == kCacheFp8;
   // Slots per wave and step. 16 where 32 rows would not leave registers for a second wave, and for
   // short sequences: more waves hide more of the chain of length, page and rows (179 x 64 heads of up to
   // 5 slots 26 -> 21 us, 200 x 64 of up to 64 within 3 %).
-  static constexpr int kTile = kInt4 ? 64 : D == 256 || kTeam == 1 ? 16 : 32;
+  static constexpr int kTile = tile_slots(D, kFormat, kTeam == 1);
   static constexpr int kBlocks = kTile / 16;         // of 16 slots
-  static constexpr int kRow = kInt4 ? D / 2 : 2 * D; // bytes of a cache row
+  static constexpr int kRow = kInt4 ? D / 2 : kFp8 ? D : 2 * D;  // bytes of a cache row
   static constexpr int kSteps = D / 32;              // mfma steps of a logit
   static constexpr int kOut = D / 16;                // blocks of output channels
   static constexpr int kKey = kRow / 4;              // bytes of a key row per lane
@@ -189,7 +198,9 @@ struct Shape {
   // different banks.
   static __device__ __forceinline__ int at(int t, int c) {
     int x;
-    if constexpr (kInt4)
+    if constexpr (kFp8)  // sixteen chunks of 256 bytes; slot bit 3 names the half of the wave
+      x = (((t & 7) | (t >> 1 & 8)) / (256 / kRow)) & (kRow / 16 - 1);
+    else if constexpr (kInt4)
       x = D == 64 ? (t >> 2) & 1 : D == 128 ? (t >> 1) & 3 : t & 7;
     else
       x = (D == 64 ? t & 3 : t & 7) << 1;
@@ -219,6 +230,13 @@ __device__ __forceinline__ v8h eight_codes(uint32_t w) {
   return v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 __device__ __forceinline__ int code_order(int e) { return (e >> 1) + 4 * (e & 1); }
+
+// Eight e4m3 codes as float16 in units of powers of two, one for each four: exact (rrs_kv.h).
+__device__ __forceinline__ v8h eight_fp8(uint32_t lo, uint32_t hi, float lo_unit, float hi_unit) {
+  const v2h a = two_fp8<0>(lo, lo_unit), b = two_fp8<1>(lo, lo_unit);
+  const v2h c = two_fp8<0>(hi, hi_unit), d = two_fp8<1>(hi, hi_unit);
+  return v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
 
 // The T at byte `at` past an address that is the same for the wave: the address stays in scalar
 // registers and the offset in one vector register (the compiler would else keep a 64-bit
@@ -333,10 +351,11 @@ __device__ __forceinline__ float2 weight_row(float top, float total) {
 // Grid: pieces x KV heads x row blocks. The row blocks of a piece and head read the same rows: they
 // are 8 apart, on one XCD, and share its L2.
 // kTeam: waves that share a piece; 1: every wave takes a whole sequence by itself.
-template <int D, bool kInt4, bool kMask, int kTeam>
-__global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
+template <int D, int kFormat, bool kMask, int kTeam>
+__global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd))
     attention_kernel(AttentionArgs a, KvView c, Plan plan) {
-  using S = Shape<D, kInt4, kTeam>;
+  using S = Shape<D, kFormat, kTeam>;
+  constexpr bool kInt4 = S::kInt4, kFp8 = S::kFp8;
   constexpr int kLds = kTeam == 1 ? S::kValues : S::kLds;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds];
   __shared__ float2 wave_stats[kTeam][kRows], row_stats[kWaves / kTeam][kRows];
@@ -369,7 +388,9 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
 #pragma unroll
   for (int i = 0; i < S::kSteps; ++i) {
     const v8h x = *reinterpret_cast<const v8h*>(
-        qrow + (kInt4 ? (D / 4) * quarter + 8 * i : 32 * i + 8 * quarter));
+        qrow + (kInt4  ? (D / 4) * quarter + 8 * i
+                : kFp8 ? 64 * (i / 2) + 16 * quarter + 8 * (i & 1)
+                       : 32 * i + 8 * quarter));
     if constexpr (kInt4) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) q[i][e] = x[code_order(e)];
@@ -408,6 +429,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
   v4u key[S::kBlocks][(S::kKey + 15) / 16];
   v4u val[S::kBlocks][S::kPieces];
   v2u ks[S::kBlocks], vs[S::kBlocks];
+  float key_unit[S::kBlocks], val_unit[S::kBlocks];  // FP8: the blocks' scales
   uint8_t mask = 0;  // of slot t0 + lane
   size_t row[S::kBlocks];  // the blocks' first rows
   // A block's last row, in whose place rows past it are not loaded: thousands of short sequences
@@ -439,6 +461,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
       if constexpr (kInt4) {  // four slots: 8 bytes, inside the page
         ks[u] = load_at<v2u>(c.k_scale + row[u], 8 * quarter);
         vs[u] = load_at<v2u>(c.v_scale + row[u], 8 * quarter);
+      }
+      if constexpr (kFp8) {
+        ks[u][0] = load_at<uint16_t>(c.k_scale + (row[u] >> 4), 0);
+        vs[u][0] = load_at<uint16_t>(c.v_scale + (row[u] >> 4), 0);
       }
     }
     if constexpr (kMask)  // up to the last block's end: inside the row
@@ -476,12 +502,19 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
     v4u vscale[(S::kBlocks + 1) / 2];  // INT4: the tile's value scales, two to a dword
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u) {
+      if constexpr (kFp8) {
+        key_unit[u] = half_to_float(ks[u][0]);
+        val_unit[u] = half_to_float(vs[u][0]);
+      }
       v4f s = {};
 #pragma unroll
       for (int i = 0; i < S::kSteps; ++i) {
         v8h k;
         if constexpr (kInt4)
           k = eight_codes(key[u][i / 4][i % 4]);
+        else if constexpr (kFp8)
+          k = eight_fp8(key[u][i / 2][2 * (i & 1)], key[u][i / 2][2 * (i & 1) + 1], key_unit[u],
+                        key_unit[u]);
         else
           k = __builtin_bit_cast(v8h, key[u][i]);
         s = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[i], s, 0, 0, 0);
@@ -594,6 +627,17 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
                                          v2h{(_Float16)1.0f, (_Float16)1.0f}, rounded, false);
     }
 
+    // FP8 under a mask: 0 times what a slot holds might not be 0.
+    v2u of_live[(S::kBlocks + 1) / 2];
+    if constexpr (kFp8 && kMask) {
+#pragma unroll
+      for (int u = 0; u < S::kBlocks; ++u) {
+        uint32_t w = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w |= live[4 * u + r] ? 0xFFu << (8 * r) : 0u;
+        of_live[u / 2][u & 1] = w;
+      }
+    }
     // Values through LDS; the wave's own tile, so no barrier. Rows past the end: 0 times what they
     // hold might not be 0 (INT4 codes are always finite).
     if (!kInt4 && t0 + S::kTile > end) {
@@ -634,6 +678,21 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kInt4, kTeam>::kPerSimd))
               v8h{p[8 * h], p[8 * h + 1], p[8 * h + 2], p[8 * h + 3], p[8 * h + 4], p[8 * h + 5],
                   p[8 * h + 6], p[8 * h + 7]},
               o[j], 0, 0, 0);
+      } else if constexpr (kFp8) {
+        // Lanes 2 r and 2 r + 1 of a quarter name row r: 16 channels of 8 slots, four of each block.
+#pragma unroll
+        for (int h = 0; h < S::kBlocks / 2; ++h) {
+          const int r = col >> 1;
+          const int t = 32 * h + 16 * (r >> 2) + 4 * quarter + (r & 3);
+          v2u w = __builtin_bit_cast(v2u, __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                                              (lds_v2i)(tile + S::at(t, j) + 8 * (col & 1))));
+          if constexpr (kMask) w &= of_live[h];
+          o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
+              eight_fp8(w[0], w[1], val_unit[2 * h], val_unit[2 * h + 1]),
+              v8h{p[8 * h], p[8 * h + 1], p[8 * h + 2], p[8 * h + 3], p[8 * h + 4], p[8 * h + 5],
+                  p[8 * h + 6], p[8 * h + 7]},
+              o[j], 0, 0, 0);
+        }
       } else {
         // Lanes 4 r .. 4 r + 3 of a quarter name row r: 16 channels of 4 slots.
         v4s w[S::kBlocks];
@@ -875,7 +934,7 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
   p.group = heads / c.heads;
   p.row_blocks = (p.group + kRows - 1) / kRows;
   const long long share = (long long)c.heads * p.row_blocks;
-  p.step = kWaves * (c.int4() ? 64 : c.dim == 256 ? 16 : 32);
+  p.step = kWaves * tile_slots(c.dim, c.format, false);
   // Workgroups that run at the same time where cutting every sequence gives no more; else four
   // times as many, not too short, so that those that end last are a small part of the whole.
   const int resident = 256 * (c.dim == 256 ? 2 : 3);
@@ -943,22 +1002,24 @@ Second second_grid(const Plan& p, const KvView& c, int heads, int max_length, bo
   return s;
 }
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 template <int D>
 hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
   const long long grid = first_grid(p, c, a.max_length);
   const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p); };
-  if (p.team == 1) {
-    if (c.int4())
-      a.mask ? run(attention_kernel<D, true, true, 1>) : run(attention_kernel<D, true, false, 1>);
-    else
-      a.mask ? run(attention_kernel<D, false, true, 1>) : run(attention_kernel<D, false, false, 1>);
-  } else {
-    if (c.int4())
-      a.mask ? run(attention_kernel<D, true, true, kWaves>)
-             : run(attention_kernel<D, true, false, kWaves>);
-    else
-      a.mask ? run(attention_kernel<D, false, true, kWaves>)
-             : run(attention_kernel<D, false, false, kWaves>);
+  const auto by_mask = [&](auto format, auto team) {
+    constexpr int f = decltype(format)::value, n = decltype(team)::value;
+    a.mask ? run(attention_kernel<D, f, true, n>) : run(attention_kernel<D, f, false, n>);
+  };
+  const auto by_team = [&](auto format) {
+    p.team == 1 ? by_mask(format, Int<1>()) : by_mask(format, Int<kWaves>());
+  };
+  switch (c.format) {
+    case kCacheInt4: by_team(Int<kCacheInt4>()); break;
+    case kCacheFp8: by_team(Int<kCacheFp8>()); break;
+    default: by_team(Int<kCacheF16>());
   }
   if (hipError_t e = hipGetLastError()) return e;
   const Second s = second_grid(p, c, a.heads, a.max_length, a.weights != nullptr);

@@ -8,12 +8,17 @@
 
 namespace rrs {
 
+// include/rrs.h, RRS_KV_*.
+constexpr int kCacheF16 = 0, kCacheInt4 = 1, kCacheFp8 = 8;
+// FP8: slots that share a scale, and its smallest and largest exponent.
+constexpr int kSlots8 = 16, kLowest8 = -15, kHighest8 = 8;
+
 // include/rrs.h, rrs_kv_cache. Row r of k or v: row_bytes() bytes at r * row_bytes(); its scale at
-// r. Products of pages, heads and slots pass 32 bits, so rows are 64-bit numbers.
+// r (FP8: r / 16, of its block). Products of pages, heads and slots pass 32 bits, so rows are 64-bit numbers.
 struct KvView {
   uint8_t* k;
   uint8_t* v;
-  uint16_t* k_scale;  // nullptr: float16 values
+  uint16_t* k_scale;  // nullptr for float16 values
   uint16_t* v_scale;
   const int32_t* table;
   int pages;
@@ -22,8 +27,12 @@ struct KvView {
   int dim;
   int sequences;
   int max_pages;
+  int format;
 
-  __host__ __device__ bool int4() const { return k_scale != nullptr; }
+  __host__ __device__ bool int4() const { return format == kCacheInt4; }
+  __host__ __device__ int row_bytes() const {
+    return format == kCacheInt4 ? dim / 2 : format == kCacheFp8 ? dim : 2 * dim;
+  }
   __host__ __device__ int capacity() const { return max_pages << log_page; }
   // First row of (page, head).
   __device__ size_t page_row(int page, int head) const {
@@ -68,7 +77,7 @@ struct RopeArgs {
   float* weights;
   int32_t* slot_pos;
 };
-bool append_fits(int M);  // ..._fits: the call's launches are within fits_grid
+bool append_fits(int M, int heads, const KvView& c);  // ..._fits: the call's launches are within fits_grid
 hipError_t launch_rope_kv_append(const RopeArgs& a, const KvView& c, hipStream_t stream);
 
 bool read_fits(const KvView& c, int max_length);
@@ -134,6 +143,20 @@ __device__ __forceinline__ v4u dequant8(uint32_t codes, float s) {
            ((uint32_t)__builtin_bit_cast(uint16_t, hi) << 16);
   }
   return w;
+}
+
+// Two e4m3 codes, bytes 2 kHalf and 2 kHalf + 1 of w, as float16 in units of a power of two (of which the
+// instruction takes the exponent). Exact from 2^-15 on: a code's smallest step is 2^-9, float16's 2^-24.
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+template <int kHalf>
+__device__ __forceinline__ v2h two_fp8(uint32_t w, float unit) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, unit, kHalf != 0);
+}
+__device__ __forceinline__ v4u dequant8_fp8(uint2 w, float unit) {
+  return v4u{__builtin_bit_cast(uint32_t, two_fp8<0>(w.x, unit)),
+             __builtin_bit_cast(uint32_t, two_fp8<1>(w.x, unit)),
+             __builtin_bit_cast(uint32_t, two_fp8<0>(w.y, unit)),
+             __builtin_bit_cast(uint32_t, two_fp8<1>(w.y, unit))};
 }
 
 }  // namespace rrs

@@ -2,6 +2,7 @@
 // stream. Every check runs on the host before any device work is enqueued.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <memory>
@@ -19,9 +20,13 @@ using rrs::is_aligned;
 
 namespace {
 
+bool has_scales(const rrs_kv_cache& c) {
+  return c.format == RRS_KV_INT4 || c.format == RRS_KV_FP8;
+}
+
 bool any_null(const rrs_kv_cache* c) {
   return !c || !c->k || !c->v || !c->table ||
-         (c->format == RRS_KV_INT4 && (!c->k_scale || !c->v_scale));
+         (has_scales(*c) && (!c->k_scale || !c->v_scale));
 }
 
 bool valid_shape(const rrs_kv_cache& c) {
@@ -41,16 +46,16 @@ bool valid_heads(const rrs_kv_cache& c, int heads) {
 }
 
 bool valid_format(const rrs_kv_cache& c) {
-  return c.format == RRS_KV_F16 || c.format == RRS_KV_INT4;
+  return c.format == RRS_KV_F16 || has_scales(c);
 }
 
 bool aligned(const rrs_kv_cache& c) {
   return is_aligned(c.k) && is_aligned(c.v) && is_aligned(c.table) &&
-         (c.format != RRS_KV_INT4 || (is_aligned(c.k_scale) && is_aligned(c.v_scale)));
+         (!has_scales(c) || (is_aligned(c.k_scale) && is_aligned(c.v_scale)));
 }
 
 rrs::KvView view(const rrs_kv_cache& c) {
-  const bool q = c.format == RRS_KV_INT4;
+  const bool q = has_scales(c);
   int log_page = 0;
   while ((1 << log_page) < c.page_size) ++log_page;
   return rrs::KvView{static_cast<uint8_t*>(c.k),
@@ -63,7 +68,8 @@ rrs::KvView view(const rrs_kv_cache& c) {
                      log_page,
                      c.head_dim,
                      c.sequences,
-                     c.max_pages};
+                     c.max_pages,
+                     c.format};
 }
 
 // ---------------------------------------------------------------------------
@@ -131,6 +137,33 @@ rrs_status debug_check_places(const rrs_kv_cache& c, const int32_t* seq, const i
   return RRS_OK;
 }
 
+// FP8: no block of 16 slots gets its tokens from two runs of rows.
+rrs_status debug_check_runs(const rrs_kv_cache& c, const int32_t* seq, const int32_t* slot, int M,
+                            void* stream) {
+  std::unique_ptr<int32_t[]> b, s;
+  if (rrs_status e = debug_fetch_new(&b, seq, (size_t)M, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&s, slot, (size_t)M, stream)) return e;
+  std::unique_ptr<int64_t[]> blocks(new (std::nothrow) int64_t[(size_t)M]);
+  if (!blocks) return RRS_ERR_HIP;
+  size_t count = 0;
+  const int per_block = rrs::kSlots8;
+  for (size_t m = 0; m < (size_t)M; ++m) {
+    if (b[m] < 0 || b[m] >= c.sequences || s[m] < 0 || s[m] >= capacity(c)) continue;
+    if (m > 0 && s[m] % per_block != 0 && b[m - 1] == b[m] && s[m - 1] == s[m] - 1) continue;
+    blocks[count++] = (int64_t)b[m] << 32 | s[m] / per_block;
+  }
+  std::sort(blocks.get(), blocks.get() + count);
+  for (size_t i = 1; i < count; ++i)
+    if (blocks[i] == blocks[i - 1]) {
+      std::fprintf(stderr,
+                   "[rrs] RRS_DEBUG: tokens of slots %lld.. of sequence %d are not in one run of "
+                   "rows\n",
+                   (long long)((blocks[i] & 0xFFFFFFFF) * per_block), (int)(blocks[i] >> 32));
+      return RRS_ERR_PRECONDITION;
+    }
+  return RRS_OK;
+}
+
 void debug_print(const char* call, const rrs_kv_cache* c) {
   if (!c) {
     std::fprintf(stderr, "[rrs] %s cache=NULL\n", call);
@@ -157,11 +190,12 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
   if (!qkv || !positions || !sections || !rope || !seq || !slot || !Q || any_null(cache))
     return RRS_ERR_NULL;
   const rrs_kv_cache& c = *cache;
-  if (!valid_shape(c) || heads < 1 || M < 1 || !rrs::append_fits(M) || axes < 1 || axes > 4 || rope_rows < 1 ||
+  if (!valid_shape(c) || heads < 1 || M < 1 || axes < 1 || axes > 4 || rope_rows < 1 ||
       rotary_dim < 16 || rotary_dim % 16 != 0 || rotary_dim > c.head_dim)
     return RRS_ERR_SHAPE;
   const int64_t width = ((int64_t)heads + 2 * (int64_t)c.kv_heads) * c.head_dim;
-  if (width >= ((int64_t)1 << 31) || row_stride < width || row_stride % 8 != 0)
+  if (width >= ((int64_t)1 << 31) || row_stride < width || row_stride % 8 != 0 ||
+      !rrs::append_fits(M, heads, view(c)))
     return RRS_ERR_SHAPE;
   rrs::RopeArgs a{};
   int64_t sum = 0;
@@ -189,6 +223,8 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
                                          "positions", stream))
       return s;
     if (rrs_status s = debug_check_places(c, seq, slot, M, stream)) return s;
+    if (c.format == RRS_KV_FP8)
+      if (rrs_status s = debug_check_runs(c, seq, slot, M, stream)) return s;
   }
   a.qkv = static_cast<const uint16_t*>(qkv);
   a.row_stride = row_stride;
@@ -249,8 +285,8 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
 }
 
 size_t rrs_kv_evict_workspace_bytes(const rrs_kv_cache* cache, int max_length, int budget) {
-  if (!cache || !valid_shape(*cache) || !valid_format(*cache) || max_length < 1 ||
-      max_length > capacity(*cache) || budget < 1 || budget > capacity(*cache) ||
+  if (!cache || !valid_shape(*cache) || !valid_format(*cache) || cache->format == RRS_KV_FP8 ||
+      max_length < 1 || max_length > capacity(*cache) || budget < 1 || budget > capacity(*cache) ||
       !rrs::evict_fits(view(*cache), max_length, budget))
     return 0;
   return rrs::evict_workspace_bytes(view(*cache), max_length, budget);
@@ -269,7 +305,7 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
   if (!valid_shape(c) || max_length < 1 || max_length > capacity(c) || budget < 1 ||
       budget > capacity(c) || !rrs::evict_fits(view(c), max_length, budget))
     return RRS_ERR_SHAPE;
-  if (!valid_format(c)) return RRS_ERR_FLAGS;
+  if (!valid_format(c) || c.format == RRS_KV_FP8) return RRS_ERR_FLAGS;
   const size_t need = rrs::evict_workspace_bytes(view(c), max_length, budget);
   if (need > 0 && !workspace) return RRS_ERR_NULL;
   if (!aligned(c) || !is_aligned(workspace) || !is_aligned(lengths) || !is_aligned(weights) || !is_aligned(slot_pos) ||

@@ -42,6 +42,7 @@ const char* text(at::ScalarType t) {
     case at::kInt: return "torch.int32";
     case at::kByte: return "torch.uint8";
     case at::kBool: return "torch.bool";
+    case at::kFloat8_e4m3fn: return "torch.float8_e4m3fn";
     default: return c10::toString(t);
   }
 }
@@ -134,13 +135,15 @@ struct Cache {
       raise(PyExc_ValueError, "cache: k must have 4 dimensions and table 2");
     const auto s = k.sizes();
     c.table = static_cast<const int32_t*>(dev(a[2], "table", at::kInt, table.sizes(), on));
-    const bool int4 = a[3] != Py_None || a[4] != Py_None;
-    const auto type = int4 ? at::kByte : at::kHalf;
+    const bool fp8 = k.scalar_type() == at::kFloat8_e4m3fn;
+    const bool int4 = !fp8 && (a[3] != Py_None || a[4] != Py_None);
+    const auto type = fp8 ? at::kFloat8_e4m3fn : int4 ? at::kByte : at::kHalf;
     c.k = dev(a[0], "k", type, s, on);
     c.v = dev(a[1], "v", type, s, on);
-    if (int4) {
-      c.k_scale = dev(a[3], "k_scale", at::kHalf, s.slice(0, 3), on);
-      c.v_scale = dev(a[4], "v_scale", at::kHalf, s.slice(0, 3), on);
+    if (int4 || fp8) {
+      const int64_t per_page[3] = {s[0], s[1], fp8 ? s[2] / 16 : s[2]};
+      c.k_scale = dev(a[3], "k_scale", at::kHalf, per_page, on);
+      c.v_scale = dev(a[4], "v_scale", at::kHalf, per_page, on);
     }
     for (const int64_t x : {s[0], s[1], s[2], 2 * s[3], table.size(0), table.size(1)})
       if (x > INT32_MAX) raise(PyExc_ValueError, "cache: a size is out of range");
@@ -148,7 +151,7 @@ struct Cache {
     dim = int4 ? 2 * s[3] : s[3];
     sequences = table.size(0);
     capacity = table.size(1) * s[2];
-    c.format = int4 ? RRS_KV_INT4 : RRS_KV_F16;
+    c.format = fp8 ? RRS_KV_FP8 : int4 ? RRS_KV_INT4 : RRS_KV_F16;
     c.pages = (int32_t)s[0];
     c.kv_heads = (int32_t)heads;
     c.page_size = (int32_t)s[2];
