@@ -729,6 +729,68 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
 rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int max_length, void* K,
                        void* V, void* stream);
 
+/*
+ * Pages of a cache: which of them the rows of the table own. No counts are kept: a page is in use if
+ * an entry below a row's length names it (pages of a row, for n slots: the first ceil(n /
+ * page_size) entries), else it is free. The planners read a table, write a new one, and name the pages that
+ * have to be copied; rrs_kv_copy_pages then copies them, in every layer whose cache goes by that
+ * table. All of it stays on the device: table, lengths and lists can live in a graph.
+ * Arguments of both planners: table, lengths of the cache's sequences; pages of the pool, at most 2^20;
+ * the sizes as in rrs_kv_cache. Entries that name no page of the pool are taken over as they are
+ * (RRS_DEBUG: RRS_ERR_PRECONDITION). Outputs and workspace must overlap neither an input nor each other.
+ */
+
+/*
+ * Rows of the table anew: forked, reordered, trimmed, freed and extended.
+ *   parent      in : NULL (row b goes on as it is), or sequences int32: new row b goes on with the
+ *                    tokens of old row parent[b]; a number outside [0, sequences) leaves the row empty.
+ *   room        in : sequences int32: slots that new row b is to have pages for, cut to
+ *                    [0, max_pages * page_size] (ignored where the row is empty).
+ *   lengths_out out: sequences int32: kept = min(lengths[parent[b]], room[b]) tokens. The pages
+ *                    of these are taken over, and may be in several rows then.
+ *   room_out    out: sequences int32: room[b], or kept where no pages are left for it.
+ *   table_out   out: sequences x max_pages int32: the row's pages for room_out[b] slots, -1 behind them.
+ *                    Fresh pages are the free ones of lowest numbers, handed out by rows.
+ *   src, dst    out: sequences int32 each: pages to be copied before anything is appended, in the order
+ *                    of rows; -1 from count[0] on.
+ *   count       out: 2 int32: the copies; free pages that are left.
+ * A row that is to grow (room[b] > kept) and whose last page is only partly filled is going to write into that page:
+ * if other rows keep it too, the row gets a fresh page in its place, a copy. Of rows that all are
+ * going to write into the page the first keeps it. If the free pages do not
+ * suffice for all rows, all rows that write into a shared page are to get a copy, and rows are
+ * served in their order while the sum of what they need, served or not, is within the free pages; the others
+ * keep their tokens and get nothing.
+ */
+size_t rrs_kv_fork_workspace_bytes(int sequences, int max_pages, int page_size, int pages);
+rrs_status rrs_kv_fork(const int32_t* table, int sequences, int max_pages, int page_size, int pages,
+                       const int32_t* lengths, const int32_t* parent, const int32_t* room,
+                       int32_t* table_out, int32_t* lengths_out, int32_t* room_out, int32_t* src,
+                       int32_t* dst, int32_t* count, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
+/*
+ * The U pages in use brought to the front of the pool: those with numbers from U on move, in order, to the
+ * free ones below U, in order.
+ *   table_out   out: sequences x max_pages int32: the new numbers, -1 past a row's pages.
+ *   src, dst    out: max(1, pages / 2) int32 each: the moves; -1 from count[0] on.
+ *   count       out: 2 int32: the moves; U.
+ * Pages past a row's length do not count as used: lengths may be the room that rrs_kv_fork gave.
+ */
+size_t rrs_kv_compact_workspace_bytes(int sequences, int max_pages, int page_size, int pages);
+rrs_status rrs_kv_compact(const int32_t* table, int sequences, int max_pages, int page_size,
+                          int pages, const int32_t* lengths, int32_t* table_out, int32_t* src,
+                          int32_t* dst, int32_t* count, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * Pages src[i] of k, v and the scales copied to dst[i], for i < n, or i < min(n, count[0]) where count is
+ * given (device memory). Pairs with a number outside [0, pages) are skipped. No page in dst is there twice
+ * or in src (RRS_DEBUG: else RRS_ERR_PRECONDITION). n >= 1; kv_heads * page_size * bytes of a row < 2^31. The
+ * cache's table is not read.
+ */
+rrs_status rrs_kv_copy_pages(const rrs_kv_cache* cache, const int32_t* src, const int32_t* dst,
+                             int n, const int32_t* count, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -51,10 +51,17 @@ from ._kv import (  # noqa: F401
     KV_F16,
     KV_FP8,
     KV_INT4,
+    CompactPlan,
+    ForkPlan,
     KVCache,
     kv_cache,
+    kv_compact,
+    kv_compact_workspace_bytes,
+    kv_copy_pages,
     kv_evict,
     kv_evict_workspace_bytes,
+    kv_fork,
+    kv_fork_workspace_bytes,
     kv_read,
     paged_attention,
     paged_attention_workspace_bytes,
@@ -63,7 +70,9 @@ from ._kv import (  # noqa: F401
 )
 
 __all__ = [
-    "KV_F16", "KV_FP8", "KV_INT4", "KVCache", "kv_cache", "kv_evict", "kv_evict_workspace_bytes",
+    "KV_F16", "KV_FP8", "KV_INT4", "KVCache", "CompactPlan", "ForkPlan", "kv_cache", "kv_compact",
+    "kv_compact_workspace_bytes", "kv_copy_pages", "kv_evict", "kv_evict_workspace_bytes", "kv_fork",
+    "kv_fork_workspace_bytes",
     "kv_read", "paged_attention",
     "paged_attention_workspace_bytes", "rope_kv_append", "rope_table",
     "REORDER_BLOCK", "SCHEME_PER_CHANNEL", "SCHEME_RUNTIME_SMOOTH", "SCHEME_SUB_CHANNEL",

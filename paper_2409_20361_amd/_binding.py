@@ -73,6 +73,11 @@ _SIGNATURES = {
                                       _sz, _vp]),
     "rrs_kv_evict_workspace_bytes": (_sz, [_vp, _i, _i]),
     "rrs_kv_read": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp]),
+    "rrs_kv_fork": (ctypes.c_int32, [_vp, _i, _i, _i, _i] + [_vp] * 10 + [_sz, _vp]),
+    "rrs_kv_fork_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "rrs_kv_compact": (ctypes.c_int32, [_vp, _i, _i, _i, _i] + [_vp] * 6 + [_sz, _vp]),
+    "rrs_kv_compact_workspace_bytes": (_sz, [_i, _i, _i, _i]),
+    "rrs_kv_copy_pages": (ctypes.c_int32, [_vp, _vp, _vp, _i, _vp, _vp]),
 }
 
 # Channels per block of the runtime reorder (include/rrs.h, RRS_REORDER_BLOCK).

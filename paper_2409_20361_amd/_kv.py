@@ -158,3 +158,62 @@ def kv_read(cache: KVCache, lengths: torch.Tensor, max_length: Optional[int] = N
     """The cached values as fp16: (K, V), each sequences x KV heads x max_length x head dim, zeros
     from a sequence's length on."""
     return (_module or _load()).kv_read(*cache, lengths, max_length, out)
+
+
+class ForkPlan(NamedTuple):
+    """What kv_fork returns: the new table, the tokens of its rows, the slots they have pages for, and the
+    copies (src, dst, count) for kv_copy_pages; count[1] says how many free pages are left."""
+    table: torch.Tensor
+    lengths: torch.Tensor
+    room: torch.Tensor
+    src: torch.Tensor
+    dst: torch.Tensor
+    count: torch.Tensor
+
+
+class CompactPlan(NamedTuple):
+    """What kv_compact returns: the new table and the moves for kv_copy_pages; count[1] says how many pages
+    are in use."""
+    table: torch.Tensor
+    src: torch.Tensor
+    dst: torch.Tensor
+    count: torch.Tensor
+
+
+def kv_fork_workspace_bytes(sequences: int, max_pages: int, page_size: int, pages: int) -> int:
+    return (_module or _load()).kv_fork_workspace_bytes(sequences, max_pages, page_size, pages)
+
+
+def kv_fork(table: torch.Tensor, lengths: torch.Tensor, parent: Optional[torch.Tensor],
+            room: torch.Tensor, pages: int, page_size: int, out: Optional[tuple] = None,
+            workspace: Optional[torch.Tensor] = None) -> ForkPlan:
+    """Rows of a page table anew: forked, reordered, trimmed, freed and extended.
+
+    New row b goes on with the tokens of row parent[b] (None: its own; out of range: the row is empty and
+    its pages are free), of which min(lengths, room[b]) are kept, and has pages for room[b] slots where
+    the pool of `pages` pages has them (else for its tokens only, in `room` of the result). Pages of
+    kept tokens are shared by the rows that keep them; a row that is going to write into a shared,
+    partly filled page gets a page of its own, to be copied with kv_copy_pages in every layer before the
+    next append. table: (sequences, pages per sequence) int32; lengths, parent, room: (sequences,)
+    int32. The result is new tensors or `out`, which overlap neither an input nor the workspace nor each other."""
+    r = (_module or _load()).kv_fork(table, lengths, parent, room, pages, page_size, out, workspace)
+    return ForkPlan._make(r)
+
+
+def kv_compact_workspace_bytes(sequences: int, max_pages: int, page_size: int, pages: int) -> int:
+    return (_module or _load()).kv_compact_workspace_bytes(sequences, max_pages, page_size, pages)
+
+
+def kv_compact(table: torch.Tensor, lengths: torch.Tensor, pages: int, page_size: int,
+               out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None) -> CompactPlan:
+    """The pages in use (those of `lengths` slots of every row) brought to the front of the pool: a new table
+    and the moves, to be made with kv_copy_pages in every layer. Arguments as kv_fork's."""
+    r = (_module or _load()).kv_compact(table, lengths, pages, page_size, out, workspace)
+    return CompactPlan._make(r)
+
+
+def kv_copy_pages(cache: KVCache, src: torch.Tensor, dst: torch.Tensor,
+                  count: Optional[torch.Tensor] = None) -> None:
+    """Copies pages src[i] of the cache to dst[i], in place: all pairs, or the first count[0]. Pairs with a
+    number that is no page are skipped; no page in dst may be there twice or in src."""
+    (_module or _load()).kv_copy_pages(*cache, src, dst, count)

@@ -25,7 +25,7 @@ SOURCES = ["rrs_api.cpp", "rrs_gemm_route.cpp", "rrs_quant.hip", "rrs_weight.hip
            "rrs_gemm_small.hip", "rrs_gemm_decode.hip", "rrs_quant_wave.hip", "rrs_reorder.hip", "rrs_quant_rows.hip",
            "rrs_gemm_stream.hip", "rrs_gemm_stream_gather.hip", "rrs_gemm_mid.hip",
            "rrs_gemm_fp6.hip", "rrs_noalloc.hip", "rrs_kv_api.cpp", "rrs_kv_append.hip",
-           "rrs_attention.hip", "rrs_evict.hip"]
+           "rrs_attention.hip", "rrs_evict.hip", "rrs_pages.hip"]
 
 # Per-source code-generation options on top of COMMON.
 # rrs_gemm_stream_gather.hip: keep MFMA results in VGPRs (the per-block

@@ -117,6 +117,44 @@ size_t evict_workspace_bytes(const KvView& c, int max_length, int budget);
 hipError_t launch_kv_evict(const EvictArgs& a, const KvView& c, void* workspace,
                            hipStream_t stream);
 
+struct ForkArgs {
+  const int32_t* table;
+  int sequences;
+  int max_pages;
+  int log_page;
+  int pages;
+  const int32_t* lengths;
+  const int32_t* parent;  // or nullptr
+  const int32_t* room;
+  int32_t* table_out;
+  int32_t* lengths_out;
+  int32_t* room_out;
+  int32_t* src;
+  int32_t* dst;
+  int32_t* count;
+};
+int most_pages();  // of the planners
+size_t fork_workspace_bytes(int sequences, int pages);
+hipError_t launch_kv_fork(const ForkArgs& a, void* workspace, hipStream_t stream);
+
+struct CompactArgs {
+  const int32_t* table;
+  int sequences;
+  int max_pages;
+  int log_page;
+  int pages;
+  const int32_t* lengths;
+  int32_t* table_out;
+  int32_t* src;
+  int32_t* dst;
+  int32_t* count;
+};
+size_t compact_workspace_bytes(int pages);
+hipError_t launch_kv_compact(const CompactArgs& a, void* workspace, hipStream_t stream);
+
+hipError_t launch_kv_copy_pages(const KvView& c, const int32_t* src, const int32_t* dst, int n,
+                                const int32_t* count, hipStream_t stream);
+
 // Inclusive prefix sums over the wave; the last lane holds the total.
 __device__ __forceinline__ int wave_prefix(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);  // from 1 lane below in the row

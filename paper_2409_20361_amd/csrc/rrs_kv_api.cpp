@@ -14,6 +14,7 @@
 using rrs::check_device;
 using rrs::debug_check_finite_f16;
 using rrs::debug_enabled;
+using rrs::debug_fetch;
 using rrs::debug_fetch_new;
 using rrs::from_hip;
 using rrs::is_aligned;
@@ -29,13 +30,29 @@ bool any_null(const rrs_kv_cache* c) {
          (has_scales(*c) && (!c->k_scale || !c->v_scale));
 }
 
+bool valid_page_size(int P) {
+  return P == 16 || P == 32 || P == 64 || P == 128 || P == 256;
+}
+
 bool valid_shape(const rrs_kv_cache& c) {
   const int P = c.page_size;
   return (c.head_dim == 64 || c.head_dim == 128 || c.head_dim == 256) &&
-         (P == 16 || P == 32 || P == 64 || P == 128 || P == 256) && c.pages >= 1 &&
+         valid_page_size(P) && c.pages >= 1 &&
          c.kv_heads >= 1 && c.sequences >= 1 && c.max_pages >= 1 &&
          (int64_t)c.sequences * c.kv_heads < ((int64_t)1 << 23) &&
          (int64_t)c.max_pages * P <= ((int64_t)1 << 30);
+}
+
+int log2_of(int P) {
+  int l = 0;
+  while ((1 << l) < P) ++l;
+  return l;
+}
+
+bool valid_table(int sequences, int max_pages, int page_size, int pages) {
+  return valid_page_size(page_size) && sequences >= 1 && sequences < (1 << 23) && max_pages >= 1 &&
+         (int64_t)max_pages * page_size <= ((int64_t)1 << 30) && pages >= 1 &&
+         pages <= rrs::most_pages();
 }
 
 int capacity(const rrs_kv_cache& c) { return c.max_pages * c.page_size; }
@@ -56,8 +73,6 @@ bool aligned(const rrs_kv_cache& c) {
 
 rrs::KvView view(const rrs_kv_cache& c) {
   const bool q = has_scales(c);
-  int log_page = 0;
-  while ((1 << log_page) < c.page_size) ++log_page;
   return rrs::KvView{static_cast<uint8_t*>(c.k),
                      static_cast<uint8_t*>(c.v),
                      q ? static_cast<uint16_t*>(c.k_scale) : nullptr,
@@ -65,7 +80,7 @@ rrs::KvView view(const rrs_kv_cache& c) {
                      c.table,
                      c.pages,
                      c.kv_heads,
-                     log_page,
+                     log2_of(c.page_size),
                      c.head_dim,
                      c.sequences,
                      c.max_pages,
@@ -134,6 +149,45 @@ rrs_status debug_check_places(const rrs_kv_cache& c, const int32_t* seq, const i
       return RRS_ERR_PRECONDITION;
     }
   }
+  return RRS_OK;
+}
+
+// Lengths not negative and within the table, and the pages below them within the pool.
+rrs_status debug_check_table(const int32_t* table, int sequences, int max_pages, int page_size,
+                             int pages, const int32_t* lengths, void* stream) {
+  rrs_kv_cache c{};
+  c.table = table;
+  c.pages = pages;
+  c.page_size = page_size;
+  c.sequences = sequences;
+  c.max_pages = max_pages;
+  return debug_check_lengths(c, lengths, max_pages * page_size, stream);
+}
+
+// Pages of the cache; no page is written twice or both read and written.
+rrs_status debug_check_pairs(const rrs_kv_cache& c, const int32_t* src, const int32_t* dst, int n,
+                             const int32_t* count, void* stream) {
+  int32_t pairs = n;
+  if (count) {
+    if (rrs_status e = debug_fetch(&pairs, count, sizeof(pairs), stream)) return e;
+    if (pairs < 0 || pairs > n) {
+      std::fprintf(stderr, "[rrs] RRS_DEBUG: count = %d is outside [0, %d]\n", (int)pairs, n);
+      return RRS_ERR_PRECONDITION;
+    }
+  }
+  if (pairs == 0) return RRS_OK;
+  if (rrs_status e = debug_check_range(src, (size_t)pairs, 0, c.pages, "src", stream)) return e;
+  if (rrs_status e = debug_check_range(dst, (size_t)pairs, 0, c.pages, "dst", stream)) return e;
+  std::unique_ptr<int32_t[]> s, d;
+  if (rrs_status e = debug_fetch_new(&s, src, (size_t)pairs, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&d, dst, (size_t)pairs, stream)) return e;
+  std::sort(d.get(), d.get() + pairs);
+  for (int i = 0; i < pairs; ++i)
+    if ((i > 0 && d[(size_t)i] == d[(size_t)i - 1]) ||
+        std::binary_search(d.get(), d.get() + pairs, s[(size_t)i])) {
+      std::fprintf(stderr, "[rrs] RRS_DEBUG: a page in dst is there twice, or in src\n");
+      return RRS_ERR_PRECONDITION;
+    }
   return RRS_OK;
 }
 
@@ -339,6 +393,94 @@ rrs_status rrs_kv_read(const rrs_kv_cache* cache, const int32_t* lengths, int ma
   return from_hip(rrs::launch_kv_read(view(c), lengths, max_length, static_cast<uint16_t*>(K),
                                       static_cast<uint16_t*>(V),
                                       static_cast<hipStream_t>(stream)));
+}
+
+size_t rrs_kv_fork_workspace_bytes(int sequences, int max_pages, int page_size, int pages) {
+  return valid_table(sequences, max_pages, page_size, pages)
+             ? rrs::fork_workspace_bytes(sequences, pages)
+             : 0;
+}
+
+rrs_status rrs_kv_fork(const int32_t* table, int sequences, int max_pages, int page_size, int pages,
+                       const int32_t* lengths, const int32_t* parent, const int32_t* room,
+                       int32_t* table_out, int32_t* lengths_out, int32_t* room_out, int32_t* src,
+                       int32_t* dst, int32_t* count, void* workspace, size_t workspace_bytes,
+                       void* stream) {
+  const bool debug = debug_enabled();
+  if (debug)
+    std::fprintf(stderr, "[rrs] kv_fork table=%p sequences=%d max_pages=%d page_size=%d pages=%d\n",
+                 (const void*)table, sequences, max_pages, page_size, pages);
+  if (!table || !lengths || !room || !table_out || !lengths_out || !room_out || !src || !dst ||
+      !count || !workspace)
+    return RRS_ERR_NULL;
+  if (!valid_table(sequences, max_pages, page_size, pages)) return RRS_ERR_SHAPE;
+  for (const void* p : {(const void*)table, (const void*)lengths, (const void*)parent,
+                        (const void*)room, (const void*)table_out, (const void*)lengths_out,
+                        (const void*)room_out, (const void*)src, (const void*)dst,
+                        (const void*)count, (const void*)workspace})
+    if (!is_aligned(p)) return RRS_ERR_ALIGN;
+  if (workspace_bytes < rrs::fork_workspace_bytes(sequences, pages)) return RRS_ERR_WORKSPACE;
+  if (rrs_status s = check_device()) return s;
+  if (debug)
+    if (rrs_status s =
+            debug_check_table(table, sequences, max_pages, page_size, pages, lengths, stream))
+      return s;
+  const rrs::ForkArgs a{table,  sequences, max_pages, log2_of(page_size), pages,
+                        lengths, parent,   room,      table_out,          lengths_out,
+                        room_out, src,     dst,       count};
+  return from_hip(rrs::launch_kv_fork(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t rrs_kv_compact_workspace_bytes(int sequences, int max_pages, int page_size, int pages) {
+  return valid_table(sequences, max_pages, page_size, pages) ? rrs::compact_workspace_bytes(pages)
+                                                             : 0;
+}
+
+rrs_status rrs_kv_compact(const int32_t* table, int sequences, int max_pages, int page_size,
+                          int pages, const int32_t* lengths, int32_t* table_out, int32_t* src,
+                          int32_t* dst, int32_t* count, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  const bool debug = debug_enabled();
+  if (debug)
+    std::fprintf(stderr,
+                 "[rrs] kv_compact table=%p sequences=%d max_pages=%d page_size=%d pages=%d\n",
+                 (const void*)table, sequences, max_pages, page_size, pages);
+  if (!table || !lengths || !table_out || !src || !dst || !count || !workspace)
+    return RRS_ERR_NULL;
+  if (!valid_table(sequences, max_pages, page_size, pages)) return RRS_ERR_SHAPE;
+  for (const void* p : {(const void*)table, (const void*)lengths, (const void*)table_out,
+                        (const void*)src, (const void*)dst, (const void*)count,
+                        (const void*)workspace})
+    if (!is_aligned(p)) return RRS_ERR_ALIGN;
+  if (workspace_bytes < rrs::compact_workspace_bytes(pages)) return RRS_ERR_WORKSPACE;
+  if (rrs_status s = check_device()) return s;
+  if (debug)
+    if (rrs_status s =
+            debug_check_table(table, sequences, max_pages, page_size, pages, lengths, stream))
+      return s;
+  const rrs::CompactArgs a{table,   sequences, max_pages, log2_of(page_size), pages,
+                           lengths, table_out, src,       dst,                count};
+  return from_hip(rrs::launch_kv_compact(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+rrs_status rrs_kv_copy_pages(const rrs_kv_cache* cache, const int32_t* src, const int32_t* dst,
+                             int n, const int32_t* count, void* stream) {
+  const bool debug = debug_enabled();
+  if (debug) debug_print("kv_copy_pages", cache);
+  if (!src || !dst || any_null(cache)) return RRS_ERR_NULL;
+  const rrs_kv_cache& c = *cache;
+  if (!valid_shape(c) || n < 1) return RRS_ERR_SHAPE;
+  if (!valid_format(c)) return RRS_ERR_FLAGS;
+  // Bytes of a page are counted in 31 bits.
+  if ((int64_t)c.kv_heads * c.page_size * view(c).row_bytes() >= ((int64_t)1 << 31))
+    return RRS_ERR_SHAPE;
+  if (!aligned(c) || !is_aligned(src) || !is_aligned(dst) || !is_aligned(count))
+    return RRS_ERR_ALIGN;
+  if (rrs_status s = check_device()) return s;
+  if (debug)
+    if (rrs_status s = debug_check_pairs(c, src, dst, n, count, stream)) return s;
+  return from_hip(rrs::launch_kv_copy_pages(view(c), src, dst, n, count,
+                                            static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

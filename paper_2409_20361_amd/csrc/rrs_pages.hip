@@ -1,0 +1,514 @@
+// Pages of a cache: rows of the page table forked, trimmed, freed and extended (kv_fork), pages in use
+// moved to the front of the pool (kv_compact), and the pages themselves copied (kv_copy_pages). gfx950 only.
+//
+// No reference counts are kept: which pages are free follows from the table and the lengths, so
+// every plan marks the pages that its rows keep, ranks the others by their numbers and hands
+// them out in the order of rows. That is integer work on a few bytes per page and entry:
+// latency bounds it. One workgroup does all of it where the table is small: pages are bits in LDS,
+// ranks are popcounts. Larger tables are marked and written by the whole card, with the
+// one workgroup between them.
+//
+// Copies: a page of a head is one run of memory, so a page is two runs of bytes (and two of scales),
+// cut into pieces of 16 KB. Bound by HBM.
+#include <algorithm>
+
+#include "rrs_device.h"
+#include "rrs_kv.h"
+
+namespace rrs {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / 64;
+
+// Tables up to so many entries, and pools up to so many pages, are planned in one launch.
+constexpr int kSmallEntries = 32768;
+constexpr int kSmallPages = 65536;
+constexpr int kMostPages = 1 << 20;  // bits in LDS
+constexpr int kFar = 1 << 29;        // running sums stop here
+
+__device__ __forceinline__ int load_agent(const int* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// Inclusive prefix sum over the workgroup, and the total. scratch: kPlanWaves ints.
+__device__ __forceinline__ int block_prefix(int x, int* scratch, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int mine = wave_prefix(x);
+  __syncthreads();
+  if (lane == 63) scratch[wave] = mine;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    before += w < wave ? scratch[w] : 0;
+    all += scratch[w];
+  }
+  *total = all;
+  return before + mine;
+}
+
+// Per page: entries that name it, rows that are about to write into it, and the first of these.
+struct PageInfo {
+  int* refs;
+  int* writers;
+  int* first;  // S - row, 0: none
+};
+
+// What is planned for a row of the new table.
+struct RowPlan {
+  int parent;  // row of the old table; -1: none
+  int have;    // entries taken over
+  int total;   // entries in the end
+  int begin;   // rank of its first fresh page; bit 31: that one replaces entry have - 1
+};
+
+struct ForkPlan {
+  PageInfo info;
+  RowPlan* rows;
+  int* fresh;  // pages handed out, by rank
+};
+
+struct Row {
+  int parent, kept, want, have, total, last;  // last: the shared page it may write into, or -1
+};
+__device__ __forceinline__ Row fork_row(const ForkArgs& a, int b) {
+  Row r{-1, 0, 0, 0, 0, -1};
+  const int p = a.parent ? a.parent[b] : b;
+  if (p < 0 || p >= a.sequences) return r;
+  const int P = 1 << a.log_page, capacity = a.max_pages << a.log_page;
+  r.parent = p;
+  r.want = min(max(a.room[b], 0), capacity);
+  r.kept = min(min(max(a.lengths[p], 0), capacity), r.want);
+  r.have = (r.kept + P - 1) >> a.log_page;
+  r.total = (r.want + P - 1) >> a.log_page;
+  if (r.want > r.kept && (r.kept & (P - 1)) != 0) {
+    r.last = a.table[(size_t)p * a.max_pages + r.have - 1];
+    if ((uint32_t)r.last >= (uint32_t)a.pages) r.last = -1;
+  }
+  return r;
+}
+
+// A row's fresh pages where the first writer of a page that has no reader keeps it, and where none does.
+struct Need {
+  bool copy, copy_tight;
+  int some, tight;
+};
+__device__ __forceinline__ Need needs(const ForkArgs& a, const PageInfo& info, const Row& r, int b) {
+  Need n{};
+  if (r.last >= 0) {
+    const int refs = load_agent(info.refs + r.last);
+    n.copy_tight = refs > 1;
+    n.copy = n.copy_tight && !(load_agent(info.writers + r.last) == refs &&
+                               load_agent(info.first + r.last) == a.sequences - b);
+  }
+  const int grown = min(r.total - r.have, a.pages + 1);
+  n.some = min(grown + n.copy, a.pages + 1);
+  n.tight = min(grown + n.copy_tight, a.pages + 1);
+  return n;
+}
+
+// An entry of the new table.
+__device__ __forceinline__ int fork_entry(const ForkArgs& a, const RowPlan& r, const int* fresh,
+                                          int i) {
+  const int copy = (uint32_t)r.begin >> 31, begin = r.begin & 0x7FFFFFFF;
+  if (i < r.have - copy) return a.table[(size_t)r.parent * a.max_pages + i];
+  if (i < r.total) return fresh[begin + i - (r.have - copy)];
+  return -1;
+}
+
+// The plan, by one workgroup. kMarks: it marks the pages itself and writes the table, too;
+// else `info` holds the marks of another launch. kWords: of 32 pages.
+template <int kWords, bool kMarks>
+__global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkArgs a, ForkPlan plan) {
+  __shared__ uint32_t used[kWords];
+  __shared__ uint32_t wanted[kMarks ? kWords : 1];  // pages that a row is about to write into
+  __shared__ int scratch[kPlanWaves];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int words = (a.pages + 31) / 32;
+  if constexpr (kMarks) {
+    for (int w = t; w < words; w += kPlanThreads) used[w] = wanted[w] = 0;
+    __syncthreads();
+    for (int b = t; b < a.sequences; b += kPlanThreads) {
+      const Row r = fork_row(a, b);
+      if (r.last < 0) continue;
+      atomicOr(&wanted[r.last / 32], 1u << (r.last % 32));
+      // Atomics, as what follows on them: they meet in the L2.
+      atomicExch(plan.info.refs + r.last, 0);
+      atomicExch(plan.info.writers + r.last, 0);
+      atomicExch(plan.info.first + r.last, 0);
+    }
+    __threadfence();
+    __syncthreads();
+    for (int b = wave; b < a.sequences; b += kPlanWaves) {
+      const Row r = fork_row(a, b);
+      for (int i = lane; i < r.have; i += 64) {
+        const int page = a.table[(size_t)r.parent * a.max_pages + i];
+        if ((uint32_t)page >= (uint32_t)a.pages) continue;
+        atomicOr(&used[page / 32], 1u << (page % 32));
+        if (wanted[page / 32] >> (page % 32) & 1) atomicAdd(plan.info.refs + page, 1);
+      }
+      if (lane == 0 && r.last >= 0) {
+        atomicAdd(plan.info.writers + r.last, 1);
+        atomicMax(plan.info.first + r.last, a.sequences - b);
+      }
+    }
+    __threadfence();
+  } else {
+    for (int w = wave; w < (words + 1) / 2; w += kPlanWaves) {
+      const int page = 64 * w + lane;
+      const uint64_t bits = __ballot(page < a.pages && plan.info.refs[min(page, a.pages - 1)] > 0);
+      if (lane == 0) {
+        used[2 * w] = (uint32_t)bits;
+        if (2 * w + 1 < words) used[2 * w + 1] = (uint32_t)(bits >> 32);
+      }
+    }
+  }
+  __syncthreads();
+
+  // Free pages of the thread's words, and of all.
+  const int per_thread = (words + kPlanThreads - 1) / kPlanThreads;
+  const int w0 = min(t * per_thread, words), w1 = min(w0 + per_thread, words);
+  const auto free_bits = [&](int w) {
+    const int left = a.pages - 32 * w;
+    return ~used[w] & (left >= 32 ? ~0u : (1u << left) - 1);
+  };
+  int mine = 0, free_pages;
+  for (int w = w0; w < w1; ++w) mine += __popc(free_bits(w));
+  const int free_upto = block_prefix(mine, scratch, &free_pages);
+
+  // Do all rows get what they need?
+  int sum = 0;
+  for (int b = t; b < a.sequences; b += kPlanThreads)
+    sum = min(sum + needs(a, plan.info, fork_row(a, b), b).some, kMostPages + 1);
+  int all;
+  block_prefix(sum, scratch, &all);
+  const bool tight = all > free_pages;
+
+  int carry = 0, copies = 0, taken = 0;
+  for (int b0 = 0; b0 < a.sequences; b0 += kPlanThreads) {
+    const int b = b0 + t;
+    Row r{-1, 0, 0, 0, 0, -1};
+    Need n{};
+    if (b < a.sequences) {
+      r = fork_row(a, b);
+      n = needs(a, plan.info, r, b);
+    }
+    const int need = tight ? n.tight : n.some;
+    int chunk, more;
+    const int upto = min(carry, kFar) + block_prefix(need, scratch, &chunk);
+    const bool served = need == 0 || upto <= free_pages;
+    const bool copy = served && (tight ? n.copy_tight : n.copy);
+    const int rank = copies + block_prefix(copy, scratch, &more) - 1;
+    int last_taken;
+    block_prefix(served ? need : 0, scratch, &last_taken);
+    if (b < a.sequences) {
+      RowPlan out{r.parent, r.have, served ? r.total : r.have, served ? upto - need : 0};
+      if (copy) {
+        out.begin |= (int)0x80000000;
+        a.src[rank] = r.last;
+        a.dst[rank] = upto - need;  // a rank, for now
+      }
+      plan.rows[b] = out;
+      a.lengths_out[b] = r.kept;
+      a.room_out[b] = served ? r.want : r.kept;
+    }
+    carry = min(min(carry, kFar) + chunk, kFar);
+    copies += more;
+    taken += last_taken;
+  }
+  if (t == 0) {
+    a.count[0] = copies;
+    a.count[1] = free_pages - taken;
+  }
+  // The pages of the first ranks.
+  int rank = free_upto - mine;
+  for (int w = w0; w < w1 && rank < taken; ++w)
+    for (uint32_t bits = free_bits(w); bits && rank < taken; bits &= bits - 1)
+      plan.fresh[rank++] = 32 * w + __builtin_ctz(bits);
+  __threadfence_block();
+  __syncthreads();
+  for (int i = t; i < a.sequences; i += kPlanThreads) {
+    if (i < copies) {
+      a.dst[i] = plan.fresh[a.dst[i]];
+    } else {
+      a.src[i] = -1;
+      a.dst[i] = -1;
+    }
+  }
+  if constexpr (kMarks)
+    for (int b = wave; b < a.sequences; b += kPlanWaves) {
+      const RowPlan r = plan.rows[b];
+      for (int i = lane; i < a.max_pages; i += 64)
+        a.table_out[(size_t)b * a.max_pages + i] = fork_entry(a, r, plan.fresh, i);
+    }
+}
+
+// Units of work on the whole card: `kColumns` entries of a row, a wave each.
+constexpr int kColumns = 512;
+template <typename F>
+__device__ __forceinline__ void for_rows(int sequences, int columns, F f) {
+  const int per_row = (columns + kColumns - 1) / kColumns;
+  const long long units = (long long)sequences * per_row;
+  const int waves = kThreads / 64;
+  for (long long u = (long long)blockIdx.x * waves + (threadIdx.x >> 6); u < units;
+       u += (long long)gridDim.x * waves) {
+    const int b = (int)(u / per_row), i0 = (int)(u % per_row) * kColumns;
+    f(b, i0, min(i0 + kColumns, columns));
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) zero_kernel(int* p, int n) {
+  for (int i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) p[i] = 0;
+}
+
+__global__ void __launch_bounds__(kThreads) fork_mark_kernel(ForkArgs a, PageInfo info) {
+  const int lane = threadIdx.x & 63;
+  for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
+    const Row r = fork_row(a, b);
+    for (int i = i0 + lane; i < min(i1, r.have); i += 64) {
+      const int page = a.table[(size_t)r.parent * a.max_pages + i];
+      if ((uint32_t)page < (uint32_t)a.pages) atomicAdd(info.refs + page, 1);
+    }
+    if (i0 == 0 && lane == 0 && r.last >= 0) {
+      atomicAdd(info.writers + r.last, 1);
+      atomicMax(info.first + r.last, a.sequences - b);
+    }
+  });
+}
+
+__global__ void __launch_bounds__(kThreads) fork_write_kernel(ForkArgs a, ForkPlan plan) {
+  const int lane = threadIdx.x & 63;
+  for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
+    const RowPlan r = plan.rows[b];
+    for (int i = i0 + lane; i < i1; i += 64)
+      a.table_out[(size_t)b * a.max_pages + i] = fork_entry(a, r, plan.fresh, i);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// Compaction. U pages are in use; those from U on move, in order, to the unused ones below U.
+// ---------------------------------------------------------------------------------------------
+
+__device__ __forceinline__ int row_pages(const CompactArgs& a, int b) {
+  const int capacity = a.max_pages << a.log_page;
+  return (min(max(a.lengths[b], 0), capacity) + (1 << a.log_page) - 1) >> a.log_page;
+}
+
+// to: of a page that moves the new number.
+__device__ __forceinline__ int compact_entry(const CompactArgs& a, const int* to, int used, int b,
+                                             int i, int have) {
+  if (i >= have) return -1;
+  const int page = a.table[(size_t)b * a.max_pages + i];
+  return page >= used && page < a.pages ? to[page] : page;
+}
+
+// flags: marks of another launch (else the kernel's own; it then writes the table, too).
+template <int kWords, bool kMarks>
+__global__ void __launch_bounds__(kPlanThreads)
+    compact_plan_kernel(CompactArgs a, const int* flags, int* to) {
+  __shared__ uint32_t used[kWords];
+  __shared__ int scratch[kPlanWaves];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int words = (a.pages + 31) / 32;
+  if constexpr (kMarks) {
+    for (int w = t; w < words; w += kPlanThreads) used[w] = 0;
+    __syncthreads();
+    for (int b = wave; b < a.sequences; b += kPlanWaves) {
+      const int have = row_pages(a, b);
+      for (int i = lane; i < have; i += 64) {
+        const int page = a.table[(size_t)b * a.max_pages + i];
+        if ((uint32_t)page < (uint32_t)a.pages) atomicOr(&used[page / 32], 1u << (page % 32));
+      }
+    }
+  } else {
+    for (int w = wave; w < (words + 1) / 2; w += kPlanWaves) {
+      const int page = 64 * w + lane;
+      const uint64_t bits = __ballot(page < a.pages && flags[min(page, a.pages - 1)] > 0);
+      if (lane == 0) {
+        used[2 * w] = (uint32_t)bits;
+        if (2 * w + 1 < words) used[2 * w + 1] = (uint32_t)(bits >> 32);
+      }
+    }
+  }
+  __syncthreads();
+  const int per_thread = (words + kPlanThreads - 1) / kPlanThreads;
+  const int w0 = min(t * per_thread, words), w1 = min(w0 + per_thread, words);
+  int mine = 0, U;
+  for (int w = w0; w < w1; ++w) mine += __popc(used[w]);
+  block_prefix(mine, scratch, &U);
+  // Bits of a word below page U.
+  const auto below = [&](int w) {
+    const int n = U - 32 * w;
+    return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1;
+  };
+  int movers = 0, holes = 0, moves, same;
+  for (int w = w0; w < w1; ++w) {
+    movers += __popc(used[w] & ~below(w));
+    holes += __popc(~used[w] & below(w));
+  }
+  int mover = block_prefix(movers, scratch, &moves) - movers;
+  int hole = block_prefix(holes, scratch, &same) - holes;
+  for (int w = w0; w < w1; ++w) {
+    for (uint32_t bits = used[w] & ~below(w); bits; bits &= bits - 1)
+      a.src[mover++] = 32 * w + __builtin_ctz(bits);
+    for (uint32_t bits = ~used[w] & below(w); bits; bits &= bits - 1)
+      a.dst[hole++] = 32 * w + __builtin_ctz(bits);
+  }
+  if (t == 0) {
+    a.count[0] = moves;
+    a.count[1] = U;
+  }
+  __threadfence_block();
+  __syncthreads();
+  const int size = max(1, a.pages / 2);
+  for (int i = t; i < size; i += kPlanThreads) {
+    if (i < moves) {
+      to[a.src[i]] = a.dst[i];
+    } else {
+      a.src[i] = -1;
+      a.dst[i] = -1;
+    }
+  }
+  if constexpr (kMarks) {
+    __threadfence_block();
+    __syncthreads();
+    for (int b = wave; b < a.sequences; b += kPlanWaves) {
+      const int have = row_pages(a, b);
+      for (int i = lane; i < a.max_pages; i += 64)
+        a.table_out[(size_t)b * a.max_pages + i] = compact_entry(a, to, U, b, i, have);
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kThreads) compact_mark_kernel(CompactArgs a, int* flags) {
+  const int lane = threadIdx.x & 63;
+  for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
+    for (int i = i0 + lane; i < min(i1, row_pages(a, b)); i += 64) {
+      const int page = a.table[(size_t)b * a.max_pages + i];
+      if ((uint32_t)page < (uint32_t)a.pages) flags[page] = 1;
+    }
+  });
+}
+
+__global__ void __launch_bounds__(kThreads) compact_write_kernel(CompactArgs a, const int* to) {
+  const int lane = threadIdx.x & 63, used = a.count[1];
+  for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
+    const int have = row_pages(a, b);
+    for (int i = i0 + lane; i < i1; i += 64)
+      a.table_out[(size_t)b * a.max_pages + i] = compact_entry(a, to, used, b, i, have);
+  });
+}
+
+// ---------------------------------------------------------------------------------------------
+// Copies
+// ---------------------------------------------------------------------------------------------
+
+constexpr int kAtOnce = 4;                             // loads in flight per thread
+constexpr int kChunk = kThreads * kAtOnce * 16;        // bytes of a piece
+
+// Units: pieces of k, then of v, then the scales of both, of each pair.
+__global__ void __launch_bounds__(kThreads)
+    copy_pages_kernel(KvView c, const int32_t* src, const int32_t* dst, const int32_t* count, int n,
+                      size_t page_bytes, int pieces, int per_pair, int scale_rows) {
+  const long long pairs = count ? min(max(*count, 0), n) : n;
+  const long long units = pairs * per_pair;
+  for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    const int pair = (int)(u / per_pair), part = (int)(u % per_pair);
+    const int from = src[pair], to = dst[pair];
+    if ((uint32_t)from >= (uint32_t)c.pages || (uint32_t)to >= (uint32_t)c.pages) continue;
+    if (part == 2 * pieces) {
+      for (int i = threadIdx.x; i < scale_rows; i += kThreads) {
+        c.k_scale[(size_t)to * scale_rows + i] = c.k_scale[(size_t)from * scale_rows + i];
+        c.v_scale[(size_t)to * scale_rows + i] = c.v_scale[(size_t)from * scale_rows + i];
+      }
+      continue;
+    }
+    uint8_t* pool = part < pieces ? c.k : c.v;
+    const size_t at = (size_t)(part % pieces) * kChunk;
+    const size_t size = min(page_bytes - at, (size_t)kChunk);
+    const v4u* in = reinterpret_cast<const v4u*>(pool + from * page_bytes + at);
+    v4u* out = reinterpret_cast<v4u*>(pool + to * page_bytes + at);
+    v4u x[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+      if ((size_t)(i * kThreads + threadIdx.x) * 16 < size) x[i] = in[i * kThreads + threadIdx.x];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)
+      if ((size_t)(i * kThreads + threadIdx.x) * 16 < size) out[i * kThreads + threadIdx.x] = x[i];
+  }
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+unsigned row_grid(int sequences, int columns) {
+  const long long units = (long long)sequences * ((columns - 1) / kColumns + 1);
+  return (unsigned)std::min<long long>((units + 3) / 4, 2048);
+}
+
+bool small(int sequences, int max_pages, int pages) {
+  return (long long)sequences * max_pages <= kSmallEntries && pages <= kSmallPages;
+}
+
+}  // namespace
+
+int most_pages() { return kMostPages; }
+
+size_t fork_workspace_bytes(int sequences, int pages) {
+  return align256((size_t)pages * 16) + align256((size_t)sequences * sizeof(RowPlan));
+}
+
+hipError_t launch_kv_fork(const ForkArgs& a, void* workspace, hipStream_t stream) {
+  int* ws = static_cast<int*>(workspace);
+  const size_t n = (size_t)a.pages;
+  ForkPlan plan{{ws, ws + n, ws + 2 * n},
+                reinterpret_cast<RowPlan*>(static_cast<uint8_t*>(workspace) + align256(n * 16)),
+                ws + 3 * n};
+  if (small(a.sequences, a.max_pages, a.pages)) {
+    fork_plan_kernel<kSmallPages / 32, true><<<1, kPlanThreads, 0, stream>>>(a, plan);
+    return hipGetLastError();
+  }
+  const unsigned grid = row_grid(a.sequences, a.max_pages);
+  zero_kernel<<<std::min((3 * a.pages - 1) / kThreads + 1, 1024), kThreads, 0, stream>>>(
+      ws, 3 * a.pages);
+  fork_mark_kernel<<<grid, kThreads, 0, stream>>>(a, plan.info);
+  fork_plan_kernel<kMostPages / 32, false><<<1, kPlanThreads, 0, stream>>>(a, plan);
+  fork_write_kernel<<<grid, kThreads, 0, stream>>>(a, plan);
+  return hipGetLastError();
+}
+
+size_t compact_workspace_bytes(int pages) { return align256((size_t)pages * 8); }
+
+hipError_t launch_kv_compact(const CompactArgs& a, void* workspace, hipStream_t stream) {
+  int* flags = static_cast<int*>(workspace);
+  int* to = flags + a.pages;
+  if (small(a.sequences, a.max_pages, a.pages)) {
+    compact_plan_kernel<kSmallPages / 32, true><<<1, kPlanThreads, 0, stream>>>(a, flags, to);
+    return hipGetLastError();
+  }
+  const unsigned grid = row_grid(a.sequences, a.max_pages);
+  zero_kernel<<<std::min((a.pages - 1) / kThreads + 1, 1024), kThreads, 0, stream>>>(flags,
+                                                                                    a.pages);
+  compact_mark_kernel<<<grid, kThreads, 0, stream>>>(a, flags);
+  compact_plan_kernel<kMostPages / 32, false><<<1, kPlanThreads, 0, stream>>>(a, flags, to);
+  compact_write_kernel<<<grid, kThreads, 0, stream>>>(a, to);
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_copy_pages(const KvView& c, const int32_t* src, const int32_t* dst, int n,
+                                const int32_t* count, hipStream_t stream) {
+  const size_t rows = (size_t)c.heads << c.log_page;
+  const size_t bytes = rows * c.row_bytes();
+  const int pieces = (int)((bytes - 1) / kChunk + 1);
+  const bool scales = c.format != kCacheF16;
+  const int scale_rows = (int)(c.format == kCacheFp8 ? rows / kSlots8 : rows);
+  const int per_pair = 2 * pieces + (scales ? 1 : 0);
+  const long long units = (long long)n * per_pair;
+  const unsigned grid = (unsigned)std::min<long long>(units, 256 * 8);
+  copy_pages_kernel<<<grid, kThreads, 0, stream>>>(c, src, dst, count, n, bytes, pieces, per_pair,
+                                                   scale_rows);
+  return hipGetLastError();
+}
+
+}  // namespace rrs

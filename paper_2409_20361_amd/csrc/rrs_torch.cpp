@@ -12,8 +12,10 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cmath>
 #include <string>
+#include <vector>
 
 #include "rrs.h"
 
@@ -199,6 +201,49 @@ struct Span {
 };
 
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
+
+// The first `outputs` spans share memory with none of the others.
+void apart(const char* call, const Span* spans, size_t outputs, size_t count) {
+  for (size_t i = 0; i < outputs; ++i)
+    for (size_t j = i + 1; j < count; ++j)
+      if (spans[i].meets(spans[j]))
+        raise(PyExc_ValueError, std::string(call) + ": " + spans[i].name + " and " +
+                                    spans[j].name + " must not overlap");
+}
+
+// A tuple of new tensors.
+PyObject* wrap_all(const at::Tensor* t, int n) {
+  PyObject* r = PyTuple_New(n);
+  for (int i = 0; r && i < n; ++i) {
+    PyObject* x = wrap(t[i]);
+    if (!x) {
+      Py_DECREF(r);
+      return nullptr;
+    }
+    PyTuple_SET_ITEM(r, i, x);
+  }
+  return r;
+}
+
+// int32 outputs: new ones, or those of the caller's tuple.
+struct Int32Out {
+  at::Tensor made[6];
+  int32_t* p[6];
+  Int32Out(PyObject* out, const char* const* names, const std::vector<int64_t>* shapes, int n,
+           const at::Tensor& like, at::Device on, const char* what) {
+    if (out != Py_None && (!PyTuple_Check(out) || PyTuple_GET_SIZE(out) != n))
+      raise(PyExc_TypeError, what);
+    for (int i = 0; i < n; ++i) {
+      if (out == Py_None) {
+        made[i] = at::empty(shapes[i], like.options());
+        p[i] = static_cast<int32_t*>(made[i].data_ptr());
+      } else {
+        p[i] = static_cast<int32_t*>(
+            dev(PyTuple_GET_ITEM(out, i), names[i], at::kInt, shapes[i], on));
+      }
+    }
+  }
+};
 
 #define RRS_CALL(name)                                                              \
   PyObject* name##_body(PyObject* const* a, Py_ssize_t n);                          \
@@ -462,6 +507,128 @@ RRS_CALL(kv_read) {
   return both;
 }
 
+// table, lengths, parent, room, pages, page_size, out, workspace
+RRS_CALL(kv_fork) {
+  arguments(n, 8, "kv_fork");
+  const at::Device on = gpu_of(a[0], "table");
+  const at::Tensor& table = tensor(a[0], "table");
+  if (table.dim() != 2) raise(PyExc_ValueError, "table must have 2 dimensions");
+  const int32_t* tp = static_cast<const int32_t*>(dev(a[0], "table", at::kInt, table.sizes(), on));
+  const int64_t S = table.size(0), C = table.size(1);
+  if (S > INT32_MAX || C > INT32_MAX) raise(PyExc_ValueError, "table is too large");
+  const void* lp = dev(a[1], "lengths", at::kInt, {S}, on);
+  const void* pp = dev_or_null(a[2], "parent", at::kInt, {S}, on);
+  const void* rp = dev(a[3], "room", at::kInt, {S}, on);
+  const int pages = to_int(a[4], "pages"), page_size = to_int(a[5], "page_size");
+  static const char* const names[] = {"table_out", "lengths_out", "room_out", "src", "dst", "count"};
+  const std::vector<int64_t> shapes[] = {{S, C}, {S}, {S}, {S}, {S}, {2}};
+  const Int32Out out(a[6], names, shapes, 6, table, on,
+                     "out must be a tuple (table, lengths, room, src, dst, count)");
+  const size_t need = rrs_kv_fork_workspace_bytes((int)S, (int)C, page_size, pages);
+  const Workspace ws(a[7], need, on);
+  if (a[6] != Py_None || a[7] != Py_None) {
+    const size_t row = (size_t)S * 4, all = (size_t)S * C * 4;
+    const Span spans[] = {{"workspace", ws.p, need}, {names[0], out.p[0], all},
+                          {names[1], out.p[1], row}, {names[2], out.p[2], row},
+                          {names[3], out.p[3], row}, {names[4], out.p[4], row},
+                          {names[5], out.p[5], 8},   {"table", tp, all},
+                          {"lengths", lp, row},      {"parent", pp, pp ? row : 0},
+                          {"room", rp, row}};
+    apart("kv_fork", spans, 7, sizeof(spans) / sizeof(spans[0]));
+  }
+  const Launch launch(on);
+  const rrs_status s =
+      rrs_kv_fork(tp, (int)S, (int)C, page_size, pages, static_cast<const int32_t*>(lp),
+                  static_cast<const int32_t*>(pp), static_cast<const int32_t*>(rp), out.p[0],
+                  out.p[1], out.p[2], out.p[3], out.p[4], out.p[5], ws.p, ws.bytes, launch.stream);
+  if (s != RRS_OK) return check(s, "rrs_kv_fork", nullptr);
+  return a[6] != Py_None ? Py_NewRef(a[6]) : wrap_all(out.made, 6);
+}
+
+// table, lengths, pages, page_size, out, workspace
+RRS_CALL(kv_compact) {
+  arguments(n, 6, "kv_compact");
+  const at::Device on = gpu_of(a[0], "table");
+  const at::Tensor& table = tensor(a[0], "table");
+  if (table.dim() != 2) raise(PyExc_ValueError, "table must have 2 dimensions");
+  const int32_t* tp = static_cast<const int32_t*>(dev(a[0], "table", at::kInt, table.sizes(), on));
+  const int64_t S = table.size(0), C = table.size(1);
+  if (S > INT32_MAX || C > INT32_MAX) raise(PyExc_ValueError, "table is too large");
+  const void* lp = dev(a[1], "lengths", at::kInt, {S}, on);
+  const int pages = to_int(a[2], "pages"), page_size = to_int(a[3], "page_size");
+  if (pages < 1) raise(PyExc_ValueError, "pages must be positive");
+  const int64_t moves = std::max(1, pages / 2);
+  static const char* const names[] = {"table_out", "src", "dst", "count"};
+  const std::vector<int64_t> shapes[] = {{S, C}, {moves}, {moves}, {2}};
+  const Int32Out out(a[4], names, shapes, 4, table, on,
+                     "out must be a tuple (table, src, dst, count)");
+  const size_t need = rrs_kv_compact_workspace_bytes((int)S, (int)C, page_size, pages);
+  const Workspace ws(a[5], need, on);
+  if (a[4] != Py_None || a[5] != Py_None) {
+    const size_t all = (size_t)S * C * 4, list = (size_t)moves * 4;
+    const Span spans[] = {{"workspace", ws.p, need}, {names[0], out.p[0], all},
+                          {names[1], out.p[1], list}, {names[2], out.p[2], list},
+                          {names[3], out.p[3], 8},    {"table", tp, all},
+                          {"lengths", lp, (size_t)S * 4}};
+    apart("kv_compact", spans, 5, sizeof(spans) / sizeof(spans[0]));
+  }
+  const Launch launch(on);
+  const rrs_status s = rrs_kv_compact(tp, (int)S, (int)C, page_size, pages,
+                                      static_cast<const int32_t*>(lp), out.p[0], out.p[1],
+                                      out.p[2], out.p[3], ws.p, ws.bytes, launch.stream);
+  if (s != RRS_OK) return check(s, "rrs_kv_compact", nullptr);
+  return a[4] != Py_None ? Py_NewRef(a[4]) : wrap_all(out.made, 4);
+}
+
+// sequences, max_pages, page_size, pages
+RRS_CALL(kv_fork_workspace_bytes) {
+  arguments(n, 4, "kv_fork_workspace_bytes");
+  return PyLong_FromSize_t(
+      rrs_kv_fork_workspace_bytes(to_int(a[0], "sequences"), to_int(a[1], "max_pages"),
+                                  to_int(a[2], "page_size"), to_int(a[3], "pages")));
+}
+RRS_CALL(kv_compact_workspace_bytes) {
+  arguments(n, 4, "kv_compact_workspace_bytes");
+  return PyLong_FromSize_t(
+      rrs_kv_compact_workspace_bytes(to_int(a[0], "sequences"), to_int(a[1], "max_pages"),
+                                     to_int(a[2], "page_size"), to_int(a[3], "pages")));
+}
+
+// cache (5), src, dst, count
+RRS_CALL(kv_copy_pages) {
+  arguments(n, 8, "kv_copy_pages");
+  const at::Device on = gpu_of(a[0], "k");
+  const Cache cache(a, on);
+  const at::Tensor& src = tensor(a[5], "src");
+  const int64_t pairs = src.dim() == 1 ? src.size(0) : -1;
+  if (pairs < 0 || pairs > INT32_MAX) raise(PyExc_ValueError, "src must have 1 dimension");
+  const void* sp = dev(a[5], "src", at::kInt, {pairs}, on);
+  const void* dp = dev(a[6], "dst", at::kInt, {pairs}, on);
+  const void* cp = nullptr;
+  if (a[7] != Py_None) {
+    const at::Tensor& count = gpu_tensor(a[7], "count", at::kInt, on);
+    if (count.numel() < 1) raise(PyExc_ValueError, "count must not be empty");
+    cp = dev(a[7], "count", at::kInt, count.sizes(), on);
+  }
+  if (pairs == 0) Py_RETURN_NONE;
+  // The lists are read while pages are written.
+  const size_t pool = THPVariable_Unpack(a[0]).nbytes();
+  const size_t scales = a[3] == Py_None ? 0 : THPVariable_Unpack(a[3]).nbytes();
+  const Span spans[] = {{"k", cache.c.k, pool},
+                        {"v", cache.c.v, pool},
+                        {"k_scale", cache.c.k_scale, scales},
+                        {"v_scale", cache.c.v_scale, scales},
+                        {"src", sp, (size_t)pairs * 4},
+                        {"dst", dp, (size_t)pairs * 4},
+                        {"count", cp, cp ? (size_t)4 : 0}};
+  apart("kv_copy_pages", spans, 4, sizeof(spans) / sizeof(spans[0]));
+  const Launch launch(on);
+  return check(rrs_kv_copy_pages(&cache.c, static_cast<const int32_t*>(sp),
+                                 static_cast<const int32_t*>(dp), (int)pairs,
+                                 static_cast<const int32_t*>(cp), launch.stream),
+               "rrs_kv_copy_pages", Py_NewRef(Py_None));
+}
+
 // The exception type for a status other than RRS_OK.
 PyObject* set_error(PyObject*, PyObject* type) {
   Py_INCREF(type);
@@ -477,6 +644,11 @@ PyMethodDef kMethods[] = {RRS_METHOD(rope_kv_append),
                           RRS_METHOD(kv_evict),
                           RRS_METHOD(kv_evict_workspace_bytes),
                           RRS_METHOD(kv_read),
+                          RRS_METHOD(kv_fork),
+                          RRS_METHOD(kv_fork_workspace_bytes),
+                          RRS_METHOD(kv_compact),
+                          RRS_METHOD(kv_compact_workspace_bytes),
+                          RRS_METHOD(kv_copy_pages),
                           {"set_error", set_error, METH_O, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 
