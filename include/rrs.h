@@ -693,6 +693,37 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Causal attention of new tokens over the caches of their sequences (the tokens' own keys and values appended
+ * before): whole prompts, parts of them, or a few tokens per sequence. With n = row_start[b + 1] -
+ * row_start[b] tokens, the last n of sequence b's lengths[b] slots are theirs:
+ *   out[row_start[b] + i, h] = sum_t p_t v_t,  p = softmax over t <= lengths[b] - n + i of scale q . k_t.
+ *   Q         in : M x heads x head_dim float16, the tokens of one sequence after those of another;
+ *                  heads as in rrs_paged_attention.
+ *   row_start in : sequences + 1 int32, not decreasing, in [0, M] (cut to it): the sequences' rows.
+ *   max_tokens   : 1 <= max_tokens <= M, at least every n (a longer run is cut to its first max_tokens
+ *                  rows, as the last of the cache). Launch and workspace follow from it and from max_length.
+ *   lengths, max_length, mask, scale: as in rrs_paged_attention.
+ *   out      out : M x heads x head_dim float16; zeros for a token that sees no slot. Rows of no
+ *                  sequence are left as they were.
+ *   lse      out : NULL, or M x heads float32, as in rrs_paged_attention.
+ *   workspace    : at least rrs_prompt_attention_workspace_bytes (may be 0: then NULL will do);
+ *                  contents ignored.
+ * RRS_KV_INT4 rows stand for fp16(q s), as rrs_kv_read gives them (of a scale of 9360 for 9352 q). Logits,
+ * softmax and sums in float32; for the product with V the weights are rounded to float16 in units of their own:
+ * off by 2^-11 relative, or by 2^-37 of the row's largest one where that is more. Results repeat bit for bit
+ * for the same arguments; they depend on other sequences through max_tokens and max_length only, which
+ * decide where sums are cut. max_tokens * heads / kv_heads < 2^31 - 128; with r = sequences * kv_heads
+ * and t = max_tokens * heads / kv_heads / 128 rounded up, r t (times the pieces that the slots are cut
+ * into) < 2^24 workgroups.
+ */
+size_t rrs_prompt_attention_workspace_bytes(const rrs_kv_cache* cache, int heads, int max_tokens,
+                                            int max_length);
+rrs_status rrs_prompt_attention(const void* Q, int M, int heads, const rrs_kv_cache* cache,
+                                const int32_t* row_start, int max_tokens, const int32_t* lengths,
+                                int max_length, float scale, const uint8_t* mask, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Eviction by accumulated attention weight. For every sequence and KV head, of the slots
  * below n = lengths[b] the first `budget` are kept in this order: protected slots
  * (slot_pos >= keep_from[b]), then larger weight, then lower slot (a NaN weight counts as

@@ -65,6 +65,8 @@ from ._kv import (  # noqa: F401
     kv_read,
     paged_attention,
     paged_attention_workspace_bytes,
+    prompt_attention,
+    prompt_attention_workspace_bytes,
     rope_kv_append,
     rope_table,
 )
@@ -74,7 +76,8 @@ __all__ = [
     "kv_compact_workspace_bytes", "kv_copy_pages", "kv_evict", "kv_evict_workspace_bytes", "kv_fork",
     "kv_fork_workspace_bytes",
     "kv_read", "paged_attention",
-    "paged_attention_workspace_bytes", "rope_kv_append", "rope_table",
+    "paged_attention_workspace_bytes", "prompt_attention", "prompt_attention_workspace_bytes",
+    "rope_kv_append", "rope_table",
     "REORDER_BLOCK", "SCHEME_PER_CHANNEL", "SCHEME_RUNTIME_SMOOTH", "SCHEME_SUB_CHANNEL",
     "SKIP_ROTATION", "SKIP_SMOOTHING", "WEIGHT_TILED", "RRSError", "gemm_path", "gemm_scratch_bytes", "lib", "lib_path", "linear", "linear_noalloc", "linear_reorder",
     "linear_reorder_workspace_bytes", "linear_workspace_bytes",

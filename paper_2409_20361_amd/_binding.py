@@ -73,6 +73,9 @@ _SIGNATURES = {
                                       _sz, _vp]),
     "rrs_kv_evict_workspace_bytes": (_sz, [_vp, _i, _i]),
     "rrs_kv_read": (ctypes.c_int32, [_vp, _vp, _i, _vp, _vp, _vp]),
+    "rrs_prompt_attention_workspace_bytes": (_sz, [_vp, _i, _i, _i]),
+    "rrs_prompt_attention": (ctypes.c_int32, [_vp, _i, _i, _vp, _vp, _i, _vp, _i, _f, _vp, _vp,
+                                              _vp, _vp, _sz, _vp]),
     "rrs_kv_fork": (ctypes.c_int32, [_vp, _i, _i, _i, _i] + [_vp] * 10 + [_sz, _vp]),
     "rrs_kv_fork_workspace_bytes": (_sz, [_i, _i, _i, _i]),
     "rrs_kv_compact": (ctypes.c_int32, [_vp, _i, _i, _i, _i] + [_vp] * 6 + [_sz, _vp]),

@@ -134,6 +134,30 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, lengths: torch.Tensor,
                                                 weights, return_lse, workspace, out)
 
 
+def prompt_attention_workspace_bytes(cache: KVCache, heads: int, max_tokens: int,
+                                     max_length: int) -> int:
+    return (_module or _load()).prompt_attention_workspace_bytes(*cache, heads, max_tokens,
+                                                                 max_length)
+
+
+def prompt_attention(Q: torch.Tensor, cache: KVCache, row_start: torch.Tensor,
+                     lengths: torch.Tensor, max_tokens: Optional[int] = None,
+                     max_length: Optional[int] = None, scale: Optional[float] = None,
+                     mask: Optional[torch.Tensor] = None, return_lse: bool = False,
+                     workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None):
+    """Causal attention of every sequence's new tokens over its cache: prompts, parts of them, or a few tokens.
+
+    Q: M x heads x head dim fp16, sequence b's tokens in rows row_start[b] to row_start[b + 1], appended to
+    the cache before as its last ones; row_start: (sequences + 1,) int32; lengths: (sequences,) int32,
+    the new tokens included; max_tokens, max_length: bounds on a sequence's rows and length (None: M and
+    the cache's capacity), by which launches and workspace are chosen, so best tight ones; scale, mask: as
+    paged_attention's. Returns the output (as Q; rows of no sequence as they were in `out`), or (output,
+    lse) with lse (M, heads) float32."""
+    return (_module or _load()).prompt_attention(Q, *cache, row_start, lengths, max_tokens,
+                                                 max_length, scale, mask, return_lse, workspace,
+                                                 out)
+
+
 def kv_evict_workspace_bytes(cache: KVCache, max_length: int, budget: int) -> int:
     return (_module or _load()).kv_evict_workspace_bytes(*cache, max_length, budget)
 

@@ -25,16 +25,18 @@ SOURCES = ["rrs_api.cpp", "rrs_gemm_route.cpp", "rrs_quant.hip", "rrs_weight.hip
            "rrs_gemm_small.hip", "rrs_gemm_decode.hip", "rrs_quant_wave.hip", "rrs_reorder.hip", "rrs_quant_rows.hip",
            "rrs_gemm_stream.hip", "rrs_gemm_stream_gather.hip", "rrs_gemm_mid.hip",
            "rrs_gemm_fp6.hip", "rrs_noalloc.hip", "rrs_kv_api.cpp", "rrs_kv_append.hip",
-           "rrs_attention.hip", "rrs_evict.hip", "rrs_pages.hip"]
+           "rrs_attention.hip", "rrs_evict.hip", "rrs_pages.hip",
+           "rrs_prompt.hip"]
 
 # Per-source code-generation options on top of COMMON.
 # rrs_gemm_stream_gather.hip: keep MFMA results in VGPRs (the per-block
 #   rescale reads every accumulator; in AGPRs each read is an extra copy).
 # rrs_gemm_fp6.hip: the same (every partial is read by the rescale).
-# rrs_attention.hip: the same (logits are read by the softmax, sums rescaled).
+# rrs_attention.hip, rrs_prompt.hip: the same (logits are read by the softmax, sums rescaled).
 EXTRA = {"rrs_gemm_stream_gather.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
          "rrs_gemm_fp6.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-         "rrs_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+         "rrs_attention.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+         "rrs_prompt.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in any kernel.
 # -ffp-contract=off: every rounding in the rotation and scale chain is an

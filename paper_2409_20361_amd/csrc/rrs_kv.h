@@ -100,6 +100,24 @@ bool attention_fits(const KvView& c, int heads, int max_length, bool with_weight
 size_t attention_workspace_bytes(const KvView& c, int heads, int max_length, bool with_weights);
 hipError_t launch_paged_attention(const AttentionArgs& a, const KvView& c, hipStream_t stream);
 
+struct PromptArgs {
+  const uint16_t* Q;
+  int M;
+  int heads;
+  const int32_t* row_start;
+  int max_tokens;
+  const int32_t* lengths;
+  int max_length;
+  float scale;
+  const uint8_t* mask;  // or nullptr
+  uint16_t* out;
+  float* lse;  // or nullptr
+};
+bool prompt_fits(const KvView& c, int heads, int max_tokens, int max_length);
+size_t prompt_workspace_bytes(const KvView& c, int heads, int max_tokens, int max_length);
+hipError_t launch_prompt_attention(const PromptArgs& a, const KvView& c, void* workspace,
+                                   hipStream_t stream);
+
 struct EvictArgs {
   const int32_t* lengths;
   int max_length;

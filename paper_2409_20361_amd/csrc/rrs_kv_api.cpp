@@ -191,6 +191,23 @@ rrs_status debug_check_pairs(const rrs_kv_cache& c, const int32_t* src, const in
   return RRS_OK;
 }
 
+// Row numbers that do not decrease, within [0, M], of at most max_tokens rows per sequence.
+rrs_status debug_check_starts(const int32_t* row_start, int sequences, int M, int max_tokens,
+                              void* stream) {
+  const size_t count = (size_t)sequences + 1;
+  if (rrs_status e = debug_check_range(row_start, count, 0, (int64_t)M + 1, "row_start", stream))
+    return e;
+  std::unique_ptr<int32_t[]> h;
+  if (rrs_status e = debug_fetch_new(&h, row_start, count, stream)) return e;
+  for (size_t b = 0; b + 1 < count; ++b)
+    if (h[b + 1] < h[b] || h[b + 1] - h[b] > max_tokens) {
+      std::fprintf(stderr, "[rrs] RRS_DEBUG: sequence %zu has rows [%d, %d), max_tokens = %d\n", b,
+                   (int)h[b], (int)h[b + 1], max_tokens);
+      return RRS_ERR_PRECONDITION;
+    }
+  return RRS_OK;
+}
+
 // FP8: no block of 16 slots gets its tokens from two runs of rows.
 rrs_status debug_check_runs(const rrs_kv_cache& c, const int32_t* seq, const int32_t* slot, int M,
                             void* stream) {
@@ -336,6 +353,49 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
   const rrs::AttentionArgs a{static_cast<const uint16_t*>(Q), heads, lengths, max_length, scale,
                              mask, weights, static_cast<uint16_t*>(out), lse, workspace};
   return from_hip(rrs::launch_paged_attention(a, view(c), static_cast<hipStream_t>(stream)));
+}
+
+size_t rrs_prompt_attention_workspace_bytes(const rrs_kv_cache* cache, int heads, int max_tokens,
+                                            int max_length) {
+  if (!cache || !valid_shape(*cache) || !valid_format(*cache) || !valid_heads(*cache, heads) ||
+      max_tokens < 1 || max_length < 1 || max_length > capacity(*cache) ||
+      !rrs::prompt_fits(view(*cache), heads, max_tokens, max_length))
+    return 0;
+  return rrs::prompt_workspace_bytes(view(*cache), heads, max_tokens, max_length);
+}
+
+rrs_status rrs_prompt_attention(const void* Q, int M, int heads, const rrs_kv_cache* cache,
+                                const int32_t* row_start, int max_tokens, const int32_t* lengths,
+                                int max_length, float scale, const uint8_t* mask, void* out,
+                                float* lse, void* workspace, size_t workspace_bytes,
+                                void* stream) {
+  const bool debug = debug_enabled();
+  if (debug) debug_print("prompt_attention", cache);
+  if (!Q || !row_start || !lengths || !out || any_null(cache)) return RRS_ERR_NULL;
+  const rrs_kv_cache& c = *cache;
+  if (!valid_shape(c) || !valid_heads(c, heads) || M < 1 || max_tokens < 1 || max_tokens > M ||
+      max_length < 1 || max_length > capacity(c) ||
+      !rrs::prompt_fits(view(c), heads, max_tokens, max_length))
+    return RRS_ERR_SHAPE;
+  if (!valid_format(c) || !std::isfinite(scale)) return RRS_ERR_FLAGS;
+  const size_t need = rrs::prompt_workspace_bytes(view(c), heads, max_tokens, max_length);
+  if (need > 0 && !workspace) return RRS_ERR_NULL;
+  if (!aligned(c) || !is_aligned(Q) || !is_aligned(row_start) || !is_aligned(lengths) ||
+      !is_aligned(mask) || !is_aligned(out) || !is_aligned(lse) || !is_aligned(workspace))
+    return RRS_ERR_ALIGN;
+  if (workspace_bytes < need) return RRS_ERR_WORKSPACE;
+  if (rrs_status s = check_device()) return s;
+  if (debug) {
+    if (rrs_status s = debug_check_starts(row_start, c.sequences, M, max_tokens, stream)) return s;
+    if (rrs_status s = debug_check_finite_f16(
+            Q, (size_t)M * (size_t)heads * (size_t)c.head_dim, "Q", stream))
+      return s;
+    if (rrs_status s = debug_check_lengths(c, lengths, max_length, stream)) return s;
+  }
+  const rrs::PromptArgs a{static_cast<const uint16_t*>(Q), M, heads, row_start, max_tokens,
+                          lengths, max_length, scale, mask, static_cast<uint16_t*>(out), lse};
+  return from_hip(rrs::launch_prompt_attention(a, view(c), workspace,
+                                               static_cast<hipStream_t>(stream)));
 }
 
 size_t rrs_kv_evict_workspace_bytes(const rrs_kv_cache* cache, int max_length, int budget) {

@@ -1,0 +1,567 @@
+// Causal attention of every sequence's new tokens over its paged cache. gfx950 only.
+//
+// For a sequence and a KV head the rows are its new tokens times the query heads that share the
+// head: row r is head r % group of token r / group, so all of them read the same keys and values, and a few
+// tokens fill a tile as well as many. A workgroup takes 128 rows, a wave 32, and walks
+// along the slots in tiles (64, or 32 at head dim 256) that its threads bring through registers to LDS, as
+// float16 whatever the cache holds (INT4 as fp16(q s), FP8 exactly), two tiles in turn:
+//   S^T = K Q^T    mfma 32x32x16, keys from LDS, queries in registers;
+//   p = 2^(S - m)  a lane holds one row's p of 16 of 32 slots (lanes l and l + 32 share a row);
+//   O^T += V^T P^T values from LDS, transposed (ds_read_b64_tr), in the order of slots that the lane's p
+//                  have, so that P goes from one product's result into the other's operand.
+// p is rounded to float16 in units that leave a row's largest at 2^12 or more, as in the attention
+// of single tokens; sums are float32. Bound by the matrix instructions and, next to them, the
+// exponentials: 4 D flops and one exponential per row and slot.
+//
+// Where the rows do not fill the card, the slots are cut into pieces, joined by a second kernel in order.
+//
+// Slots that a row must not see get p = 0. What is there may still not be finite, and 0 times
+// it is NaN: slots past the end and under the mask are 0 in LDS; of tiles on the diagonal the
+// numbers that are not finite are, too, and are added to the rows that do see them afterwards.
+#include <algorithm>
+#include <type_traits>
+
+#include "rrs_device.h"
+#include "rrs_kv.h"
+
+namespace rrs {
+namespace {
+
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) v4s* lds_v4s;
+
+constexpr int kThreads = 256;
+constexpr int kRows = 128;  // of a workgroup
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kLift = 12;
+constexpr float kRoom = 15.0f;
+
+template <int D, int kFormat>
+struct Tile {
+  static constexpr int kSlots = D == 256 ? 32 : 64;
+  static constexpr int kBlocks = kSlots / 32;
+  static constexpr int kSteps = D / 16;   // mfma steps of a logit
+  static constexpr int kOut = D / 32;     // blocks of output channels
+  static constexpr int kBytes = kSlots * D * 2;
+  // Loads: 16 bytes per thread, kLanes threads to a row.
+  static constexpr int kRow = kFormat == kCacheInt4 ? D / 2 : kFormat == kCacheFp8 ? D : 2 * D;
+  static constexpr int kLanes = kRow / 16;
+  static constexpr int kRowsAtOnce = kThreads / kLanes;
+  static constexpr int kPasses = kSlots > kRowsAtOnce ? kSlots / kRowsAtOnce : 1;
+  static constexpr int kPerSimd = D == 256 ? 1 : 2;
+
+  // Byte of 16-byte chunk c of slot t. Keys are read 16 rows at a time, a chunk of each; values four
+  // rows, four neighbouring chunks of each: both then touch all banks.
+  static constexpr int kPerLine = 2 * D < 256 ? 256 / (2 * D) : 1;  // rows of a line of banks
+  static __device__ __forceinline__ int key_at(int t, int c) {
+    const int x = t / kPerLine & (D / 8 < 16 ? D / 8 - 1 : 15);
+    return t * (2 * D) + ((c ^ x) << 4);
+  }
+  static __device__ __forceinline__ int value_at(int t, int c) {
+    const int x = (t / kPerLine & (D / 8 < 16 ? D / 32 - 1 : 3)) << 2;
+    return t * (2 * D) + ((c ^ x) << 4);
+  }
+};
+
+struct Plan {
+  int group;
+  int tiles;   // of rows, per sequence and KV head
+  int pieces;  // of the slots, per tile
+  int pairs;   // sequences x KV heads
+  bool by_xcd;
+  float* part;    // pairs x tiles x pieces x kRows x D: sums relative to m; nullptr: one piece
+  float2* stats;  // the same without D: m (base 2) and the sum of p
+};
+
+__device__ __forceinline__ float larger(float a, float b) {
+  return __builtin_elementwise_maximum(a, b);
+}
+// The larger of the two lanes of a row.
+__device__ __forceinline__ float row_max(float x) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return larger(__builtin_bit_cast(float, (uint32_t)a[0]),
+                __builtin_bit_cast(float, (uint32_t)a[1]));
+}
+
+__device__ __forceinline__ float log_sum(float m, float sum) {
+  if (sum == 0.0f) return -INFINITY;
+  const float e = m + (float)__builtin_amdgcn_frexp_expf(sum);
+  return (e + __builtin_amdgcn_logf(__builtin_amdgcn_frexp_mantf(sum))) / kLog2e;
+}
+
+// Eight INT4 codes times s, each rounded once: fp16(q s). The largest scale there is, 9360, counts as
+// the float16 below it, so that 7 s is finite.
+__device__ __forceinline__ v4u eight_int4(uint32_t w, _Float16 s) {
+  const v2h s2 = {s, s};
+  const v2h off = {(_Float16)1032.0f, (_Float16)1032.0f};
+  uint32_t y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {  // codes i and i + 4: exact as 1024 + code + 8
+    const uint32_t x = ((w >> (4 * i)) & 0x000F000Fu) ^ 0x64086408u;
+    y[i] = __builtin_bit_cast(uint32_t, (__builtin_bit_cast(v2h, x) - off) * s2);
+  }
+  return v4u{__builtin_amdgcn_perm(y[1], y[0], 0x05040100u),
+             __builtin_amdgcn_perm(y[3], y[2], 0x05040100u),
+             __builtin_amdgcn_perm(y[1], y[0], 0x07060302u),
+             __builtin_amdgcn_perm(y[3], y[2], 0x07060302u)};
+}
+
+// Halves of w that are not finite: a bit for each (0 and 16).
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  const uint32_t e = w & 0x7C007C00u;
+  return ((e + 0x04000400u) >> 15) & 0x00010001u;
+}
+
+// Where a tile of rows belongs: new tokens [0, count) of sequence b, the first of which is row `first` of
+// Q and sees slots [0, seen).
+struct Where {
+  int b, hk, tile, piece, count, seen, length;
+  size_t first;
+};
+__device__ __forceinline__ bool find_tile(const PromptArgs& a, const KvView& c, const Plan& plan,
+                                          Where* w) {
+  // Tiles that see most come first. Those of a pair are on one XCD and share its L2, where that
+  // leaves no XCD without work.
+  const int per = plan.tiles * plan.pieces;
+  int pair, k;
+  if (plan.by_xcd) {
+    pair = blockIdx.x / (8 * per) * 8 + blockIdx.x % 8;
+    if (pair >= plan.pairs) return false;
+    k = blockIdx.x / 8 % per;
+  } else {
+    pair = blockIdx.x % plan.pairs;
+    k = blockIdx.x / plan.pairs;
+  }
+  w->tile = plan.tiles - 1 - k / plan.pieces;
+  w->piece = k % plan.pieces;
+  w->b = pair / c.heads;
+  w->hk = pair % c.heads;
+  const int start = min(max(a.row_start[w->b], 0), a.M);
+  const int end = min(max(a.row_start[w->b + 1], start), a.M);
+  w->first = start;
+  w->count = min(end - start, a.max_tokens);
+  w->length = min(max(a.lengths[w->b], 0), a.max_length);
+  w->seen = w->length - w->count + 1;
+  return (long long)w->tile * kRows < (long long)w->count * plan.group;
+}
+
+template <int D, int kFormat, bool kMask>
+__global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
+    prompt_kernel(PromptArgs a, KvView c, Plan plan) {
+  using T = Tile<D, kFormat>;
+  __shared__ __attribute__((aligned(16))) uint8_t keys[2][T::kBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t values[2][T::kBytes];
+  // Of three tiles (the one in use, the next, and the last, whose are cleared): slots with values that
+  // are not finite, and those that the mask leaves.
+  __shared__ uint32_t bad_rows[3][2];
+  __shared__ uint32_t live_slots[kMask ? 3 : 1][2];
+
+  Where at;
+  if (!find_tile(a, c, plan, &at)) return;
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = at.count * plan.group;  // below 2^31: checked by the host
+  const int row0 = at.tile * kRows;
+  const int my_row = min(row0 + 32 * wave + col, rows - 1);
+  const int token = my_row / plan.group;
+  const int head = at.hk * plan.group + my_row % plan.group;
+  const int seen = min(max(at.seen + token, 0), at.length);
+  // Slots that all, or any, of the wave's and the workgroup's rows see.
+  const auto seen_by = [&](int r) {
+    return min(max(at.seen + min(r, rows - 1) / plan.group, 0), at.length);
+  };
+  const int wave_all = seen_by(row0 + 32 * wave), wave_any = seen_by(row0 + 32 * wave + 31);
+  const int all = seen_by(row0), any = seen_by(row0 + kRows - 1);
+  const bool wave_works = row0 + 32 * wave < rows;
+
+  const int steps = (any + T::kSlots - 1) / T::kSlots;
+  const int s0 = (int)((long long)steps * at.piece / plan.pieces);
+  const int s1 = (int)((long long)steps * (at.piece + 1) / plan.pieces);
+
+  // Queries: column col, channels 16 i + 8 half ...
+  v8h q[T::kSteps];
+  const uint16_t* qrow = a.Q + ((at.first + token) * a.heads + head) * D;
+#pragma unroll
+  for (int i = 0; i < T::kSteps; ++i)
+    q[i] = *reinterpret_cast<const v8h*>(qrow + 16 * i + 8 * half);
+  // Logits are compared unscaled: a negative scale turns the queries around, and of no scale at
+  // all every logit is 0.
+  float scale = a.scale * kLog2e;
+  if (!(scale > 0.0f)) {
+    const _Float16 turn = (_Float16)(scale < 0.0f ? -1.0f : 0.0f);
+#pragma unroll
+    for (int i = 0; i < T::kSteps; ++i) q[i] *= turn;
+    scale = scale < 0.0f ? -scale : 1.0f;
+  }
+
+  v16f o[T::kOut] = {};
+  float m = -INFINITY, sum = 0.0f;
+
+  // A thread's part of a tile: rows my_slot, my_slot + kRowsAtOnce, ...
+  const int my_slot = threadIdx.x / T::kLanes, my_lane = threadIdx.x % T::kLanes;
+  const bool loads = T::kRowsAtOnce <= T::kSlots || my_slot < T::kSlots;
+  v4u key[T::kPasses], val[T::kPasses];
+  uint16_t key_scale[T::kPasses], val_scale[T::kPasses];
+  uint8_t mask[T::kPasses];
+  int page[T::kPasses];
+  const auto load_pages = [&](int step) {
+#pragma unroll
+    for (int p = 0; p < T::kPasses; ++p) {
+      const int t = min(step * T::kSlots + my_slot + p * T::kRowsAtOnce, at.length - 1);
+      page[p] = c.page_of(at.b, t >> c.log_page);
+    }
+  };
+  const auto load = [&](int step) {
+    if (!loads) return;
+#pragma unroll
+    for (int p = 0; p < T::kPasses; ++p) {
+      const int t = min(step * T::kSlots + my_slot + p * T::kRowsAtOnce, at.length - 1);
+      const size_t row = c.page_row(page[p], at.hk) + (t & ((1 << c.log_page) - 1));
+      key[p] = *reinterpret_cast<const v4u*>(c.k + row * T::kRow + 16 * my_lane);
+      val[p] = *reinterpret_cast<const v4u*>(c.v + row * T::kRow + 16 * my_lane);
+      if constexpr (kFormat != kCacheF16) {
+        const size_t s = kFormat == kCacheFp8 ? row / kSlots8 : row;
+        key_scale[p] = c.k_scale[s];
+        val_scale[p] = c.v_scale[s];
+      }
+      if constexpr (kMask) mask[p] = a.mask[(size_t)at.b * c.capacity() + t];
+    }
+  };
+  const auto store = [&](int step, int buf, int flags) {
+    if (!loads) return;
+    const bool diagonal = (step + 1) * T::kSlots > all;
+#pragma unroll
+    for (int p = 0; p < T::kPasses; ++p) {
+      const int r = my_slot + p * T::kRowsAtOnce;
+      const bool live = step * T::kSlots + r < at.length && (!kMask || mask[p] != 0);
+      if constexpr (kMask)
+        if (my_lane == 0 && live) atomicOr(&live_slots[flags][r / 32], 1u << (r % 32));
+      constexpr int kChunks = kFormat == kCacheInt4 ? 4 : kFormat == kCacheFp8 ? 2 : 1;
+      v4u k[kChunks], v[kChunks];
+      if constexpr (kFormat == kCacheInt4) {
+        _Float16 ks = __builtin_bit_cast(_Float16, key_scale[p]);
+        _Float16 vs = __builtin_bit_cast(_Float16, val_scale[p]);
+        ks = ks == (_Float16)9360.0f ? (_Float16)9352.0f : ks;
+        vs = vs == (_Float16)9360.0f ? (_Float16)9352.0f : vs;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          k[i] = eight_int4(key[p][i], ks);
+          v[i] = eight_int4(val[p][i], vs);
+        }
+      } else if constexpr (kFormat == kCacheFp8) {
+        const float ks = half_to_float(key_scale[p]), vs = half_to_float(val_scale[p]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          k[i] = dequant8_fp8(make_uint2(key[p][2 * i], key[p][2 * i + 1]), ks);
+          v[i] = dequant8_fp8(make_uint2(val[p][2 * i], val[p][2 * i + 1]), vs);
+        }
+      } else {
+        k[0] = key[p];
+        v[0] = val[p];
+      }
+      if (!live) {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) v[i] = v4u{};
+      } else if (diagonal) {
+        uint32_t found = 0;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = not_finite(v[i][e]);
+            found |= bits;
+            v[i][e] &= ~(bits * 0xFFFFu);
+          }
+        if (found) atomicOr(&bad_rows[flags][r / 32], 1u << (r % 32));
+      }
+#pragma unroll
+      for (int i = 0; i < kChunks; ++i) {
+        *reinterpret_cast<v4u*>(keys[buf] + T::key_at(r, my_lane * kChunks + i)) = k[i];
+        *reinterpret_cast<v4u*>(values[buf] + T::value_at(r, my_lane * kChunks + i)) = v[i];
+      }
+    }
+  };
+  const auto clear = [&](int flags) {
+    if (threadIdx.x < 2) {
+      bad_rows[flags][threadIdx.x] = 0;
+      if constexpr (kMask) live_slots[flags][threadIdx.x] = 0;
+    }
+  };
+
+  if (s0 < s1) {
+    clear(0);
+    clear(1);
+    load_pages(s0);
+    load(s0);
+    if (s0 + 1 < s1) load_pages(s0 + 1);
+    __syncthreads();
+    store(s0, 0, 0);
+  }
+  __syncthreads();
+  int flags = 0;
+  for (int step = s0; step < s1; ++step) {
+    const int buf = (step - s0) & 1, t0 = step * T::kSlots;
+    const int next_flags = flags == 2 ? 0 : flags + 1;
+    clear(next_flags == 2 ? 0 : next_flags + 1);
+    if (step + 1 < s1) {
+      load(step + 1);
+      if (step + 2 < s1) load_pages(step + 2);
+    }
+    if (wave_works && t0 < wave_any) {
+      v16f l[T::kBlocks];
+#pragma unroll
+      for (int u = 0; u < T::kBlocks; ++u) {
+        l[u] = v16f{};
+#pragma unroll
+        for (int i = 0; i < T::kSteps; ++i)
+          l[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              *reinterpret_cast<const v8h*>(keys[buf] + T::key_at(32 * u + col, 2 * i + half)),
+              q[i], l[u], 0, 0, 0);
+      }
+      if (kMask || t0 + T::kSlots > wave_all) {
+#pragma unroll
+        for (int u = 0; u < T::kBlocks; ++u) {
+          uint32_t on = ~0u;
+          if constexpr (kMask) on = live_slots[flags][u];
+          const int n = seen - t0 - 32 * u;  // slots of the block that the row sees
+          on &= n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
+          on >>= 4 * half;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            l[u][r] = on >> (8 * (r / 4) + r % 4) & 1 ? l[u][r] : -INFINITY;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int u = 0; u < T::kBlocks; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = larger(top, l[u][r]);
+      if (__any(top * scale > m + kRoom)) {
+        top = row_max(top) * scale;
+        const float up = fmaxf(m, top - kLift);
+        const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
+        m = up;
+        sum *= shrink;
+#pragma unroll
+        for (int j = 0; j < T::kOut; ++j) o[j] *= shrink;
+      }
+      const float base = m == -INFINITY ? 0.0f : m;
+      v8h p[2 * T::kBlocks];
+#pragma unroll
+      for (int u = 0; u < T::kBlocks; ++u)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
+          sum += x;
+          p[2 * u + r / 8][r % 8] = (_Float16)x;
+        }
+      // Lanes 4 r .. 4 r + 3 of 16 name row r: 16 channels of 4 slots; those of half h begin at 4 h
+      // and 8 + 4 h.
+      const int vt = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+      for (int w = 0; w < 2 * T::kBlocks; ++w)
+#pragma unroll
+        for (int j = 0; j < T::kOut; ++j) {
+          const uint8_t* lo = values[buf] + T::value_at(16 * w + vt, 4 * j + vc) + 8 * (lane & 1);
+          const uint8_t* hi =
+              values[buf] + T::value_at(16 * w + 8 + vt, 4 * j + vc) + 8 * (lane & 1);
+          const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)lo);
+          const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)hi);
+          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              __builtin_bit_cast(v8h, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7)), p[w],
+              o[j], 0, 0, 0);
+        }
+      // Values that are not finite, for the rows that see them.
+      if (t0 + T::kSlots > all) {
+        for (int u = 0; u < T::kBlocks; ++u)
+          for (uint32_t left = bad_rows[flags][u]; left; left &= left - 1) {
+            const int t = t0 + 32 * u + __builtin_ctz(left);
+            const size_t row = c.row_of(at.b, at.hk, t);
+            if (t >= seen) continue;
+#pragma unroll 1
+            for (int d = 0; d < D; ++d) {
+              float v;
+              if constexpr (kFormat == kCacheInt4)
+                v = half_to_float(c.v_scale[row]);
+              else if constexpr (kFormat == kCacheFp8)
+                v = (c.v[row * D + d] & 127) == 127 ? NAN : 0.0f;
+              else
+                v = half_to_float(reinterpret_cast<const uint16_t*>(c.v)[row * D + d]);
+              if (kFormat == kCacheInt4) v = v - v == 0.0f ? 0.0f : NAN;
+              if (v - v == 0.0f || (d >> 2 & 1) != half) continue;
+#pragma unroll
+              for (int j = 0; j < T::kOut; ++j)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                  if (32 * j + 8 * (r / 4) + 4 * half + r % 4 == d) o[j][r] += v;
+            }
+          }
+      }
+    }
+    if (step + 1 < s1) store(step + 1, buf ^ 1, next_flags);
+    __syncthreads();
+    flags = next_flags;
+  }
+
+  {
+    const uint32_t u = __builtin_bit_cast(uint32_t, sum);
+    const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    sum = __builtin_bit_cast(float, (uint32_t)x[0]) + __builtin_bit_cast(float, (uint32_t)x[1]);
+  }
+  if (row0 + 32 * wave + col >= rows) return;
+  if (plan.part) {
+    const size_t unit =
+        (((size_t)(at.b * c.heads + at.hk) * plan.tiles + at.tile) * plan.pieces + at.piece) *
+            kRows + 32 * wave + col;
+    if (half == 0) plan.stats[unit] = make_float2(m, sum);
+    float* out = plan.part + unit * D;
+#pragma unroll
+    for (int j = 0; j < T::kOut; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; r += 4)
+        *reinterpret_cast<v4f*>(out + 32 * j + 2 * r + 4 * half) =
+            v4f{o[j][r], o[j][r + 1], o[j][r + 2], o[j][r + 3]};
+    return;
+  }
+  const size_t row = (at.first + token) * a.heads + head;
+  const float inv = sum != 0.0f ? 1.0f / sum : 0.0f;  // (NaN where the sum is)
+  uint16_t* out = a.out + row * D;
+#pragma unroll
+  for (int j = 0; j < T::kOut; ++j)
+#pragma unroll
+    for (int r = 0; r < 16; r += 4)
+      *reinterpret_cast<v4h*>(out + 32 * j + 2 * r + 4 * half) =
+          v4h{(_Float16)(o[j][r] * inv), (_Float16)(o[j][r + 1] * inv),
+              (_Float16)(o[j][r + 2] * inv), (_Float16)(o[j][r + 3] * inv)};
+  if (half == 0 && a.lse) a.lse[row] = log_sum(m, sum);
+}
+
+// Pieces of a row joined: D / 4 threads to a row. Grid: pairs x tiles x groups of rows.
+template <int D>
+__global__ void __launch_bounds__(kThreads)
+    prompt_join_kernel(PromptArgs a, KvView c, Plan plan) {
+  constexpr int kAtOnce = kThreads / (D / 4);
+  constexpr int kGroups = kRows / kAtOnce;
+  const int unit = blockIdx.x / kGroups;
+  const int pair = unit / plan.tiles, tile = unit % plan.tiles;
+  const int b = pair / c.heads, hk = pair % c.heads;
+  const int r = blockIdx.x % kGroups * kAtOnce + threadIdx.x / (D / 4);
+  const int d = threadIdx.x % (D / 4) * 4;
+  const int start = min(max(a.row_start[b], 0), a.M);
+  const int end = min(max(a.row_start[b + 1], start), a.M);
+  const long long my_row = (long long)tile * kRows + r;
+  if (my_row >= (long long)min(end - start, a.max_tokens) * plan.group) return;
+  const size_t first = (size_t)unit * plan.pieces * kRows + r;
+  float top = -INFINITY;
+  for (int i = 0; i < plan.pieces; ++i)
+    top = fmaxf(top, plan.stats[first + (size_t)i * kRows].x);
+  const float base = top == -INFINITY ? 0.0f : top;
+  float total = 0.0f;
+  v4f acc = {};
+#pragma unroll 4
+  for (int i = 0; i < plan.pieces; ++i) {
+    const size_t at = first + (size_t)i * kRows;
+    const float2 st = plan.stats[at];
+    const float f = __builtin_amdgcn_exp2f(st.x - base);
+    total += st.y * f;
+    acc += *reinterpret_cast<const v4f*>(plan.part + at * D + d) * f;
+  }
+  const float inv = total != 0.0f ? 1.0f / total : 0.0f;
+  const size_t row = ((size_t)start + my_row / plan.group) * a.heads + hk * plan.group +
+                     my_row % plan.group;
+  *reinterpret_cast<v4h*>(a.out + row * D + d) =
+      v4h{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv),
+          (_Float16)(acc[3] * inv)};
+  if (d == 0 && a.lse) a.lse[row] = log_sum(top, total);
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+long long units_of(const Plan& p) { return (long long)p.pairs * p.tiles * p.pieces; }
+long long first_grid(const Plan& p) {
+  return (p.by_xcd ? ((long long)p.pairs + 7) / 8 * 8 : p.pairs) * p.tiles * p.pieces;
+}
+long long second_grid(const Plan& p, int dim) {
+  return p.pieces > 1 ? (long long)p.pairs * p.tiles * (kRows / (kThreads / (dim / 4))) : 0;
+}
+
+Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void* workspace,
+               size_t* bytes) {
+  Plan p{};
+  p.group = heads / c.heads;
+  p.pairs = c.sequences * c.heads;
+  p.by_xcd = p.pairs % 8 == 0 || p.pairs >= 64;
+  p.tiles = (int)(((long long)max_tokens * p.group - 1) / kRows + 1);
+  // Pieces, of four steps at least, where the tiles alone do not fill the card.
+  const int slots = c.dim == 256 ? 32 : 64;
+  const long long resident = c.dim == 256 ? 256 : 512;
+  const long long units = (long long)p.pairs * p.tiles;
+  const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
+  p.pieces = (int)std::min(most, std::max(1ll, resident / units));
+  const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * kRows : 0;
+  const size_t stats = align256(rows * sizeof(float2));
+  *bytes = stats + rows * c.dim * 4;
+  if (workspace && rows) {
+    p.stats = static_cast<float2*>(workspace);
+    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + stats);
+  }
+  return p;
+}
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+template <int D>
+hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
+  const unsigned grid = (unsigned)first_grid(p);
+  const auto run = [&](auto format) {
+    constexpr int f = decltype(format)::value;
+    if (a.mask)
+      prompt_kernel<D, f, true><<<grid, kThreads, 0, stream>>>(a, c, p);
+    else
+      prompt_kernel<D, f, false><<<grid, kThreads, 0, stream>>>(a, c, p);
+  };
+  switch (c.format) {
+    case kCacheInt4: run(Int<kCacheInt4>()); break;
+    case kCacheFp8: run(Int<kCacheFp8>()); break;
+    default: run(Int<kCacheF16>());
+  }
+  if (hipError_t e = hipGetLastError()) return e;
+  if (p.pieces > 1)
+    prompt_join_kernel<D><<<(unsigned)second_grid(p, D), kThreads, 0, stream>>>(a, c, p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+bool prompt_fits(const KvView& c, int heads, int max_tokens, int max_length) {
+  // Rows of a sequence and KV head are numbered in 31 bits.
+  if ((long long)max_tokens * (heads / c.heads) >= (1ll << 31) - kRows) return false;
+  size_t bytes;
+  const Plan p = make_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
+  return fits_grid(first_grid(p), kThreads) && fits_grid(second_grid(p, c.dim), kThreads);
+}
+
+size_t prompt_workspace_bytes(const KvView& c, int heads, int max_tokens, int max_length) {
+  size_t bytes;
+  make_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
+  return bytes;
+}
+
+hipError_t launch_prompt_attention(const PromptArgs& a, const KvView& c, void* workspace,
+                                   hipStream_t stream) {
+  size_t bytes;
+  const Plan p = make_plan(c, a.heads, a.max_tokens, a.max_length, workspace, &bytes);
+  switch (c.dim) {
+    case 64: return launch<64>(a, c, p, stream);
+    case 128: return launch<128>(a, c, p, stream);
+    default: return launch<256>(a, c, p, stream);
+  }
+}
+
+}  // namespace rrs

@@ -374,6 +374,79 @@ RRS_CALL(paged_attention) {
   return both;
 }
 
+// Q, cache (5), row_start, lengths, max_tokens, max_length, scale, mask, return_lse, workspace, out
+RRS_CALL(prompt_attention) {
+  arguments(n, 15, "prompt_attention");
+  const at::Device on = gpu_of(a[0], "Q");
+  const Cache cache(a + 1, on);
+  const at::Tensor& Q = tensor(a[0], "Q");
+  const int64_t B = cache.sequences, M = Q.dim() == 3 ? Q.size(0) : 0;
+  const int64_t heads = Q.dim() == 3 ? Q.size(1) : 0;
+  if (heads > INT32_MAX || M > INT32_MAX) raise(PyExc_ValueError, "Q is too large");
+  const int64_t shape[3] = {M, heads, cache.dim};
+  const void* qp = dev(a[0], "Q", at::kHalf, shape, on);
+  const void* sp = dev(a[6], "row_start", at::kInt, {B + 1}, on);
+  const void* lp = dev(a[7], "lengths", at::kInt, {B}, on);
+  const int tokens = a[8] == Py_None ? (int)M : to_int(a[8], "max_tokens");
+  const int top = cache.bound(a[9]);
+  double scale = 1.0 / std::sqrt((double)cache.dim);
+  if (a[10] != Py_None) {
+    scale = PyFloat_AsDouble(a[10]);
+    if (scale == -1.0 && PyErr_Occurred()) throw Raised{};
+  }
+  const void* mp = dev_or_null(a[11], "mask", at::kBool, {B, cache.capacity}, on);
+  const bool want_lse = to_bool(a[12]);
+  at::Tensor made, lse;
+  void* yp;
+  if (a[14] == Py_None) {
+    made = at::empty(shape, Q.options());
+    yp = made.data_ptr();
+  } else {
+    yp = dev(a[14], "out", at::kHalf, shape, on);
+  }
+  if (want_lse) lse = at::empty({M, heads}, Q.options().dtype(at::kFloat));
+  const size_t need = rrs_prompt_attention_workspace_bytes(&cache.c, (int)heads, tokens, top);
+  const Workspace ws(a[13], need, on);
+  const size_t rows = (size_t)(M * heads * cache.dim) * 2;
+  if (a[13] != Py_None || a[14] != Py_None) {
+    const size_t pool = THPVariable_Unpack(a[1]).nbytes();
+    const size_t scales = a[4] == Py_None ? 0 : THPVariable_Unpack(a[4]).nbytes();
+    const Span spans[] = {{"workspace", ws.p, need},
+                          {"out", yp, rows},
+                          {"Q", qp, rows},
+                          {"row_start", sp, (size_t)(B + 1) * 4},
+                          {"lengths", lp, (size_t)B * 4},
+                          {"mask", mp, mp ? (size_t)(B * cache.capacity) : 0},
+                          {"table", cache.c.table, (size_t)B * cache.c.max_pages * 4},
+                          {"k", cache.c.k, pool},
+                          {"v", cache.c.v, pool},
+                          {"k_scale", cache.c.k_scale, scales},
+                          {"v_scale", cache.c.v_scale, scales}};
+    apart("prompt_attention", spans, 2, sizeof(spans) / sizeof(spans[0]));
+  }
+  const Launch launch(on);
+  const rrs_status s = rrs_prompt_attention(
+      qp, (int)M, (int)heads, &cache.c, static_cast<const int32_t*>(sp), tokens,
+      static_cast<const int32_t*>(lp), top, (float)scale, static_cast<const uint8_t*>(mp), yp,
+      want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr, ws.p, ws.bytes, launch.stream);
+  if (s != RRS_OK) return check(s, "rrs_prompt_attention", nullptr);
+  PyObject* y = a[14] == Py_None ? wrap(made) : Py_NewRef(a[14]);
+  if (!want_lse || !y) return y;
+  PyObject* l = wrap(lse);
+  PyObject* both = l ? PyTuple_Pack(2, y, l) : nullptr;
+  Py_DECREF(y);
+  Py_XDECREF(l);
+  return both;
+}
+
+// cache (5), heads, max_tokens, max_length
+RRS_CALL(prompt_attention_workspace_bytes) {
+  arguments(n, 8, "prompt_attention_workspace_bytes");
+  const Cache cache(a, gpu_of(a[0], "k"));
+  return PyLong_FromSize_t(rrs_prompt_attention_workspace_bytes(
+      &cache.c, to_int(a[5], "heads"), to_int(a[6], "max_tokens"), to_int(a[7], "max_length")));
+}
+
 // cache (5), heads, max_length, with_weights
 RRS_CALL(paged_attention_workspace_bytes) {
   arguments(n, 8, "paged_attention_workspace_bytes");
@@ -644,6 +717,8 @@ PyMethodDef kMethods[] = {RRS_METHOD(rope_kv_append),
                           RRS_METHOD(kv_evict),
                           RRS_METHOD(kv_evict_workspace_bytes),
                           RRS_METHOD(kv_read),
+                          RRS_METHOD(prompt_attention),
+                          RRS_METHOD(prompt_attention_workspace_bytes),
                           RRS_METHOD(kv_fork),
                           RRS_METHOD(kv_fork_workspace_bytes),
                           RRS_METHOD(kv_compact),
