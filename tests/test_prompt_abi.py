@@ -25,7 +25,7 @@ def test_caches():
 
 
 @pytest.mark.parametrize("kw,want", [
-    *[({n: None}, A.NULL) for n in ("Q", "cache", "row_start", "lengths", "out")],
+    *[({n: None}, A.NULL) for n in ("Q", "row_start", "lengths", "out")],
     (dict(heads=0), A.SHAPE), (dict(heads=3), A.SHAPE), (dict(heads=1 << 22), A.SHAPE),
     (dict(M=0), A.SHAPE), (dict(tokens=0), A.SHAPE), (dict(tokens=21), A.SHAPE),
     (dict(top=0), A.SHAPE), (dict(top=81), A.SHAPE),
