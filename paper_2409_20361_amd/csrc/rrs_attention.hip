@@ -167,16 +167,18 @@ __device__ __forceinline__ bool find_piece(const AttentionArgs& a, const KvView&
 // Slots per wave and step.
 constexpr int tile_slots(int dim, int format, bool alone) {
   if (format == kCacheInt4) return 64;
-  const int n = dim == 256 || alone ? 16 : 32;
-  return format == kCacheFp8 ? 2 * n : n;
+  // Two blocks of 16 make one product of the values. 64 slots at head dim 128 need more registers than
+  // three waves per SIMD have (64 x 1..8192, 8 KV heads: 154 against 113 us).
+  if (format == kCacheFp8) return 32;
+  // 16 where 32 rows would not leave registers for a second wave, and for short sequences: more waves
+  // hide more of the chain of length, page and rows (179 x 64 heads of up to 5 slots 26 -> 21 us, 200 x 64
+  // of up to 64 within 3 %).
+  return dim == 256 || alone ? 16 : 32;
 }
 
 template <int D, int kFormat, int kTeam = kWaves>
 struct Shape {
   static constexpr bool kInt4 = kFormat == kCacheInt4, kFp8 = kFormat == kCacheFp8;
-  // Slots per wave and step. 16 where 32 rows would not leave registers for a second wave, and for
-  // short sequences: more waves hide more of the chain of length, page and rows (179 x 64 heads of up to
-  // 5 slots 26 -> 21 us, 200 x 64 of up to 64 within 3 %).
   static constexpr int kTile = tile_slots(D, kFormat, kTeam == 1);
   static constexpr int kBlocks = kTile / 16;         // of 16 slots
   static constexpr int kRow = kInt4 ? D / 2 : kFp8 ? D : 2 * D;  // bytes of a cache row
@@ -191,7 +193,8 @@ struct Shape {
   static constexpr int kSums = kRows * kLdO * 4;
   static constexpr int kLds = kValues > kSums ? kValues : kSums;  // per wave
   // Waves: limits the registers.
-  static constexpr int kPerSimd = D == 256 ? 2 : kTeam == 1 && !kInt4 ? 4 : 3;
+  static constexpr int kPerSimd =
+      D == 256 ? 2 : kTeam == 1 && kFormat == kCacheF16 ? 4 : 3;
 
   // Where 16-byte chunk c of slot t's value row lies in the wave's tile. The chunks of a row are
   // permuted by the slot, so that the rows that one transposed read touches lie in
@@ -940,6 +943,10 @@ Plan make_plan(const KvView& c, int heads, int max_length, bool with_weights, vo
   const int resident = 256 * (c.dim == 256 ? 2 : 3);
   const bool one_round = c.sequences * share <= resident;
   p.target = one_round ? resident : 4 * resident;
+  // FP8 with fewer than two pieces to a sequence in one round: pieces of very different sizes, so two
+  // rounds (64 x 1..8192, 8 KV heads: 115 -> 107 us; with more, 16 x 1..8192: 28 against 32 us).
+  if (c.format == kCacheFp8 && one_round && 2 * c.sequences * share > resident)
+    p.target = 2 * resident;
   p.steps = one_round ? 2 : 8;
   const long long steps = (max_length - 1) / p.step + 1;
   // Sequences of a few steps stay whole, which spares them the second launch (17 x 3 KV heads

@@ -40,6 +40,9 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kLift = 12;
 constexpr float kRoom = 15.0f;
 
+template <int N>
+using Int = std::integral_constant<int, N>;
+
 template <int D, int kFormat>
 struct Tile {
   static constexpr int kSlots = D == 256 ? 32 : 64;
@@ -47,11 +50,15 @@ struct Tile {
   static constexpr int kSteps = D / 16;   // mfma steps of a logit
   static constexpr int kOut = D / 32;     // blocks of output channels
   static constexpr int kBytes = kSlots * D * 2;
-  // Loads: 16 bytes per thread, kLanes threads to a row.
+  // Loads: kWidth bytes per thread, kLanes threads to a row. The rows that a wave loads at a time, at most
+  // 16, lie in one block of 16 slots: their page and address are the wave's.
   static constexpr int kRow = kFormat == kCacheInt4 ? D / 2 : kFormat == kCacheFp8 ? D : 2 * D;
-  static constexpr int kLanes = kRow / 16;
-  static constexpr int kRowsAtOnce = kThreads / kLanes;
-  static constexpr int kPasses = kSlots > kRowsAtOnce ? kSlots / kRowsAtOnce : 1;
+  static constexpr int kWidth = kRow < 64 ? 8 : 16;
+  static constexpr int kLanes = kRow / kWidth;
+  static constexpr int kWaveRows = 64 / kLanes;
+  static constexpr int kPasses = kSlots / (4 * kWaveRows);
+  // 8 float16 numbers each.
+  static constexpr int kChunks = kWidth / (kFormat == kCacheInt4 ? 4 : kFormat == kCacheFp8 ? 8 : 16);
   static constexpr int kPerSimd = D == 256 ? 1 : 2;
 
   // Byte of 16-byte chunk c of slot t. Keys are read 16 rows at a time, a chunk of each; values four
@@ -117,6 +124,15 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w) {
   return ((e + 0x04000400u) >> 15) & 0x00010001u;
 }
 
+// The T at byte `at` past an address that is the same for the wave, which stays in scalar registers.
+template <typename T>
+__device__ __forceinline__ T load_at(const void* base, uint32_t at) {
+  typedef const __attribute__((address_space(1))) uint8_t* Global;
+  Global p = (Global)base;
+  asm("" : "+s"(p), "+v"(at));
+  return *(const __attribute__((address_space(1))) T*)(p + at);
+}
+
 // Where a tile of rows belongs: new tokens [0, count) of sequence b, the first of which is row `first` of
 // Q and sees slots [0, seen).
 struct Where {
@@ -156,10 +172,9 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
   using T = Tile<D, kFormat>;
   __shared__ __attribute__((aligned(16))) uint8_t keys[2][T::kBytes];
   __shared__ __attribute__((aligned(16))) uint8_t values[2][T::kBytes];
-  // Of three tiles (the one in use, the next, and the last, whose are cleared): slots with values that
-  // are not finite, and those that the mask leaves.
-  __shared__ uint32_t bad_rows[3][2];
-  __shared__ uint32_t live_slots[kMask ? 3 : 1][2];
+  // Slots with values that are not finite, of the tiles that some rows see in part.
+  constexpr int kPartial = kRows / T::kSlots + 2;
+  __shared__ uint32_t bad_slots[kPartial * T::kBlocks];
 
   Where at;
   if (!find_tile(a, c, plan, &at)) return;
@@ -175,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
   const auto seen_by = [&](int r) {
     return min(max(at.seen + min(r, rows - 1) / plan.group, 0), at.length);
   };
-  const int wave_all = seen_by(row0 + 32 * wave), wave_any = seen_by(row0 + 32 * wave + 31);
+  const int wave_all = seen_by(row0 + 32 * wave);
   const int all = seen_by(row0), any = seen_by(row0 + kRows - 1);
   const bool wave_works = row0 + 32 * wave < rows;
 
@@ -202,211 +217,332 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
   v16f o[T::kOut] = {};
   float m = -INFINITY, sum = 0.0f;
 
-  // A thread's part of a tile: rows my_slot, my_slot + kRowsAtOnce, ...
-  const int my_slot = threadIdx.x / T::kLanes, my_lane = threadIdx.x % T::kLanes;
-  const bool loads = T::kRowsAtOnce <= T::kSlots || my_slot < T::kSlots;
-  v4u key[T::kPasses], val[T::kPasses];
-  uint16_t key_scale[T::kPasses], val_scale[T::kPasses];
-  uint8_t mask[T::kPasses];
-  int page[T::kPasses];
-  const auto load_pages = [&](int step) {
+  // A wave's part of a tile: in pass p rows kWaveRows (4 p + wave) ... of it, kLanes threads to each.
+  const int my_row_of = lane / T::kLanes, my_lane = lane % T::kLanes;
+  const uint32_t lane_at = my_row_of * T::kRow + my_lane * T::kWidth;
+  typedef uint32_t Piece __attribute__((ext_vector_type(T::kWidth / 4)));
+  struct Loaded {
+    Piece x[T::kPasses];
+    uint16_t scale[T::kPasses];
+  };
+  Loaded key, val;
+  const int last = (at.length - 1) & ~15;
+  // ahead: 32 for keys, whose tiles lie a block of 32 slots later.
+  const auto group_slot = [&](int step, int p, int ahead) {
+    return max(min(step * T::kSlots + ahead + T::kWaveRows * (4 * p + wave),
+                   last + 16 - T::kWaveRows), 0);
+  };
+  const int32_t* table = c.table + (size_t)at.b * c.max_pages;
+  const int page_slots = 1 << c.log_page;
+  const size_t page_rows = (size_t)c.heads << c.log_page, head_rows = (size_t)at.hk << c.log_page;
+  const auto load_pages = [&](int step, int ahead, int (&page)[T::kPasses]) {
+#pragma unroll
+    for (int p = 0; p < T::kPasses; ++p)
+      page[p] = load_at<int>(table + (group_slot(step, p, ahead) >> c.log_page), 0);
+  };
+  const auto load = [&](int step, int ahead, const int (&page)[T::kPasses], const uint8_t* pool,
+                        const uint16_t* scales, Loaded& x) {
 #pragma unroll
     for (int p = 0; p < T::kPasses; ++p) {
-      const int t = min(step * T::kSlots + my_slot + p * T::kRowsAtOnce, at.length - 1);
-      page[p] = c.page_of(at.b, t >> c.log_page);
+      const int t = group_slot(step, p, ahead) & (page_slots - 1);
+      const uint32_t id = __builtin_amdgcn_readfirstlane(page[p]);
+      const size_t row = (id < (uint32_t)c.pages ? id : 0) * page_rows + (head_rows + t);
+      x.x[p] = load_at<Piece>(pool + row * T::kRow, lane_at);
+      if constexpr (kFormat == kCacheFp8) x.scale[p] = load_at<uint16_t>(scales + row / kSlots8, 0);
+      if constexpr (kFormat == kCacheInt4)
+        x.scale[p] = load_at<uint16_t>(scales + row, 2 * my_row_of);
     }
   };
-  const auto load = [&](int step) {
-    if (!loads) return;
+  // The mask: a lane has its slot of the tile, and of the tile's rows that it brings.
+  uint8_t mask[kMask ? T::kPasses : 1], mask_of_tile = 0;
+  const uint8_t* mask_row = kMask ? a.mask + (size_t)at.b * c.capacity() : nullptr;
+  const auto load_mask = [&](int step) {
+    if constexpr (kMask)
 #pragma unroll
-    for (int p = 0; p < T::kPasses; ++p) {
-      const int t = min(step * T::kSlots + my_slot + p * T::kRowsAtOnce, at.length - 1);
-      const size_t row = c.page_row(page[p], at.hk) + (t & ((1 << c.log_page) - 1));
-      key[p] = *reinterpret_cast<const v4u*>(c.k + row * T::kRow + 16 * my_lane);
-      val[p] = *reinterpret_cast<const v4u*>(c.v + row * T::kRow + 16 * my_lane);
-      if constexpr (kFormat != kCacheF16) {
-        const size_t s = kFormat == kCacheFp8 ? row / kSlots8 : row;
-        key_scale[p] = c.k_scale[s];
-        val_scale[p] = c.v_scale[s];
-      }
-      if constexpr (kMask) mask[p] = a.mask[(size_t)at.b * c.capacity() + t];
+      for (int p = 0; p < T::kPasses; ++p)
+        mask[p] = load_at<uint8_t>(mask_row + group_slot(step, p, 0), my_row_of);
+  };
+  const auto load_tile_mask = [&](int step) {
+    if constexpr (kMask)
+      mask_of_tile =
+          load_at<uint8_t>(mask_row, min(step * T::kSlots + lane % T::kSlots, at.length - 1));
+  };
+  // Chunk i (of 8 numbers) of pass p as float16.
+  const auto convert = [&](const Loaded& from, int p, int i) -> v4u {
+    if constexpr (kFormat == kCacheInt4) {
+      _Float16 s = __builtin_bit_cast(_Float16, from.scale[p]);
+      s = s == (_Float16)9360.0f ? (_Float16)9352.0f : s;
+      return eight_int4(from.x[p][i], s);
+    } else if constexpr (kFormat == kCacheFp8) {
+      return dequant8_fp8(make_uint2(from.x[p][2 * i], from.x[p][2 * i + 1]),
+                          half_to_float(from.scale[p]));
+    } else {
+      return from.x[p];
     }
   };
-  const auto store = [&](int step, int buf, int flags) {
-    if (!loads) return;
-    const bool diagonal = (step + 1) * T::kSlots > all;
+  constexpr int kParts = T::kPasses * T::kChunks;  // of a thread
+  struct Rows {
+    v4u x[kParts];
+  };
+  const auto convert_all = [&](const Loaded& from, Rows& to) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) to.x[k] = convert(from, k / T::kChunks, k % T::kChunks);
+  };
+  const auto write_keys = [&](int k, v4u x, int buf) {
+    const int r = T::kWaveRows * (4 * (k / T::kChunks) + wave) + my_row_of;
+    *reinterpret_cast<v4u*>(keys[buf] + T::key_at(r, my_lane * T::kChunks + k % T::kChunks)) = x;
+  };
+  const auto write_values = [&](const Rows& v, int buf) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k) {
+      const int r = T::kWaveRows * (4 * (k / T::kChunks) + wave) + my_row_of;
+      *reinterpret_cast<v4u*>(values[buf] +
+                              T::value_at(r, my_lane * T::kChunks + k % T::kChunks)) = v.x[k];
+    }
+  };
+  const auto write_all_keys = [&](const Loaded& from, int buf) {
+#pragma unroll
+    for (int k = 0; k < kParts; ++k)
+      write_keys(k, convert(from, k / T::kChunks, k % T::kChunks), buf);
+  };
+  // Values that not every row of the tile sees: 0 where no row does, and 0 and a mark where a number is not
+  // finite, of tiles from first_partial on.
+  const int first_partial = all / T::kSlots;
+  const auto guarded = [&](int step) { return kMask || step >= first_partial; };
+  const auto guard = [&](int step, Rows& v) {
+    const bool marks = step >= first_partial;
 #pragma unroll
     for (int p = 0; p < T::kPasses; ++p) {
-      const int r = my_slot + p * T::kRowsAtOnce;
+      const int r = T::kWaveRows * (4 * p + wave) + my_row_of;
       const bool live = step * T::kSlots + r < at.length && (!kMask || mask[p] != 0);
-      if constexpr (kMask)
-        if (my_lane == 0 && live) atomicOr(&live_slots[flags][r / 32], 1u << (r % 32));
-      constexpr int kChunks = kFormat == kCacheInt4 ? 4 : kFormat == kCacheFp8 ? 2 : 1;
-      v4u k[kChunks], v[kChunks];
-      if constexpr (kFormat == kCacheInt4) {
-        _Float16 ks = __builtin_bit_cast(_Float16, key_scale[p]);
-        _Float16 vs = __builtin_bit_cast(_Float16, val_scale[p]);
-        ks = ks == (_Float16)9360.0f ? (_Float16)9352.0f : ks;
-        vs = vs == (_Float16)9360.0f ? (_Float16)9352.0f : vs;
+      uint32_t found = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          k[i] = eight_int4(key[p][i], ks);
-          v[i] = eight_int4(val[p][i], vs);
+      for (int i = 0; i < T::kChunks; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = v.x[p * T::kChunks + i][e];
+          const uint32_t bits = marks ? not_finite(w) : 0;
+          found |= bits;
+          v.x[p * T::kChunks + i][e] = live ? w & ~(bits * 0xFFFFu) : 0u;
         }
-      } else if constexpr (kFormat == kCacheFp8) {
-        const float ks = half_to_float(key_scale[p]), vs = half_to_float(val_scale[p]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          k[i] = dequant8_fp8(make_uint2(key[p][2 * i], key[p][2 * i + 1]), ks);
-          v[i] = dequant8_fp8(make_uint2(val[p][2 * i], val[p][2 * i + 1]), vs);
-        }
-      } else {
-        k[0] = key[p];
-        v[0] = val[p];
-      }
-      if (!live) {
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) v[i] = v4u{};
-      } else if (diagonal) {
-        uint32_t found = 0;
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t bits = not_finite(v[i][e]);
-            found |= bits;
-            v[i][e] &= ~(bits * 0xFFFFu);
-          }
-        if (found) atomicOr(&bad_rows[flags][r / 32], 1u << (r % 32));
-      }
-#pragma unroll
-      for (int i = 0; i < kChunks; ++i) {
-        *reinterpret_cast<v4u*>(keys[buf] + T::key_at(r, my_lane * kChunks + i)) = k[i];
-        *reinterpret_cast<v4u*>(values[buf] + T::value_at(r, my_lane * kChunks + i)) = v[i];
-      }
+      if (live && found)
+        atomicOr(&bad_slots[(step - first_partial) * T::kBlocks + r / 32], 1u << (r % 32));
     }
   };
-  const auto clear = [&](int flags) {
-    if (threadIdx.x < 2) {
-      bad_rows[flags][threadIdx.x] = 0;
-      if constexpr (kMask) live_slots[flags][threadIdx.x] = 0;
-    }
+  // Operands: keys of block u of a tile, channels 16 i ...; values of 16 slots 16 w ... of it, channels
+  // 32 j ...: lanes 4 r .. 4 r + 3 of 16 name row r, 16 channels of 4 slots; those of half h begin
+  // at 4 h and 8 + 4 h.
+  const auto key_of = [&](int buf, int u, int i) {
+    return *reinterpret_cast<const v8h*>(keys[buf] + T::key_at(32 * u + col, 2 * i + half));
+  };
+  const int vt = 4 * half + ((lane & 15) >> 2);
+  const int vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const auto value_of = [&](int buf, int u, int w, int j) {
+    const uint8_t* lo =
+        values[buf] + T::value_at(32 * u + 16 * w + vt, 4 * j + vc) + 8 * (lane & 1);
+    const uint8_t* hi =
+        values[buf] + T::value_at(32 * u + 16 * w + 8 + vt, 4 * j + vc) + 8 * (lane & 1);
+    const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)lo);
+    const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)hi);
+    return __builtin_bit_cast(v8h, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  const auto top_of = [](const v16f& s) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top = larger(top, s[r]);
+    return top;
   };
 
+  // The logits of a block of 32 slots are computed beside the exponentials of the block before it. Step n
+  // has its tile of values and the keys 32 slots later in buffer n & 1, step n + 1's in registers.
   if (s0 < s1) {
-    clear(0);
-    clear(1);
-    load_pages(s0);
-    load(s0);
-    if (s0 + 1 < s1) load_pages(s0 + 1);
+    int page[T::kPasses];
+    Rows v;
+    if (threadIdx.x < kPartial * T::kBlocks) bad_slots[threadIdx.x] = 0;
+    load_tile_mask(s0);
+    load_pages(s0 - 1, 32, page);
+    load(s0 - 1, 32, page, c.k, c.k_scale, key);
+    load_pages(s0, 0, page);
+    load(s0, 0, page, c.v, c.v_scale, val);
+    load_mask(s0);
     __syncthreads();
-    store(s0, 0, 0);
+    write_all_keys(key, 1);
+    load_pages(s0, 32, page);
+    load(s0, 32, page, c.k, c.k_scale, key);
+    convert_all(val, v);
+    if (guarded(s0)) guard(s0, v);
+    write_values(v, 0);
+    load_pages(s0 + 1, 0, page);
+    load(s0 + 1, 0, page, c.v, c.v_scale, val);
+    load_mask(s0 + 1);
+    write_all_keys(key, 0);
+    load_pages(s0 + 1, 32, page);
+    load(s0 + 1, 32, page, c.k, c.k_scale, key);
   }
   __syncthreads();
-  int flags = 0;
-  for (int step = s0; step < s1; ++step) {
-    const int buf = (step - s0) & 1, t0 = step * T::kSlots;
-    const int next_flags = flags == 2 ? 0 : flags + 1;
-    clear(next_flags == 2 ? 0 : next_flags + 1);
-    if (step + 1 < s1) {
-      load(step + 1);
-      if (step + 2 < s1) load_pages(step + 2);
+
+  float top = -INFINITY;  // of the lane's logits of the block that is next
+  // Block u of step `step`: its logits are in l, those of the block after it go to `next`.
+  const auto run = [&](int step, auto parity, auto block, v16f& l, v16f& next) {
+    constexpr int buf = decltype(parity)::value, u = decltype(block)::value;
+    constexpr bool kFirst = u == 0, kLast = u == T::kBlocks - 1;
+    const int t0 = step * T::kSlots + 32 * u;
+    int key_page[T::kPasses], val_page[T::kPasses];
+    if constexpr (kFirst) load_pages(step + 2, 32, key_page);
+    if constexpr (kLast) load_pages(step + 2, 0, val_page);
+    if (kMask || t0 + 32 > wave_all) {
+      uint32_t on = ~0u;
+      if constexpr (kMask) on = (uint32_t)(__ballot(mask_of_tile != 0) >> (32 * u));
+      const int n = seen - t0;  // slots of the block that the row sees
+      on &= n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
+      on >>= 4 * half;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) l[r] = on >> (8 * (r / 4) + r % 4) & 1 ? l[r] : -INFINITY;
+      top = top_of(l);
     }
-    if (wave_works && t0 < wave_any) {
-      v16f l[T::kBlocks];
+    if (__any(top * scale > m + kRoom)) {
+      top = row_max(top) * scale;
+      const float up = fmaxf(m, top - kLift);
+      const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
+      m = up;
+      sum *= shrink;
 #pragma unroll
-      for (int u = 0; u < T::kBlocks; ++u) {
-        l[u] = v16f{};
-#pragma unroll
-        for (int i = 0; i < T::kSteps; ++i)
-          l[u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-              *reinterpret_cast<const v8h*>(keys[buf] + T::key_at(32 * u + col, 2 * i + half)),
-              q[i], l[u], 0, 0, 0);
-      }
-      if (kMask || t0 + T::kSlots > wave_all) {
-#pragma unroll
-        for (int u = 0; u < T::kBlocks; ++u) {
-          uint32_t on = ~0u;
-          if constexpr (kMask) on = live_slots[flags][u];
-          const int n = seen - t0 - 32 * u;  // slots of the block that the row sees
-          on &= n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
-          on >>= 4 * half;
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            l[u][r] = on >> (8 * (r / 4) + r % 4) & 1 ? l[u][r] : -INFINITY;
-        }
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int u = 0; u < T::kBlocks; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = larger(top, l[u][r]);
-      if (__any(top * scale > m + kRoom)) {
-        top = row_max(top) * scale;
-        const float up = fmaxf(m, top - kLift);
-        const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
-        m = up;
-        sum *= shrink;
-#pragma unroll
-        for (int j = 0; j < T::kOut; ++j) o[j] *= shrink;
-      }
-      const float base = m == -INFINITY ? 0.0f : m;
-      v8h p[2 * T::kBlocks];
-#pragma unroll
-      for (int u = 0; u < T::kBlocks; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
-          sum += x;
-          p[2 * u + r / 8][r % 8] = (_Float16)x;
-        }
-      // Lanes 4 r .. 4 r + 3 of 16 name row r: 16 channels of 4 slots; those of half h begin at 4 h
-      // and 8 + 4 h.
-      const int vt = 4 * half + ((lane & 15) >> 2), vc = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-      for (int w = 0; w < 2 * T::kBlocks; ++w)
-#pragma unroll
-        for (int j = 0; j < T::kOut; ++j) {
-          const uint8_t* lo = values[buf] + T::value_at(16 * w + vt, 4 * j + vc) + 8 * (lane & 1);
-          const uint8_t* hi =
-              values[buf] + T::value_at(16 * w + 8 + vt, 4 * j + vc) + 8 * (lane & 1);
-          const v4s x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)lo);
-          const v4s y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)hi);
-          o[j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-              __builtin_bit_cast(v8h, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7)), p[w],
-              o[j], 0, 0, 0);
-        }
-      // Values that are not finite, for the rows that see them.
-      if (t0 + T::kSlots > all) {
-        for (int u = 0; u < T::kBlocks; ++u)
-          for (uint32_t left = bad_rows[flags][u]; left; left &= left - 1) {
-            const int t = t0 + 32 * u + __builtin_ctz(left);
-            const size_t row = c.row_of(at.b, at.hk, t);
-            if (t >= seen) continue;
-#pragma unroll 1
-            for (int d = 0; d < D; ++d) {
-              float v;
-              if constexpr (kFormat == kCacheInt4)
-                v = half_to_float(c.v_scale[row]);
-              else if constexpr (kFormat == kCacheFp8)
-                v = (c.v[row * D + d] & 127) == 127 ? NAN : 0.0f;
-              else
-                v = half_to_float(reinterpret_cast<const uint16_t*>(c.v)[row * D + d]);
-              if (kFormat == kCacheInt4) v = v - v == 0.0f ? 0.0f : NAN;
-              if (v - v == 0.0f || (d >> 2 & 1) != half) continue;
-#pragma unroll
-              for (int j = 0; j < T::kOut; ++j)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                  if (32 * j + 8 * (r / 4) + 4 * half + r % 4 == d) o[j][r] += v;
-            }
-          }
-      }
+      for (int j = 0; j < T::kOut; ++j) o[j] *= shrink;
     }
-    if (step + 1 < s1) store(step + 1, buf ^ 1, next_flags);
+    const float base = m == -INFINITY ? 0.0f : m;
+    // The order below is the one that is issued: operands are read kAhead products ahead, and the vector
+    // instructions stand between the products, which take 32 cycles each.
+    constexpr int kAhead = 3, kProducts = 2 * T::kOut, kEach = 16 / T::kSteps;
+    v8h p[2], ks[kAhead], vs[kAhead];
+    Rows v;
+    float x[16];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ks[i] = key_of(buf, u, i);
+    next = v16f{};
+    const auto add = [&](int r) {  // of a pair
+      sum += x[r];
+      sum += x[r + 1];
+      p[r / 8][r % 8] = (_Float16)x[r];
+      p[r / 8][r % 8 + 1] = (_Float16)x[r + 1];
+    };
+#pragma unroll
+    for (int i = 0; i < T::kSteps; ++i) {
+      next = __builtin_amdgcn_mfma_f32_32x32x16_f16(ks[i % kAhead], q[i], next, 0, 0, 0);
+      if (i + kAhead < T::kSteps)
+        ks[i % kAhead] = key_of(buf, u, i + kAhead);
+      else if (i + kAhead - T::kSteps < kProducts)
+        vs[i + kAhead - T::kSteps] = value_of(buf, u, (i + kAhead - T::kSteps) / T::kOut,
+                                              (i + kAhead - T::kSteps) % T::kOut);
+#pragma unroll
+      for (int r = kEach * i; r < kEach * (i + 1); ++r) {
+        x[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(l[r], scale, -base));
+        if (r % 2 == 1 && r >= 3) add(r - 3);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    add(14);
+    top = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < kProducts; ++n) {
+      o[n % T::kOut] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vs[n % kAhead], p[n / T::kOut],
+                                                             o[n % T::kOut], 0, 0, 0);
+      if (n + kAhead < kProducts)
+        vs[n % kAhead] = value_of(buf, u, (n + kAhead) / T::kOut, (n + kAhead) % T::kOut);
+      if (n % (kProducts / kParts) == 0) {
+        const int k = n / (kProducts / kParts);
+        if constexpr (kFirst) write_keys(k, convert(key, k / T::kChunks, k % T::kChunks), buf ^ 1);
+        if constexpr (kLast) v.x[k] = convert(val, k / T::kChunks, k % T::kChunks);
+      }
+      if (n >= kProducts / 2) {  // the new logits are there
+#pragma unroll
+        for (int r = 32 / kProducts * (n - kProducts / 2);
+             r < 32 / kProducts * (n + 1 - kProducts / 2); ++r)
+          top = larger(top, next[r]);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (kFirst) load(step + 2, 32, key_page, c.k, c.k_scale, key);
+    if constexpr (kLast) {
+      if (step + 1 < s1 && guarded(step + 1)) guard(step + 1, v);
+      write_values(v, buf ^ 1);
+      load(step + 2, 0, val_page, c.v, c.v_scale, val);
+      load_mask(step + 2);
+      load_tile_mask(step + 1);
+      __syncthreads();
+    }
+  };
+  if (wave_works) {
+    v16f l[2];
+    if (s0 < s1) {
+      l[0] = v16f{};
+#pragma unroll
+      for (int i = 0; i < T::kSteps; ++i)
+        l[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(key_of(1, T::kBlocks - 1, i), q[i], l[0], 0,
+                                                      0, 0);
+      top = top_of(l[0]);
+    }
     __syncthreads();
-    flags = next_flags;
+    for (int step = s0; step < s1; step += 2) {
+      if constexpr (T::kBlocks == 2) {
+        run(step, Int<0>(), Int<0>(), l[0], l[1]);
+        run(step, Int<0>(), Int<1>(), l[1], l[0]);
+        if (step + 1 == s1) break;
+        run(step + 1, Int<1>(), Int<0>(), l[0], l[1]);
+        run(step + 1, Int<1>(), Int<1>(), l[1], l[0]);
+      } else {
+        run(step, Int<0>(), Int<0>(), l[0], l[1]);
+        if (step + 1 == s1) break;
+        run(step + 1, Int<1>(), Int<0>(), l[1], l[0]);
+      }
+    }
+  } else {  // loads for the others
+    __syncthreads();
+    for (int step = s0; step < s1; ++step) {
+      const int buf = (step - s0) & 1;
+      int page[T::kPasses];
+      Rows x;
+      write_all_keys(key, buf ^ 1);
+      load_pages(step + 2, 32, page);
+      load(step + 2, 32, page, c.k, c.k_scale, key);
+      convert_all(val, x);
+      if (step + 1 < s1 && guarded(step + 1)) guard(step + 1, x);
+      write_values(x, buf ^ 1);
+      load_pages(step + 2, 0, page);
+      load(step + 2, 0, page, c.v, c.v_scale, val);
+      load_mask(step + 2);
+      __syncthreads();
+    }
   }
+
+  // Values that are not finite, for the rows that see them.
+  for (int i = 0; s0 < s1 && i < kPartial * T::kBlocks; ++i)
+    for (uint32_t left = bad_slots[i]; left; left &= left - 1) {
+      const int t = first_partial * T::kSlots + 32 * i + __builtin_ctz(left);
+      if (t >= s1 * T::kSlots) break;
+      const size_t row = c.row_of(at.b, at.hk, t);
+      float all_of_row = 0.0f;  // INT4: a scale that is not finite
+      if constexpr (kFormat == kCacheInt4) all_of_row = half_to_float(c.v_scale[row]) * 0.0f;
+#pragma unroll
+      for (int j = 0; j < T::kOut; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const int d = 32 * j + 2 * r + 4 * half;
+          uint2 w = make_uint2(0, 0);
+          if constexpr (kFormat == kCacheFp8)
+            w.x = *reinterpret_cast<const uint32_t*>(c.v + row * D + d);
+          else if constexpr (kFormat == kCacheF16)
+            w = *reinterpret_cast<const uint2*>(c.v + (row * D + d) * 2);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float x = all_of_row;
+            if constexpr (kFormat == kCacheFp8)
+              x = (w.x >> (8 * e) & 127) == 127 ? NAN : 0.0f;
+            else if constexpr (kFormat == kCacheF16)
+              x = half_to_float((e < 2 ? w.x : w.y) >> (16 * (e & 1)) & 0xFFFFu);
+            if (t < seen && !(fabsf(x) < INFINITY)) o[j][r + e] += x;
+          }
+        }
+    }
 
   {
     const uint32_t u = __builtin_bit_cast(uint32_t, sum);
@@ -512,9 +648,6 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   }
   return p;
 }
-
-template <int N>
-using Int = std::integral_constant<int, N>;
 
 template <int D>
 hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
