@@ -9,7 +9,8 @@
 // one workgroup between them.
 //
 // Copies: a page of a head is one run of memory, so a page is two runs of bytes (and two of scales),
-// cut into pieces of 16 KB. Bound by HBM.
+// cut into pieces of 16 KB. Bound by HBM: 2019 pages of 2 x 128 KiB, with their plan, 197 us (5.36 TB/s
+// read and written, as a plain copy of that size). Past the caches: 221 us with ordinary loads and stores.
 #include <algorithm>
 
 #include "rrs_device.h"
@@ -22,8 +23,10 @@ constexpr int kThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / 64;
 
-// Tables up to so many entries, and pools up to so many pages, are planned in one launch.
-constexpr int kSmallEntries = 32768;
+// Tables up to so many rows and entries, and pools up to so many pages, are planned in one launch: forks of
+// 16640 entries with their copies 25.3 us, in four launches 28.7; of 32000 28.1 and 26.2, of 58000 50 and 31.
+constexpr int kSmallRows = 2048;
+constexpr int kSmallEntries = 24576;
 constexpr int kSmallPages = 65536;
 constexpr int kMostPages = 1 << 20;  // bits in LDS
 constexpr int kFar = 1 << 29;        // running sums stop here
@@ -65,6 +68,7 @@ struct RowPlan {
 };
 
 struct ForkPlan {
+  uint32_t* used;  // bits of pages that rows keep; where a launch of its own marks them
   PageInfo info;
   RowPlan* rows;
   int* fresh;  // pages handed out, by rank
@@ -109,63 +113,101 @@ __device__ __forceinline__ Need needs(const ForkArgs& a, const PageInfo& info, c
   return n;
 }
 
-// An entry of the new table.
-__device__ __forceinline__ int fork_entry(const ForkArgs& a, const RowPlan& r, const int* fresh,
-                                          int i) {
+// Where an entry of the new table comes from; nullptr: there is none (-1).
+__device__ __forceinline__ const int32_t* fork_entry(const ForkArgs& a, const RowPlan& r,
+                                                     const int* fresh, int i) {
   const int copy = (uint32_t)r.begin >> 31, begin = r.begin & 0x7FFFFFFF;
-  if (i < r.have - copy) return a.table[(size_t)r.parent * a.max_pages + i];
-  if (i < r.total) return fresh[begin + i - (r.have - copy)];
-  return -1;
+  if (i < r.have - copy) return a.table + (size_t)r.parent * a.max_pages + i;
+  return i < r.total ? fresh + begin + i - (r.have - copy) : nullptr;
 }
 
-// The plan, by one workgroup. kMarks: it marks the pages itself and writes the table, too;
-// else `info` holds the marks of another launch. kWords: of 32 pages.
+// Entries (row, column) of a table, kPlanThreads apart: at(row, column) is where an entry's number lies
+// (nullptr: nowhere), use(row, column, number, there) what becomes of it. kAhead loads of a thread are under
+// way at a time: one after the other they took 1 us each.
+template <typename At, typename Use>
+__device__ __forceinline__ void for_entries(int rows, int columns, At at, Use use) {
+  constexpr int kAhead = 8;
+  const int down = kPlanThreads / columns, right = kPlanThreads % columns;
+  int b = threadIdx.x / columns, i = threadIdx.x % columns;
+  while (b < rows) {
+    int bs[kAhead], is[kAhead], x[kAhead];
+    const int32_t* from[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      bs[k] = b;
+      is[k] = i;
+      from[k] = b < rows ? at(b, i) : nullptr;
+      b += down;
+      i += right;
+      if (i >= columns) {
+        i -= columns;
+        ++b;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) x[k] = from[k] ? *from[k] : -1;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (bs[k] < rows) use(bs[k], is[k], x[k], from[k] != nullptr);
+  }
+}
+
+// The plan, by one workgroup. kMarks: it marks the pages itself and writes the table, too, with the
+// rows in LDS; else `used` and `info` hold the marks of another launch. kWords: of 32 pages.
 template <int kWords, bool kMarks>
 __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkArgs a, ForkPlan plan) {
   __shared__ uint32_t used[kWords];
   __shared__ uint32_t wanted[kMarks ? kWords : 1];  // pages that a row is about to write into
+  __shared__ RowPlan in_lds[kMarks ? kSmallRows : 1];
   __shared__ int scratch[kPlanWaves];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  constexpr int kOwn = kSmallRows / kPlanThreads;  // rows of a thread
+  const int t = threadIdx.x;
   const int words = (a.pages + 31) / 32;
+  Row own[kOwn];
   if constexpr (kMarks) {
     for (int w = t; w < words; w += kPlanThreads) used[w] = wanted[w] = 0;
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int b = k * kPlanThreads + t;
+      own[k] = b < a.sequences ? fork_row(a, b) : Row{-1, 0, 0, 0, 0, -1};
+      if (b < a.sequences) in_lds[b] = RowPlan{own[k].parent, own[k].have, 0, 0};
+    }
     __syncthreads();
-    for (int b = t; b < a.sequences; b += kPlanThreads) {
-      const Row r = fork_row(a, b);
-      if (r.last < 0) continue;
-      atomicOr(&wanted[r.last / 32], 1u << (r.last % 32));
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int page = own[k].last;
+      if (page < 0) continue;
+      atomicOr(&wanted[page / 32], 1u << (page % 32));
       // Atomics, as what follows on them: they meet in the L2.
-      atomicExch(plan.info.refs + r.last, 0);
-      atomicExch(plan.info.writers + r.last, 0);
-      atomicExch(plan.info.first + r.last, 0);
+      atomicExch(plan.info.refs + page, 0);
+      atomicExch(plan.info.writers + page, 0);
+      atomicExch(plan.info.first + page, 0);
     }
-    __threadfence();
+    __threadfence_block();
     __syncthreads();
-    for (int b = wave; b < a.sequences; b += kPlanWaves) {
-      const Row r = fork_row(a, b);
-      for (int i = lane; i < r.have; i += 64) {
-        const int page = a.table[(size_t)r.parent * a.max_pages + i];
-        if ((uint32_t)page >= (uint32_t)a.pages) continue;
-        atomicOr(&used[page / 32], 1u << (page % 32));
-        if (wanted[page / 32] >> (page % 32) & 1) atomicAdd(plan.info.refs + page, 1);
+    for_entries(
+        a.sequences, a.max_pages,
+        [&](int b, int i) -> const int32_t* {
+          const RowPlan r = in_lds[b];
+          return i < r.have ? a.table + (size_t)r.parent * a.max_pages + i : nullptr;
+        },
+        [&](int, int, int page, bool there) {
+          if (!there || (uint32_t)page >= (uint32_t)a.pages) return;
+          atomicOr(&used[page / 32], 1u << (page % 32));
+          if (wanted[page / 32] >> (page % 32) & 1) atomicAdd(plan.info.refs + page, 1);
+        });
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+      if (own[k].last >= 0) {
+        atomicAdd(plan.info.writers + own[k].last, 1);
+        atomicMax(plan.info.first + own[k].last, a.sequences - (k * kPlanThreads + t));
       }
-      if (lane == 0 && r.last >= 0) {
-        atomicAdd(plan.info.writers + r.last, 1);
-        atomicMax(plan.info.first + r.last, a.sequences - b);
-      }
-    }
-    __threadfence();
+    __threadfence_block();
   } else {
-    for (int w = wave; w < (words + 1) / 2; w += kPlanWaves) {
-      const int page = 64 * w + lane;
-      const uint64_t bits = __ballot(page < a.pages && plan.info.refs[min(page, a.pages - 1)] > 0);
-      if (lane == 0) {
-        used[2 * w] = (uint32_t)bits;
-        if (2 * w + 1 < words) used[2 * w + 1] = (uint32_t)(bits >> 32);
-      }
-    }
+    for (int w = t; w < words; w += kPlanThreads) used[w] = plan.used[w];
   }
   __syncthreads();
+  const auto row_of = [&](int b) { return kMarks ? own[b / kPlanThreads] : fork_row(a, b); };
 
   // Free pages of the thread's words, and of all.
   const int per_thread = (words + kPlanThreads - 1) / kPlanThreads;
@@ -179,29 +221,30 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkArgs a, For
   const int free_upto = block_prefix(mine, scratch, &free_pages);
 
   // Do all rows get what they need?
+  Need own_need[kOwn];
   int sum = 0;
-  for (int b = t; b < a.sequences; b += kPlanThreads)
-    sum = min(sum + needs(a, plan.info, fork_row(a, b), b).some, kMostPages + 1);
+  if constexpr (kMarks) {
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      own_need[k] = needs(a, plan.info, own[k], k * kPlanThreads + t);
+      sum = min(sum + own_need[k].some, kMostPages + 1);
+    }
+  } else {
+    for (int b = t; b < a.sequences; b += kPlanThreads)
+      sum = min(sum + needs(a, plan.info, row_of(b), b).some, kMostPages + 1);
+  }
   int all;
   block_prefix(sum, scratch, &all);
   const bool tight = all > free_pages;
 
   int carry = 0, copies = 0, taken = 0;
-  for (int b0 = 0; b0 < a.sequences; b0 += kPlanThreads) {
-    const int b = b0 + t;
-    Row r{-1, 0, 0, 0, 0, -1};
-    Need n{};
-    if (b < a.sequences) {
-      r = fork_row(a, b);
-      n = needs(a, plan.info, r, b);
-    }
+  const auto chunk = [&](int b, const Row& r, const Need& n) {
     const int need = tight ? n.tight : n.some;
-    int chunk, more;
-    const int upto = min(carry, kFar) + block_prefix(need, scratch, &chunk);
+    int here, more, last_taken;
+    const int upto = carry + block_prefix(need, scratch, &here);
     const bool served = need == 0 || upto <= free_pages;
     const bool copy = served && (tight ? n.copy_tight : n.copy);
     const int rank = copies + block_prefix(copy, scratch, &more) - 1;
-    int last_taken;
     block_prefix(served ? need : 0, scratch, &last_taken);
     if (b < a.sequences) {
       RowPlan out{r.parent, r.have, served ? r.total : r.have, served ? upto - need : 0};
@@ -210,13 +253,29 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkArgs a, For
         a.src[rank] = r.last;
         a.dst[rank] = upto - need;  // a rank, for now
       }
-      plan.rows[b] = out;
+      (kMarks ? in_lds : plan.rows)[b] = out;
       a.lengths_out[b] = r.kept;
       a.room_out[b] = served ? r.want : r.kept;
     }
-    carry = min(min(carry, kFar) + chunk, kFar);
+    carry = min(carry + here, kFar);
     copies += more;
     taken += last_taken;
+  };
+  if constexpr (kMarks) {
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k)
+      if (k * kPlanThreads < a.sequences) chunk(k * kPlanThreads + t, own[k], own_need[k]);
+  } else {
+    for (int b0 = 0; b0 < a.sequences; b0 += kPlanThreads) {
+      const int b = b0 + t;
+      Row r{-1, 0, 0, 0, 0, -1};
+      Need n{};
+      if (b < a.sequences) {
+        r = fork_row(a, b);
+        n = needs(a, plan.info, r, b);
+      }
+      chunk(b, r, n);
+    }
   }
   if (t == 0) {
     a.count[0] = copies;
@@ -238,11 +297,10 @@ __global__ void __launch_bounds__(kPlanThreads) fork_plan_kernel(ForkArgs a, For
     }
   }
   if constexpr (kMarks)
-    for (int b = wave; b < a.sequences; b += kPlanWaves) {
-      const RowPlan r = plan.rows[b];
-      for (int i = lane; i < a.max_pages; i += 64)
-        a.table_out[(size_t)b * a.max_pages + i] = fork_entry(a, r, plan.fresh, i);
-    }
+    for_entries(
+        a.sequences, a.max_pages,
+        [&](int b, int i) { return fork_entry(a, in_lds[b], plan.fresh, i); },
+        [&](int b, int i, int page, bool) { a.table_out[(size_t)b * a.max_pages + i] = page; });
 }
 
 // Units of work on the whole card: `kColumns` entries of a row, a wave each.
@@ -263,13 +321,16 @@ __global__ void __launch_bounds__(kThreads) zero_kernel(int* p, int n) {
   for (int i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) p[i] = 0;
 }
 
-__global__ void __launch_bounds__(kThreads) fork_mark_kernel(ForkArgs a, PageInfo info) {
+__global__ void __launch_bounds__(kThreads) fork_mark_kernel(ForkArgs a, ForkPlan plan) {
+  const PageInfo info = plan.info;
   const int lane = threadIdx.x & 63;
   for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
     const Row r = fork_row(a, b);
     for (int i = i0 + lane; i < min(i1, r.have); i += 64) {
       const int page = a.table[(size_t)r.parent * a.max_pages + i];
-      if ((uint32_t)page < (uint32_t)a.pages) atomicAdd(info.refs + page, 1);
+      if ((uint32_t)page >= (uint32_t)a.pages) continue;
+      atomicOr(plan.used + page / 32, 1u << (page % 32));
+      atomicAdd(info.refs + page, 1);
     }
     if (i0 == 0 && lane == 0 && r.last >= 0) {
       atomicAdd(info.writers + r.last, 1);
@@ -282,8 +343,11 @@ __global__ void __launch_bounds__(kThreads) fork_write_kernel(ForkArgs a, ForkPl
   const int lane = threadIdx.x & 63;
   for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
     const RowPlan r = plan.rows[b];
-    for (int i = i0 + lane; i < i1; i += 64)
-      a.table_out[(size_t)b * a.max_pages + i] = fork_entry(a, r, plan.fresh, i);
+#pragma unroll 4
+    for (int i = i0 + lane; i < i1; i += 64) {
+      const int32_t* from = fork_entry(a, r, plan.fresh, i);
+      a.table_out[(size_t)b * a.max_pages + i] = from ? *from : -1;
+    }
   });
 }
 
@@ -304,33 +368,30 @@ __device__ __forceinline__ int compact_entry(const CompactArgs& a, const int* to
   return page >= used && page < a.pages ? to[page] : page;
 }
 
-// flags: marks of another launch (else the kernel's own; it then writes the table, too).
+// marks: bits of another launch (else the kernel's own; it then writes the table, too).
 template <int kWords, bool kMarks>
 __global__ void __launch_bounds__(kPlanThreads)
-    compact_plan_kernel(CompactArgs a, const int* flags, int* to) {
+    compact_plan_kernel(CompactArgs a, const uint32_t* marks, int* to) {
   __shared__ uint32_t used[kWords];
+  __shared__ int have_of[kMarks ? kSmallRows : 1];
   __shared__ int scratch[kPlanWaves];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int t = threadIdx.x;
   const int words = (a.pages + 31) / 32;
+  const auto entry_of = [&](int b, int i) -> const int32_t* {
+    return i < have_of[b] ? a.table + (size_t)b * a.max_pages + i : nullptr;
+  };
   if constexpr (kMarks) {
     for (int w = t; w < words; w += kPlanThreads) used[w] = 0;
+    for (int b = t; b < a.sequences; b += kPlanThreads) have_of[b] = row_pages(a, b);
     __syncthreads();
-    for (int b = wave; b < a.sequences; b += kPlanWaves) {
-      const int have = row_pages(a, b);
-      for (int i = lane; i < have; i += 64) {
-        const int page = a.table[(size_t)b * a.max_pages + i];
-        if ((uint32_t)page < (uint32_t)a.pages) atomicOr(&used[page / 32], 1u << (page % 32));
-      }
-    }
+    for_entries(
+        a.sequences, a.max_pages, entry_of,
+        [&](int, int, int page, bool there) {
+          if (there && (uint32_t)page < (uint32_t)a.pages)
+            atomicOr(&used[page / 32], 1u << (page % 32));
+        });
   } else {
-    for (int w = wave; w < (words + 1) / 2; w += kPlanWaves) {
-      const int page = 64 * w + lane;
-      const uint64_t bits = __ballot(page < a.pages && flags[min(page, a.pages - 1)] > 0);
-      if (lane == 0) {
-        used[2 * w] = (uint32_t)bits;
-        if (2 * w + 1 < words) used[2 * w + 1] = (uint32_t)(bits >> 32);
-      }
-    }
+    for (int w = t; w < words; w += kPlanThreads) used[w] = marks[w];
   }
   __syncthreads();
   const int per_thread = (words + kPlanThreads - 1) / kPlanThreads;
@@ -374,20 +435,18 @@ __global__ void __launch_bounds__(kPlanThreads)
   if constexpr (kMarks) {
     __threadfence_block();
     __syncthreads();
-    for (int b = wave; b < a.sequences; b += kPlanWaves) {
-      const int have = row_pages(a, b);
-      for (int i = lane; i < a.max_pages; i += 64)
-        a.table_out[(size_t)b * a.max_pages + i] = compact_entry(a, to, U, b, i, have);
-    }
+    for_entries(a.sequences, a.max_pages, entry_of, [&](int b, int i, int page, bool) {
+      a.table_out[(size_t)b * a.max_pages + i] = page >= U && page < a.pages ? to[page] : page;
+    });
   }
 }
 
-__global__ void __launch_bounds__(kThreads) compact_mark_kernel(CompactArgs a, int* flags) {
+__global__ void __launch_bounds__(kThreads) compact_mark_kernel(CompactArgs a, uint32_t* marks) {
   const int lane = threadIdx.x & 63;
   for_rows(a.sequences, a.max_pages, [&](int b, int i0, int i1) {
     for (int i = i0 + lane; i < min(i1, row_pages(a, b)); i += 64) {
       const int page = a.table[(size_t)b * a.max_pages + i];
-      if ((uint32_t)page < (uint32_t)a.pages) flags[page] = 1;
+      if ((uint32_t)page < (uint32_t)a.pages) atomicOr(marks + page / 32, 1u << (page % 32));
     }
   });
 }
@@ -433,10 +492,12 @@ __global__ void __launch_bounds__(kThreads)
     v4u x[kAtOnce];
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      if ((size_t)(i * kThreads + threadIdx.x) * 16 < size) x[i] = in[i * kThreads + threadIdx.x];
+      if ((size_t)(i * kThreads + threadIdx.x) * 16 < size)
+        x[i] = __builtin_nontemporal_load(in + i * kThreads + threadIdx.x);
 #pragma unroll
     for (int i = 0; i < kAtOnce; ++i)
-      if ((size_t)(i * kThreads + threadIdx.x) * 16 < size) out[i * kThreads + threadIdx.x] = x[i];
+      if ((size_t)(i * kThreads + threadIdx.x) * 16 < size)
+        __builtin_nontemporal_store(x[i], out + i * kThreads + threadIdx.x);
   }
 }
 
@@ -448,50 +509,64 @@ unsigned row_grid(int sequences, int columns) {
 }
 
 bool small(int sequences, int max_pages, int pages) {
-  return (long long)sequences * max_pages <= kSmallEntries && pages <= kSmallPages;
+  return sequences <= kSmallRows && (long long)sequences * max_pages <= kSmallEntries &&
+         pages <= kSmallPages;
 }
+
+// Clears n ints.
+void zero(int* p, int n, hipStream_t stream) {
+  zero_kernel<<<std::min((n - 1) / kThreads + 1, 1024), kThreads, 0, stream>>>(p, n);
+}
+
+int words_of(int pages) { return (pages + 31) / 32; }
 
 }  // namespace
 
 int most_pages() { return kMostPages; }
 
+// Bits, three numbers per page, the pages handed out; the rows.
 size_t fork_workspace_bytes(int sequences, int pages) {
-  return align256((size_t)pages * 16) + align256((size_t)sequences * sizeof(RowPlan));
+  return align256(((size_t)words_of(pages) + 4 * (size_t)pages) * 4) +
+         align256((size_t)sequences * sizeof(RowPlan));
 }
 
 hipError_t launch_kv_fork(const ForkArgs& a, void* workspace, hipStream_t stream) {
-  int* ws = static_cast<int*>(workspace);
-  const size_t n = (size_t)a.pages;
-  ForkPlan plan{{ws, ws + n, ws + 2 * n},
-                reinterpret_cast<RowPlan*>(static_cast<uint8_t*>(workspace) + align256(n * 16)),
-                ws + 3 * n};
+  int* bits = static_cast<int*>(workspace);
+  const size_t n = (size_t)a.pages, words = (size_t)words_of(a.pages);
+  int* info = bits + words;
+  ForkPlan plan{reinterpret_cast<uint32_t*>(bits),
+                {info, info + n, info + 2 * n},
+                reinterpret_cast<RowPlan*>(static_cast<uint8_t*>(workspace) +
+                                           align256((words + 4 * n) * 4)),
+                info + 3 * n};
   if (small(a.sequences, a.max_pages, a.pages)) {
     fork_plan_kernel<kSmallPages / 32, true><<<1, kPlanThreads, 0, stream>>>(a, plan);
     return hipGetLastError();
   }
   const unsigned grid = row_grid(a.sequences, a.max_pages);
-  zero_kernel<<<std::min((3 * a.pages - 1) / kThreads + 1, 1024), kThreads, 0, stream>>>(
-      ws, 3 * a.pages);
-  fork_mark_kernel<<<grid, kThreads, 0, stream>>>(a, plan.info);
+  zero(bits, (int)(words + 3 * n), stream);
+  fork_mark_kernel<<<grid, kThreads, 0, stream>>>(a, plan);
   fork_plan_kernel<kMostPages / 32, false><<<1, kPlanThreads, 0, stream>>>(a, plan);
   fork_write_kernel<<<grid, kThreads, 0, stream>>>(a, plan);
   return hipGetLastError();
 }
 
-size_t compact_workspace_bytes(int pages) { return align256((size_t)pages * 8); }
+// Bits, and the new numbers.
+size_t compact_workspace_bytes(int pages) {
+  return align256(((size_t)words_of(pages) + (size_t)pages) * 4);
+}
 
 hipError_t launch_kv_compact(const CompactArgs& a, void* workspace, hipStream_t stream) {
-  int* flags = static_cast<int*>(workspace);
-  int* to = flags + a.pages;
+  uint32_t* marks = static_cast<uint32_t*>(workspace);
+  int* to = static_cast<int*>(workspace) + words_of(a.pages);
   if (small(a.sequences, a.max_pages, a.pages)) {
-    compact_plan_kernel<kSmallPages / 32, true><<<1, kPlanThreads, 0, stream>>>(a, flags, to);
+    compact_plan_kernel<kSmallPages / 32, true><<<1, kPlanThreads, 0, stream>>>(a, marks, to);
     return hipGetLastError();
   }
   const unsigned grid = row_grid(a.sequences, a.max_pages);
-  zero_kernel<<<std::min((a.pages - 1) / kThreads + 1, 1024), kThreads, 0, stream>>>(flags,
-                                                                                    a.pages);
-  compact_mark_kernel<<<grid, kThreads, 0, stream>>>(a, flags);
-  compact_plan_kernel<kMostPages / 32, false><<<1, kPlanThreads, 0, stream>>>(a, flags, to);
+  zero(static_cast<int*>(workspace), words_of(a.pages), stream);
+  compact_mark_kernel<<<grid, kThreads, 0, stream>>>(a, marks);
+  compact_plan_kernel<kMostPages / 32, false><<<1, kPlanThreads, 0, stream>>>(a, marks, to);
   compact_write_kernel<<<grid, kThreads, 0, stream>>>(a, to);
   return hipGetLastError();
 }
@@ -505,7 +580,8 @@ hipError_t launch_kv_copy_pages(const KvView& c, const int32_t* src, const int32
   const int scale_rows = (int)(c.format == kCacheFp8 ? rows / kSlots8 : rows);
   const int per_pair = 2 * pieces + (scales ? 1 : 0);
   const long long units = (long long)n * per_pair;
-  const unsigned grid = (unsigned)std::min<long long>(units, 256 * 8);
+  // Four rounds of workgroups, which balance each other (one: 217 us against 197).
+  const unsigned grid = (unsigned)std::min<long long>(units, 256 * 32);
   copy_pages_kernel<<<grid, kThreads, 0, stream>>>(c, src, dst, count, n, bytes, pieces, per_pair,
                                                    scale_rows);
   return hipGetLastError();

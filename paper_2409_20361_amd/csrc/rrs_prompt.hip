@@ -59,7 +59,7 @@ struct Tile {
   static constexpr int kPasses = kSlots / (4 * kWaveRows);
   // 8 float16 numbers each.
   static constexpr int kChunks = kWidth / (kFormat == kCacheInt4 ? 4 : kFormat == kCacheFp8 ? 8 : 16);
-  static constexpr int kPerSimd = D == 256 ? 1 : 2;
+  static constexpr int kPerSimd = D == 256 ? 1 : D == 64 ? 3 : 2;
 
   // Byte of 16-byte chunk c of slot t. Keys are read 16 rows at a time, a chunk of each; values four
   // rows, four neighbouring chunks of each: both then touch all banks.
@@ -69,7 +69,7 @@ struct Tile {
     return t * (2 * D) + ((c ^ x) << 4);
   }
   static __device__ __forceinline__ int value_at(int t, int c) {
-    const int x = (t / kPerLine & (D / 8 < 16 ? D / 32 - 1 : 3)) << 2;
+    const int y = t / kPerLine & (D / 8 < 16 ? D / 32 - 1 : 3), x = (y << 2) | (y & 1);
     return t * (2 * D) + ((c ^ x) << 4);
   }
 };
@@ -635,7 +635,7 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   p.tiles = (int)(((long long)max_tokens * p.group - 1) / kRows + 1);
   // Pieces, of four steps at least, where the tiles alone do not fill the card.
   const int slots = c.dim == 256 ? 32 : 64;
-  const long long resident = c.dim == 256 ? 256 : 512;
+  const long long resident = c.dim == 256 ? 256 : c.dim == 64 ? 768 : 512;
   const long long units = (long long)p.pairs * p.tiles;
   const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
   p.pieces = (int)std::min(most, std::max(1ll, resident / units));
