@@ -712,7 +712,7 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
  * softmax and sums in float32; for the product with V the weights are rounded to float16 in units of their own:
  * off by 2^-11 relative, or by 2^-37 of the row's largest one where that is more. Results repeat bit for bit
  * for the same arguments; they depend on other sequences through max_tokens and max_length only, which
- * decide where sums are cut. max_tokens * heads / kv_heads < 2^31 - 128; with r = sequences * kv_heads
+ * decide where sums are cut. max_tokens * heads / kv_heads < 2^31 - 256; with r = sequences * kv_heads
  * and t = max_tokens * heads / kv_heads / 128 rounded up, r t (times the pieces that the slots are cut
  * into) < 2^24 workgroups.
  */

@@ -2,22 +2,33 @@
 //
 // For a sequence and a KV head the rows are its new tokens times the query heads that share the
 // head: row r is head r % group of token r / group, so all of them read the same keys and values, and a few
-// tokens fill a tile as well as many. A workgroup takes 128 rows, a wave 32, and walks
-// along the slots in tiles (64, or 32 at head dim 256) that its threads bring through registers to LDS, as
-// float16 whatever the cache holds (INT4 as fp16(q s), FP8 exactly), two tiles in turn:
+// tokens fill a tile as well as many. A workgroup takes 128 or 256 rows, a wave 32, and walks
+// along the slots in tiles (64, or 32 at head dim 256) that its waves bring through registers to LDS, as
+// float16 whatever the cache holds (INT4 as fp16(q s), FP8 exactly), two tiles in turn. Per block of 32 slots:
 //   S^T = K Q^T    mfma 32x32x16, keys from LDS, queries in registers;
 //   p = 2^(S - m)  a lane holds one row's p of 16 of 32 slots (lanes l and l + 32 share a row);
 //   O^T += V^T P^T values from LDS, transposed (ds_read_b64_tr), in the order of slots that the lane's p
 //                  have, so that P goes from one product's result into the other's operand.
 // p is rounded to float16 in units that leave a row's largest at 2^12 or more, as in the attention
-// of single tokens; sums are float32. Bound by the matrix instructions and, next to them, the
-// exponentials: 4 D flops and one exponential per row and slot.
+// of single tokens; sums are float32.
+//
+// The matrix instructions bound it (4 D flops per row and slot), if the vector instructions (an exponential, a
+// product, a sum and a maximum per row and slot, and a part of each tile's way to LDS) run beside them.
+// The next block's S^T is computed beside this block's exponentials, and every product's operands are
+// read three products ahead, in an issue order that is written out: left to itself the compiler reads an
+// operand and waits for it (prompts of 8192 tokens, four, 32 / 8 heads of 128, FP8: 1147 -> 915 us).
+// Addresses of a wave's rows are scalar (its rows lie in one block of 16 slots, one page), and what is rare is
+// kept out of the loop, where its constants cost the scalar registers of all (1147 -> 983 us).
+// Measured: that batch 900 us (950 TFLOP/s; a float16 product of 8192^3 in the library reaches 1210; without the
+// exponentials, or without the way to LDS, 7 and 12 % less); as float16 945 us; two of 8192 with 16 / 8
+// heads of 256 880 (670); 1024 tokens after 12288 in INT4 275 us (780). Small calls are a chain of
+// launch, rows, pages and tiles and a second launch: nine sequences of up to 7 tokens after 1501 16 us.
 //
 // Where the rows do not fill the card, the slots are cut into pieces, joined by a second kernel in order.
 //
 // Slots that a row must not see get p = 0. What is there may still not be finite, and 0 times
 // it is NaN: slots past the end and under the mask are 0 in LDS; of tiles on the diagonal the
-// numbers that are not finite are, too, and are added to the rows that do see them afterwards.
+// numbers that are not finite are, too, and are added at the end to the rows that do see them.
 #include <algorithm>
 #include <type_traits>
 
@@ -34,8 +45,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) v4s* lds_v4s;
 
-constexpr int kThreads = 256;
-constexpr int kRows = 128;  // of a workgroup
+constexpr int kJoinThreads = 256;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kLift = 12;
 constexpr float kRoom = 15.0f;
@@ -43,20 +53,21 @@ constexpr float kRoom = 15.0f;
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-template <int D, int kFormat>
+template <int D, int kFormat, int kWaves>
 struct Tile {
+  static constexpr int kThreads = 64 * kWaves, kRows = 32 * kWaves;
   static constexpr int kSlots = D == 256 ? 32 : 64;
   static constexpr int kBlocks = kSlots / 32;
   static constexpr int kSteps = D / 16;   // mfma steps of a logit
   static constexpr int kOut = D / 32;     // blocks of output channels
   static constexpr int kBytes = kSlots * D * 2;
-  // Loads: kWidth bytes per thread, kLanes threads to a row. The rows that a wave loads at a time, at most
+  // Loads: kWidth bytes per thread (16, or what gives every wave something), kLanes threads to a row. The rows that a wave loads at a time, at most
   // 16, lie in one block of 16 slots: their page and address are the wave's.
   static constexpr int kRow = kFormat == kCacheInt4 ? D / 2 : kFormat == kCacheFp8 ? D : 2 * D;
-  static constexpr int kWidth = kRow < 64 ? 8 : 16;
-  static constexpr int kLanes = kRow / kWidth;
+  static constexpr int kLanes = kRow / 16 > kThreads / kSlots ? kRow / 16 : kThreads / kSlots;
+  static constexpr int kWidth = kRow / kLanes;
   static constexpr int kWaveRows = 64 / kLanes;
-  static constexpr int kPasses = kSlots / (4 * kWaveRows);
+  static constexpr int kPasses = kSlots / (kWaves * kWaveRows);
   // 8 float16 numbers each.
   static constexpr int kChunks = kWidth / (kFormat == kCacheInt4 ? 4 : kFormat == kCacheFp8 ? 8 : 16);
   static constexpr int kPerSimd = D == 256 ? 1 : D == 64 ? 3 : 2;
@@ -76,11 +87,13 @@ struct Tile {
 
 struct Plan {
   int group;
+  int waves;   // per workgroup
+  int rows;    // per workgroup, 32 per wave
   int tiles;   // of rows, per sequence and KV head
   int pieces;  // of the slots, per tile
   int pairs;   // sequences x KV heads
   bool by_xcd;
-  float* part;    // pairs x tiles x pieces x kRows x D: sums relative to m; nullptr: one piece
+  float* part;    // pairs x tiles x pieces x rows x D: sums relative to m; nullptr: one piece
   float2* stats;  // the same without D: m (base 2) and the sum of p
 };
 
@@ -163,17 +176,18 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, const KvView& c, 
   w->count = min(end - start, a.max_tokens);
   w->length = min(max(a.lengths[w->b], 0), a.max_length);
   w->seen = w->length - w->count + 1;
-  return (long long)w->tile * kRows < (long long)w->count * plan.group;
+  return (long long)w->tile * plan.rows < (long long)w->count * plan.group;
 }
 
-template <int D, int kFormat, bool kMask>
-__global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
+template <int D, int kFormat, bool kMask, int kWaves>
+__global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
+                                  (Tile<D, kFormat, kWaves>::kPerSimd))
     prompt_kernel(PromptArgs a, KvView c, Plan plan) {
-  using T = Tile<D, kFormat>;
+  using T = Tile<D, kFormat, kWaves>;
   __shared__ __attribute__((aligned(16))) uint8_t keys[2][T::kBytes];
   __shared__ __attribute__((aligned(16))) uint8_t values[2][T::kBytes];
   // Slots with values that are not finite, of the tiles that some rows see in part.
-  constexpr int kPartial = kRows / T::kSlots + 2;
+  constexpr int kPartial = T::kRows / T::kSlots + 2;
   __shared__ uint32_t bad_slots[kPartial * T::kBlocks];
 
   Where at;
@@ -181,7 +195,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rows = at.count * plan.group;  // below 2^31: checked by the host
-  const int row0 = at.tile * kRows;
+  const int row0 = at.tile * T::kRows;
   const int my_row = min(row0 + 32 * wave + col, rows - 1);
   const int token = my_row / plan.group;
   const int head = at.hk * plan.group + my_row % plan.group;
@@ -191,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
     return min(max(at.seen + min(r, rows - 1) / plan.group, 0), at.length);
   };
   const int wave_all = seen_by(row0 + 32 * wave);
-  const int all = seen_by(row0), any = seen_by(row0 + kRows - 1);
+  const int all = seen_by(row0), any = seen_by(row0 + T::kRows - 1);
   const bool wave_works = row0 + 32 * wave < rows;
 
   const int steps = (any + T::kSlots - 1) / T::kSlots;
@@ -229,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
   const int last = (at.length - 1) & ~15;
   // ahead: 32 for keys, whose tiles lie a block of 32 slots later.
   const auto group_slot = [&](int step, int p, int ahead) {
-    return max(min(step * T::kSlots + ahead + T::kWaveRows * (4 * p + wave),
+    return max(min(step * T::kSlots + ahead + T::kWaveRows * (kWaves * p + wave),
                    last + 16 - T::kWaveRows), 0);
   };
   const int32_t* table = c.table + (size_t)at.b * c.max_pages;
@@ -289,13 +303,13 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
     for (int k = 0; k < kParts; ++k) to.x[k] = convert(from, k / T::kChunks, k % T::kChunks);
   };
   const auto write_keys = [&](int k, v4u x, int buf) {
-    const int r = T::kWaveRows * (4 * (k / T::kChunks) + wave) + my_row_of;
+    const int r = T::kWaveRows * (kWaves * (k / T::kChunks) + wave) + my_row_of;
     *reinterpret_cast<v4u*>(keys[buf] + T::key_at(r, my_lane * T::kChunks + k % T::kChunks)) = x;
   };
   const auto write_values = [&](const Rows& v, int buf) {
 #pragma unroll
     for (int k = 0; k < kParts; ++k) {
-      const int r = T::kWaveRows * (4 * (k / T::kChunks) + wave) + my_row_of;
+      const int r = T::kWaveRows * (kWaves * (k / T::kChunks) + wave) + my_row_of;
       *reinterpret_cast<v4u*>(values[buf] +
                               T::value_at(r, my_lane * T::kChunks + k % T::kChunks)) = v.x[k];
     }
@@ -313,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
     const bool marks = step >= first_partial;
 #pragma unroll
     for (int p = 0; p < T::kPasses; ++p) {
-      const int r = T::kWaveRows * (4 * p + wave) + my_row_of;
+      const int r = T::kWaveRows * (kWaves * p + wave) + my_row_of;
       const bool live = step * T::kSlots + r < at.length && (!kMask || mask[p] != 0);
       uint32_t found = 0;
 #pragma unroll
@@ -553,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
   if (plan.part) {
     const size_t unit =
         (((size_t)(at.b * c.heads + at.hk) * plan.tiles + at.tile) * plan.pieces + at.piece) *
-            kRows + 32 * wave + col;
+            T::kRows + 32 * wave + col;
     if (half == 0) plan.stats[unit] = make_float2(m, sum);
     float* out = plan.part + unit * D;
 #pragma unroll
@@ -579,29 +593,28 @@ __global__ void __launch_bounds__(kThreads, (Tile<D, kFormat>::kPerSimd))
 
 // Pieces of a row joined: D / 4 threads to a row. Grid: pairs x tiles x groups of rows.
 template <int D>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kJoinThreads)
     prompt_join_kernel(PromptArgs a, KvView c, Plan plan) {
-  constexpr int kAtOnce = kThreads / (D / 4);
-  constexpr int kGroups = kRows / kAtOnce;
-  const int unit = blockIdx.x / kGroups;
+  constexpr int kAtOnce = kJoinThreads / (D / 4);
+  const int groups = plan.rows / kAtOnce, unit = blockIdx.x / groups;
   const int pair = unit / plan.tiles, tile = unit % plan.tiles;
   const int b = pair / c.heads, hk = pair % c.heads;
-  const int r = blockIdx.x % kGroups * kAtOnce + threadIdx.x / (D / 4);
+  const int r = blockIdx.x % groups * kAtOnce + threadIdx.x / (D / 4);
   const int d = threadIdx.x % (D / 4) * 4;
   const int start = min(max(a.row_start[b], 0), a.M);
   const int end = min(max(a.row_start[b + 1], start), a.M);
-  const long long my_row = (long long)tile * kRows + r;
+  const long long my_row = (long long)tile * plan.rows + r;
   if (my_row >= (long long)min(end - start, a.max_tokens) * plan.group) return;
-  const size_t first = (size_t)unit * plan.pieces * kRows + r;
+  const size_t first = (size_t)unit * plan.pieces * plan.rows + r;
   float top = -INFINITY;
   for (int i = 0; i < plan.pieces; ++i)
-    top = fmaxf(top, plan.stats[first + (size_t)i * kRows].x);
+    top = fmaxf(top, plan.stats[first + (size_t)i * plan.rows].x);
   const float base = top == -INFINITY ? 0.0f : top;
   float total = 0.0f;
   v4f acc = {};
 #pragma unroll 4
   for (int i = 0; i < plan.pieces; ++i) {
-    const size_t at = first + (size_t)i * kRows;
+    const size_t at = first + (size_t)i * plan.rows;
     const float2 st = plan.stats[at];
     const float f = __builtin_amdgcn_exp2f(st.x - base);
     total += st.y * f;
@@ -616,6 +629,12 @@ __global__ void __launch_bounds__(kThreads)
   if (d == 0 && a.lse) a.lse[row] = log_sum(top, total);
 }
 
+// Rows of all sequences and KV heads times slots from which, at head dim 128, workgroups of eight waves are
+// taken. They bring each tile to LDS for twice as many rows, but are half as many. With 32 / 8 heads: 8192 tokens
+// of four sequences, FP8, 937 -> 891 us, 4096 of one 186 -> 164, 1024 after 12288 in INT4 293 -> 275; 2048
+// of one 65 -> 77, 1024 after 2000 in INT4 81 -> 89.
+constexpr long long kWide = 5ll << 26;
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 long long units_of(const Plan& p) { return (long long)p.pairs * p.tiles * p.pieces; }
@@ -623,7 +642,7 @@ long long first_grid(const Plan& p) {
   return (p.by_xcd ? ((long long)p.pairs + 7) / 8 * 8 : p.pairs) * p.tiles * p.pieces;
 }
 long long second_grid(const Plan& p, int dim) {
-  return p.pieces > 1 ? (long long)p.pairs * p.tiles * (kRows / (kThreads / (dim / 4))) : 0;
+  return p.pieces > 1 ? (long long)p.pairs * p.tiles * (p.rows / (kJoinThreads / (dim / 4))) : 0;
 }
 
 Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void* workspace,
@@ -632,14 +651,17 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   p.group = heads / c.heads;
   p.pairs = c.sequences * c.heads;
   p.by_xcd = p.pairs % 8 == 0 || p.pairs >= 64;
-  p.tiles = (int)(((long long)max_tokens * p.group - 1) / kRows + 1);
+  const long long all_rows = (long long)max_tokens * p.group * p.pairs;
+  p.waves = c.dim == 128 && all_rows >= kWide / max_length ? 8 : 4;
+  p.rows = 32 * p.waves;
+  p.tiles = (int)(((long long)max_tokens * p.group - 1) / p.rows + 1);
   // Pieces, of four steps at least, where the tiles alone do not fill the card.
   const int slots = c.dim == 256 ? 32 : 64;
   const long long resident = c.dim == 256 ? 256 : c.dim == 64 ? 768 : 512;
   const long long units = (long long)p.pairs * p.tiles;
   const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
   p.pieces = (int)std::min(most, std::max(1ll, resident / units));
-  const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * kRows : 0;
+  const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * p.rows : 0;
   const size_t stats = align256(rows * sizeof(float2));
   *bytes = stats + rows * c.dim * 4;
   if (workspace && rows) {
@@ -654,10 +676,13 @@ hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream
   const unsigned grid = (unsigned)first_grid(p);
   const auto run = [&](auto format) {
     constexpr int f = decltype(format)::value;
-    if (a.mask)
-      prompt_kernel<D, f, true><<<grid, kThreads, 0, stream>>>(a, c, p);
-    else
-      prompt_kernel<D, f, false><<<grid, kThreads, 0, stream>>>(a, c, p);
+    const auto go = [&](auto kernel) { kernel<<<grid, 64 * p.waves, 0, stream>>>(a, c, p); };
+    if constexpr (D == 128)
+      if (p.waves == 8) {
+        a.mask ? go(prompt_kernel<D, f, true, 8>) : go(prompt_kernel<D, f, false, 8>);
+        return;
+      }
+    a.mask ? go(prompt_kernel<D, f, true, 4>) : go(prompt_kernel<D, f, false, 4>);
   };
   switch (c.format) {
     case kCacheInt4: run(Int<kCacheInt4>()); break;
@@ -666,7 +691,7 @@ hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream
   }
   if (hipError_t e = hipGetLastError()) return e;
   if (p.pieces > 1)
-    prompt_join_kernel<D><<<(unsigned)second_grid(p, D), kThreads, 0, stream>>>(a, c, p);
+    prompt_join_kernel<D><<<(unsigned)second_grid(p, D), kJoinThreads, 0, stream>>>(a, c, p);
   return hipGetLastError();
 }
 
@@ -674,10 +699,10 @@ hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream
 
 bool prompt_fits(const KvView& c, int heads, int max_tokens, int max_length) {
   // Rows of a sequence and KV head are numbered in 31 bits.
-  if ((long long)max_tokens * (heads / c.heads) >= (1ll << 31) - kRows) return false;
+  if ((long long)max_tokens * (heads / c.heads) >= (1ll << 31) - 256) return false;
   size_t bytes;
   const Plan p = make_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
-  return fits_grid(first_grid(p), kThreads) && fits_grid(second_grid(p, c.dim), kThreads);
+  return fits_grid(first_grid(p), 64 * p.waves) && fits_grid(second_grid(p, c.dim), kJoinThreads);
 }
 
 size_t prompt_workspace_bytes(const KvView& c, int heads, int max_tokens, int max_length) {

@@ -223,3 +223,26 @@ def test_graph(mask):
         for x, y in zip(got, call()):
             assert torch.equal(x, y)
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4", "fp8"])
+@pytest.mark.parametrize("mask", [False, True])
+def test_many_rows(fmt, mask):
+    """Bounds of 4096 tokens with 64 heads and 8192 slots take workgroups of eight waves, tight ones of four."""
+    gen = torch.Generator().manual_seed(10)
+    hk, heads, D, B = 16, 64, 128, 2
+    cache, plain = R.make_cache(gen, B, 8192, hk, D, 64, fmt)
+    counts, lengths = [70, 3], [640, 77]
+    starts, rows = _starts(counts)
+    Q = torch.randn((4096, heads, D), generator=gen).half().cuda()
+    n, s = _int(lengths), _int(starts)
+    m = None
+    if mask:
+        m = (torch.rand((B, cache.capacity), generator=gen) < 0.7).cuda()
+    _fill_dead(cache, n, m, fmt)
+    out, lse = rrs.prompt_attention(Q, cache, s, n, mask=m, return_lse=True)
+    ref = R.attention(Q, plain, rows, lengths, D ** -0.5, m)
+    R.check(out, lse, ref, rows)
+    out, lse = rrs.prompt_attention(Q, cache, s, n, max_tokens=70, max_length=640, mask=m,
+                                    return_lse=True)
+    R.check(out, lse, ref, rows)
