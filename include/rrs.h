@@ -571,7 +571,7 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *  - RRS_KV_FP8: k, v hold head_dim bytes per row, 8-bit floats of 4 exponent and 3 mantissa bits (bias
  *    7, no infinities, 0x7F and 0xFF are NaN, largest 448). k_scale, v_scale: pages x kv_heads x
  *    page_size / 16 float16, one for each block of 16 slots of a page and head: a power of two s
- *    in [2^-15, 2^8]. A row stands for q s, which is a float16 number exactly. What an append makes of it
+ *    in [2^-15, 2^8] (0 counts as 2^-15). A row stands for q s, which is a float16 number exactly. What an append makes of it
  *    is stated at rrs_rope_kv_append. rrs_kv_evict moves single rows and refuses this format.
  *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
  *    read. No page belongs to two rows of the table in a call that writes the cache.

@@ -506,8 +506,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u) {
       if constexpr (kFp8) {
-        key_unit[u] = half_to_float(ks[u][0]);
-        val_unit[u] = half_to_float(vs[u][0]);
+        key_unit[u] = block_unit(ks[u][0]);
+        val_unit[u] = block_unit(vs[u][0]);
       }
       v4f s = {};
 #pragma unroll

@@ -201,6 +201,12 @@ __device__ __forceinline__ v4u dequant8(uint32_t codes, float s) {
   return w;
 }
 
+// An FP8 block's scale: 2 to its exponent, a finite number whatever the float16 is (of a block that was
+// never written, all of whose slots take no part).
+__device__ __forceinline__ float block_unit(uint32_t half) {
+  return __builtin_bit_cast(float, ((half & 0x7C00u) << 13) + ((127u - 15u) << 23));
+}
+
 // Two e4m3 codes, bytes 2 kHalf and 2 kHalf + 1 of w, as float16 in units of a power of two (of which the
 // instruction takes the exponent). Exact from 2^-15 on: a code's smallest step is 2^-9, float16's 2^-24.
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));

@@ -460,8 +460,8 @@ __global__ void __launch_bounds__(kThreads)
   if (t < lengths[b]) {
     const size_t row = c.row_of(b, h, t);
     if constexpr (kFormat == kCacheFp8) {
-      const float ks = half_to_float(c.k_scale[row / kSlots8]);
-      const float vs = half_to_float(c.v_scale[row / kSlots8]);
+      const float ks = block_unit(c.k_scale[row / kSlots8]);
+      const float vs = block_unit(c.v_scale[row / kSlots8]);
       k = dequant8_fp8(reinterpret_cast<const uint2*>(c.k + row * D)[i], ks);
       v = dequant8_fp8(reinterpret_cast<const uint2*>(c.v + row * D)[i], vs);
     } else if constexpr (kFormat == kCacheInt4) {

@@ -289,7 +289,7 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
       return eight_int4(from.x[p][i], s);
     } else if constexpr (kFormat == kCacheFp8) {
       return dequant8_fp8(make_uint2(from.x[p][2 * i], from.x[p][2 * i + 1]),
-                          half_to_float(from.scale[p]));
+                          block_unit(from.scale[p]));
     } else {
       return from.x[p];
     }

@@ -254,12 +254,16 @@ def test_attention(D, heads, hk, page, lengths, mask, weights):
     slots = torch.arange(cache.capacity, device="cuda")
     dead = slots >= n[:, None] if m is None else (slots >= n[:, None]) | ~m
     for pool in (cache.k, cache.v):
-        bad = pool.view(torch.uint8)[cache.table.long()].transpose(1, 2)   # B, pages, P, hk, D ...
         rows = pool.view(torch.uint8)
         for b in range(B):
             t = slots[dead[b]]
             rows[cache.table[b, t // page].long(), :, t % page] = 127
-        del bad
+    # The scales of blocks none of whose slots take part, too.
+    blocks = dead.view(B, -1, 16).all(-1)
+    for b in range(B):
+        j = torch.arange(blocks.shape[1], device="cuda")[blocks[b]]
+        for s in (cache.k_scale, cache.v_scale):
+            s[cache.table[b, j * 16 // page].long(), :, j * 16 % page // 16] = math.nan
     w = torch.rand((B, hk, cache.capacity), generator=gen).cuda() if weights else None
     w0 = w.cpu() if weights else None
     out, lse = rrs.paged_attention(Q, cache, n, max_length=max(top, 1), mask=m, weights=w,

@@ -36,6 +36,10 @@ def _fill_dead(cache, n, mask, fmt):
                 scale[page, :, at] = math.nan
             else:
                 pool.view(torch.uint8)[page, :, at] = 127
+        if fmt == "fp8":   # scales of blocks none of whose slots take part
+            j = slots[::16][dead[b].view(-1, 16).all(-1)]
+            for scale in (cache.k_scale, cache.v_scale):
+                scale[cache.table[b, j // P].long(), :, j % P // 16] = math.nan
 
 
 CASES = [
