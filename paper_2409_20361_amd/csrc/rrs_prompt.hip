@@ -21,7 +21,7 @@
 // kept out of the loop, where its constants cost the scalar registers of all (1147 -> 983 us).
 // Measured: that batch 900 us (950 TFLOP/s; a float16 product of 8192^3 in the library reaches 1210; without the
 // exponentials, or without the way to LDS, 7 and 12 % less); as float16 945 us; two of 8192 with 16 / 8
-// heads of 256 880 (670); 1024 tokens after 12288 in INT4 275 us (780). Small calls are a chain of
+// heads of 256 880 (670); 1024 tokens after 12288 in INT4 265 us (810). Small calls are a chain of
 // launch, rows, pages and tiles and a second launch: nine sequences of up to 7 tokens after 1501 16 us.
 //
 // Where the rows do not fill the card, the slots are cut into pieces, joined by a second kernel in order.
@@ -629,11 +629,18 @@ __global__ void __launch_bounds__(kJoinThreads)
   if (d == 0 && a.lse) a.lse[row] = log_sum(top, total);
 }
 
-// Rows of all sequences and KV heads times slots from which, at head dim 128, workgroups of eight waves are
-// taken. They bring each tile to LDS for twice as many rows, but are half as many. With 32 / 8 heads: 8192 tokens
-// of four sequences, FP8, 937 -> 891 us, 4096 of one 186 -> 164, 1024 after 12288 in INT4 293 -> 275; 2048
-// of one 65 -> 77, 1024 after 2000 in INT4 81 -> 89.
+// At head dim 128 workgroups of eight waves bring each tile to LDS for twice as many rows, but are half as many.
+// They are taken for 1024 rows or more of one sequence behind at least as many cached tokens (32 / 8 heads: 1024 after 8000, INT4,
+// 206 -> 187 us, 512 after 8000, FP8, 106 -> 97; 2000 after 2000, 32 / 32 heads, float16, 163 -> 144; but 300 after 300, 32 / 32 heads, 26 against 31) and from so
+// many rows of all sequences and KV heads times slots on (4096 tokens of one sequence 188 -> 170, 8192 of four 937
+// -> 891); not for less without a past (2048 of one 66 against 72, 512 of four after up to 4000 120 against 129).
 constexpr long long kWide = 5ll << 26;
+bool eight_waves(const KvView& c, int heads, int max_tokens, int max_length) {
+  if (c.dim != 128) return false;
+  const long long rows = (long long)max_tokens * (heads / c.heads);
+  if (c.sequences == 1 && rows >= 1024 && max_length / 2 >= max_tokens) return true;
+  return rows * c.heads * c.sequences >= kWide / max_length;
+}
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -651,13 +658,12 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   p.group = heads / c.heads;
   p.pairs = c.sequences * c.heads;
   p.by_xcd = p.pairs % 8 == 0 || p.pairs >= 64;
-  const long long all_rows = (long long)max_tokens * p.group * p.pairs;
-  p.waves = c.dim == 128 && all_rows >= kWide / max_length ? 8 : 4;
+  p.waves = eight_waves(c, heads, max_tokens, max_length) ? 8 : 4;
   p.rows = 32 * p.waves;
   p.tiles = (int)(((long long)max_tokens * p.group - 1) / p.rows + 1);
   // Pieces, of four steps at least, where the tiles alone do not fill the card.
   const int slots = c.dim == 256 ? 32 : 64;
-  const long long resident = c.dim == 256 ? 256 : c.dim == 64 ? 768 : 512;
+  const long long resident = c.dim == 256 || p.waves == 8 ? 256 : c.dim == 64 ? 768 : 512;
   const long long units = (long long)p.pairs * p.tiles;
   const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
   p.pieces = (int)std::min(most, std::max(1ll, resident / units));
