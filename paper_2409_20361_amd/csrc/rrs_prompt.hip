@@ -591,35 +591,59 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
   if (half == 0 && a.lse) a.lse[row] = log_sum(m, sum);
 }
 
-// Pieces of a row joined: D / 4 threads to a row. Grid: pairs x tiles x groups of rows.
-template <int D>
+// Pieces of a row joined: D / 4 threads to a row, or several groups of so many, which take the row's pieces in
+// turn. Grid: pairs x tiles x groups of kRowsAtOnce rows.
+template <int D, int kRowsAtOnce>
 __global__ void __launch_bounds__(kJoinThreads)
     prompt_join_kernel(PromptArgs a, KvView c, Plan plan) {
-  constexpr int kAtOnce = kJoinThreads / (D / 4);
-  const int groups = plan.rows / kAtOnce, unit = blockIdx.x / groups;
+  constexpr int kLanes = D / 4, kGroups = kJoinThreads / (kLanes * kRowsAtOnce);
+  __shared__ v4f sums[kGroups > 1 ? kJoinThreads : 1];
+  __shared__ float2 stats[kGroups > 1 ? kGroups : 1][kRowsAtOnce];
+  const int blocks = plan.rows / kRowsAtOnce, unit = blockIdx.x / blocks;
   const int pair = unit / plan.tiles, tile = unit % plan.tiles;
   const int b = pair / c.heads, hk = pair % c.heads;
-  const int r = blockIdx.x % groups * kAtOnce + threadIdx.x / (D / 4);
-  const int d = threadIdx.x % (D / 4) * 4;
+  const int mine = threadIdx.x / kLanes % kRowsAtOnce, group = threadIdx.x / (kLanes * kRowsAtOnce);
+  const int r = blockIdx.x % blocks * kRowsAtOnce + mine;
+  const int d = threadIdx.x % kLanes * 4;
   const int start = min(max(a.row_start[b], 0), a.M);
   const int end = min(max(a.row_start[b + 1], start), a.M);
   const long long my_row = (long long)tile * plan.rows + r;
-  if (my_row >= (long long)min(end - start, a.max_tokens) * plan.group) return;
+  const bool there = my_row < (long long)min(end - start, a.max_tokens) * plan.group;
   const size_t first = (size_t)unit * plan.pieces * plan.rows + r;
-  float top = -INFINITY;
-  for (int i = 0; i < plan.pieces; ++i)
-    top = fmaxf(top, plan.stats[first + (size_t)i * plan.rows].x);
-  const float base = top == -INFINITY ? 0.0f : top;
-  float total = 0.0f;
+  float top = -INFINITY, total = 0.0f;
   v4f acc = {};
+  if (there) {
 #pragma unroll 4
-  for (int i = 0; i < plan.pieces; ++i) {
-    const size_t at = first + (size_t)i * plan.rows;
-    const float2 st = plan.stats[at];
-    const float f = __builtin_amdgcn_exp2f(st.x - base);
-    total += st.y * f;
-    acc += *reinterpret_cast<const v4f*>(plan.part + at * D + d) * f;
+    for (int i = group; i < plan.pieces; i += kGroups)
+      top = fmaxf(top, plan.stats[first + (size_t)i * plan.rows].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll 4
+    for (int i = group; i < plan.pieces; i += kGroups) {
+      const size_t at = first + (size_t)i * plan.rows;
+      const float2 st = plan.stats[at];
+      const float f = __builtin_amdgcn_exp2f(st.x - base);
+      total += st.y * f;
+      acc += *reinterpret_cast<const v4f*>(plan.part + at * D + d) * f;
+    }
   }
+  if constexpr (kGroups > 1) {
+    sums[threadIdx.x] = acc;
+    if (d == 0) stats[group][mine] = make_float2(top, total);
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) top = fmaxf(top, stats[g][mine].x);
+    const float base = top == -INFINITY ? 0.0f : top;
+    total = 0.0f;
+    acc = v4f{};
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const float f = __builtin_amdgcn_exp2f(stats[g][mine].x - base);
+      total += stats[g][mine].y * f;
+      acc += sums[g * kLanes * kRowsAtOnce + threadIdx.x] * f;
+    }
+  }
+  if (!there) return;
   const float inv = total != 0.0f ? 1.0f / total : 0.0f;
   const size_t row = ((size_t)start + my_row / plan.group) * a.heads + hk * plan.group +
                      my_row % plan.group;
@@ -627,6 +651,14 @@ __global__ void __launch_bounds__(kJoinThreads)
       v4h{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv),
           (_Float16)(acc[3] * inv)};
   if (d == 0 && a.lse) a.lse[row] = log_sum(top, total);
+}
+
+// Rows of a workgroup of the join: up to eight pieces one after the other; more by eight groups of threads (head
+// dim 256: four) at once (62 pieces of 5 tokens with 40 heads over 16000 slots: 40 -> 22 us; 5 pieces of 96
+// tiles 41 -> 47).
+int join_rows(int dim, int pieces) {
+  const int all = kJoinThreads / (dim / 4);
+  return pieces <= 8 ? all : all > 8 ? all / 8 : 1;
 }
 
 // At head dim 128 workgroups of eight waves bring each tile to LDS for twice as many rows, but are half as many.
@@ -649,7 +681,7 @@ long long first_grid(const Plan& p) {
   return (p.by_xcd ? ((long long)p.pairs + 7) / 8 * 8 : p.pairs) * p.tiles * p.pieces;
 }
 long long second_grid(const Plan& p, int dim) {
-  return p.pieces > 1 ? (long long)p.pairs * p.tiles * (p.rows / (kJoinThreads / (dim / 4))) : 0;
+  return p.pieces > 1 ? (long long)p.pairs * p.tiles * (p.rows / join_rows(dim, p.pieces)) : 0;
 }
 
 Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void* workspace,
@@ -667,6 +699,9 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   const long long units = (long long)p.pairs * p.tiles;
   const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
   p.pieces = (int)std::min(most, std::max(1ll, resident / units));
+  // With a workgroup on every CU already, a second one and the join pay from some 20 steps on (32 / 8 heads:
+  // 1024 tokens 39 us in two pieces, 34 in one, 32 x 4 after up to 700 26 and 22, after up to 2000 38 and 48).
+  if (units >= 256 && max_length < 1280) p.pieces = 1;
   const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * p.rows : 0;
   const size_t stats = align256(rows * sizeof(float2));
   *bytes = stats + rows * c.dim * 4;
@@ -696,8 +731,14 @@ hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream
     default: run(Int<kCacheF16>());
   }
   if (hipError_t e = hipGetLastError()) return e;
-  if (p.pieces > 1)
-    prompt_join_kernel<D><<<(unsigned)second_grid(p, D), kJoinThreads, 0, stream>>>(a, c, p);
+  if (p.pieces > 1) {
+    constexpr int kAll = kJoinThreads / (D / 4);
+    const unsigned joins = (unsigned)second_grid(p, D);
+    if (join_rows(D, p.pieces) == kAll)
+      prompt_join_kernel<D, kAll><<<joins, kJoinThreads, 0, stream>>>(a, c, p);
+    else
+      prompt_join_kernel<D, (kAll > 8 ? kAll / 8 : 1)><<<joins, kJoinThreads, 0, stream>>>(a, c, p);
+  }
   return hipGetLastError();
 }
 
