@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over its paged cache. gfx950 only.
 //
 // For a sequence and a KV head, up to 16 of the query heads that share it are the columns of the
-// matrix products. A wave takes tiles of slots (32 float16, 64 INT4), with
+// matrix products. A wave takes tiles of slots (32 float16 or FP8, 64 INT4), with
 // the running maximum m and sum of the softmax of each column kept in its registers:
 //   S^T = K Q^T    mfma 16x16x32: a lane reads 16 bytes of its slot's row (lane & 15) as the
 //                  operand itself, straight from the cache;
@@ -10,6 +10,8 @@
 //                  side: its rows go through LDS and are read back transposed
 //                  (ds_read_b64_tr). The slots that a quarter of the wave reads are those whose p it holds,
 //                  so P goes from the first product's result into the second's operand without leaving the lane.
+// FP8 codes become float16 in the units of their block's scale, exactly (one instruction for two), keys as they come,
+// values behind the transposed read (of 8-bit elements), so that all else is as for float16.
 // All of it is streaming: HBM bounds it (4 D bytes and 4 D flops per slot and query head), so
 // loads for the next tile are issued before the current one is done with.
 //
@@ -35,7 +37,9 @@
 // codes' way to float16, at three waves per SIMD; 64 of 1 to 8192 with 16 KV heads
 // 127 us with the join, 4.4 TB/s); 8 x 40 heads over one KV head of 256 with a mask, 19 us (2.0 TB/s: latency of three or
 // four tiles per wave, the rows read by three row blocks); one sequence of 117 slots, 32 heads, 5
-// us (latency); 179 x 64 heads of up to 5 slots 14 us.
+// us (latency); 179 x 64 heads of up to 5 slots 14 us. FP8: 64 sequences of 1 to 8192 slots, 8 KV heads of 128, 100 to
+// 105 us (5.0 to 5.2 TB/s: pieces of different sizes), one of 131071 with a mask 51 to 54 (5.0 to 5.2; a piece is 11
+// steps, of which the first waits for its loads), one of 213 with 32 heads 5.8.
 #include <type_traits>
 
 #include "rrs_device.h"

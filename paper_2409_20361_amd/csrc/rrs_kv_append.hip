@@ -10,6 +10,10 @@
 // of 32 + 32 + 32 heads of 128, float16, 78.0 us (5.2 TB/s read and written; a copy of 400 MiB reaches
 // 5.4); 1117 tokens of 32 + 8 + 8 into INT4, 9.0 to 10.4 us, one token 2.3 to 2.7 us (latency).
 //
+// Into FP8 a block of 16 slots shares a scale, so a block's new tokens belong to one wave, with the rows that they find
+// there (rope_kv_append8_kernel). The same bytes bound it: 6113 tokens of 32 + 32 + 32 heads of 128 59 us (4.3
+// TB/s read and written), one token 4.0 to 4.6 us (one more chain: the rows of its run, the block's scale).
+//
 // Read-back. One row of K and V per D / 8 lanes; bound by the writes, which go past the caches
 // (134 MB from 2048 slots of 4 x 32 INT4 heads: 25.7 us, 40.8 with ordinary stores;
 // 41 with both where inputs and outputs in use outgrow the last-level cache).

@@ -250,3 +250,19 @@ def test_many_rows(fmt, mask):
     out, lse = rrs.prompt_attention(Q, cache, s, n, max_tokens=70, max_length=640, mask=m,
                                     return_lse=True)
     R.check(out, lse, ref, rows)
+
+
+@pytest.mark.parametrize("D,hk,L,fmt", [(128, 1, 5003, "fp8"), (256, 2, 3001, "int4"),
+                                        (64, 1, 9001, "f16")])
+def test_many_pieces(D, hk, L, fmt):
+    """A few tokens over one long cache: many pieces, the join by groups of threads; a row without a slot."""
+    gen = torch.Generator().manual_seed(D)
+    cache, plain = R.make_cache(gen, 1, L, hk, D, 64, fmt)
+    starts, rows = _starts([5])
+    Q = torch.randn((5, 3 * hk, D), generator=gen).half().cuda()
+    m = torch.ones((1, cache.capacity), dtype=torch.bool, device="cuda")
+    m[0, :L - 4] = False
+    for mask in (None, m):
+        out, lse = rrs.prompt_attention(Q, cache, _int(starts), _int([L]), mask=mask,
+                                        return_lse=True)
+        R.check(out, lse, R.attention(Q, plain, rows, [L], D ** -0.5, mask), rows)
