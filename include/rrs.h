@@ -574,7 +574,8 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *    in [2^-15, 2^8] (0 counts as 2^-15). A row stands for q s, which is a float16 number exactly. What an append makes of it
  *    is stated at rrs_rope_kv_append. rrs_kv_evict moves single rows and refuses this format.
  *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
- *    read. No page belongs to two rows of the table in a call that writes the cache.
+ *    read. A page that a call writes into belongs to one row of the table: that of a token that is
+ *    appended, and every page of a cache that rrs_kv_evict takes. Others may be shared.
  * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,
  * sequences, max_pages, pages >= 1; sequences * kv_heads < 2^23; max_pages * page_size
  * <= 2^30. The struct is read on the host during the call only. A launch holds fewer than 2^32
@@ -816,8 +817,8 @@ rrs_status rrs_kv_compact(const int32_t* table, int sequences, int max_pages, in
 /*
  * Pages src[i] of k, v and the scales copied to dst[i], for i < n, or i < min(n, count[0]) where count is
  * given (device memory). Pairs with a number outside [0, pages) are skipped. No page in dst is there twice
- * or in src (RRS_DEBUG: else RRS_ERR_PRECONDITION). n >= 1; kv_heads * page_size * bytes of a row < 2^31. The
- * cache's table is not read.
+ * or in src (RRS_DEBUG: else RRS_ERR_PRECONDITION), and src, dst and count lie outside the pools. n >= 1;
+ * kv_heads * page_size * bytes of a row < 2^31. The cache's table is not read.
  */
 rrs_status rrs_kv_copy_pages(const rrs_kv_cache* cache, const int32_t* src, const int32_t* dst,
                              int n, const int32_t* count, void* stream);
