@@ -582,7 +582,7 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  * threads, of 256 or (kv_evict's selection) 1024 per workgroup: larger calls are RRS_ERR_SHAPE, with
  * nothing enqueued. These are, with r = sequences * kv_heads and all quotients rounded up,
  *  - rrs_rope_kv_append: M >= 2^24; into RRS_KV_FP8 M + M / 16 >= 2^24 or, for M < 768,
- *    M (kv_heads / 2 + heads * head_dim / 4096) >= 2^24;
+ *    2048 + M min(heads * head_dim / 4096, 65535) >= 2^24;
  *  - rrs_paged_attention with weights, where they take a second launch (more than 16 query
  *    heads per KV head, or sequences that are cut): r * max_length / 1024, and sequences * heads
  *    if they are cut, >= 2^24;

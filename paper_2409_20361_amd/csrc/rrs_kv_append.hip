@@ -275,16 +275,16 @@ __device__ __forceinline__ uint32_t rescale4(uint32_t w, float shrink, float mos
 }
 
 // FP8. The first workgroups write keys and values: blocks of 16 slots, whose tokens lie in a run of
-// rows (one sequence, one slot after the other). Each looks through `window` rows for those that
-// begin a run; a wave takes the keys, or the values, of a head of a run: 64 lanes hold 16 rows, so
+// rows (one sequence, one slot after the other). `parts` workgroups look through the same 16 rows for those that
+// begin a run, and share the runs' pairs of heads: a
+// wave takes the keys, or the values, of a head of a run: 64 lanes hold 16 rows, so
 // the block's largest value, its scale and its codes need nothing from another wave. Rows of the
 // block that are not in the run keep their codes, or get new ones where the scale has grown: by a
 // power of two, so that only codes below 2^-6 are rounded again. The other
 // workgroups rotate queries, as above.
 template <int D>
 __global__ void __launch_bounds__(kThreads)
-    rope_kv_append8_kernel(RopeArgs a, KvView c, int window, int parts, int block_groups,
-                           int query_parts) {
+    rope_kv_append8_kernel(RopeArgs a, KvView c, int parts, int block_groups, int query_parts) {
   constexpr int kLanes = D / 16;             // lanes per head row
   constexpr int kHeads = kThreads / kLanes;  // head rows per pass
   constexpr int kRowsAtOnce = 64 / kLanes;   // rows of a block per wave and pass
@@ -339,10 +339,10 @@ __global__ void __launch_bounds__(kThreads)
 
   // Rows m0 .. m0 + 31: bit j of `joins`: row m0 + j goes on with the run of the row before it.
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int m0 = blockIdx.x / parts * window, part = blockIdx.x % parts;
+  const int m0 = blockIdx.x / parts * kSlots8, part = blockIdx.x % parts;
   bool stored = false, joined = false;
   int my_seq = 0, my_slot = 0;
-  if (lane < window + kSlots8 - 1 && m0 + lane < a.M) {
+  if (lane < 2 * kSlots8 - 1 && m0 + lane < a.M) {
     my_seq = a.seq[m0 + lane];
     my_slot = a.slot[m0 + lane];
     size_t row;
@@ -352,13 +352,20 @@ __global__ void __launch_bounds__(kThreads)
              a.seq[m0 + lane - 1] == my_seq && a.slot[m0 + lane - 1] == my_slot - 1;
   }
   const uint64_t joins = __ballot(joined);
-  uint64_t leads = __ballot(stored && !joined) & ((1ull << window) - 1);
+  uint64_t leads = __ballot(stored && !joined) & ((1ull << kSlots8) - 1);
 
   const bool value = wave >= 2;  // waves 0, 1: keys
   const int stride = 2 * parts;
-  while (leads) {
+  // Item n of the window, pair n % pairs of the heads of run n / pairs, is part n % parts's.
+  const int pairs = (c.heads + 1) / 2;
+  for (int own = part; leads; leads &= leads - 1) {
+    const int pair = own;  // its first of this run
+    if (pair >= pairs) {
+      own -= pairs;
+      continue;
+    }
+    own += (pairs - pair + parts - 1) / parts * parts - pairs;
     const int lead = __builtin_ctzll(leads);
-    leads &= leads - 1;
     const int count = 1 + __builtin_ctzll(~(joins >> (lead + 1)));
     const int m = m0 + lead;
     const int seq = __builtin_amdgcn_readlane(my_seq, lead);
@@ -389,7 +396,7 @@ __global__ void __launch_bounds__(kThreads)
           y_next[p] = *reinterpret_cast<const uint4*>(src + ch.o1);
         }
     };
-    int hk = 2 * part + (wave & 1);
+    int hk = 2 * pair + (wave & 1);
     load(hk);
     for (; hk < c.heads; hk += stride) {
       const size_t row = row0 + ((size_t)hk << c.log_page);
@@ -482,22 +489,26 @@ __global__ void __launch_bounds__(kThreads)
   __builtin_nontemporal_store(v, reinterpret_cast<v4u*>(V + out));
 }
 
-// Workgroups of an append into FP8.
+// Workgroups of an append into FP8. A window of 16 rows has work for one workgroup per pair of heads if its
+// tokens are a prompt's, and for 16 if each is of another sequence, which the host does not know. Workgroups
+// without work delay the others, so there are more than the pairs only up to two per CU (into 8 heads of 128: 500
+// tokens of a prompt 11.6 us, with four per CU 14.7, 2000 17.8 and 21.6; one per sequence, 1000 131 us, with
+// none added 147, 800 into one head of 64 16, 14.7 with four, 42 with none), and fewer where windows alone
+// are many (6113 tokens into 32 heads: 2048 in all 99 us, 1024 109, 4096 108).
 struct Append8 {
-  int window, parts, query_parts;
+  int parts, query_parts;
   int block_groups;
   long long grid;
 };
 Append8 append8_sizes(int M, int heads, const KvView& c) {
   Append8 s;
-  const bool few = M < 768;  // as below: all rows in flight at once
   const int per_pass = kThreads / (c.dim / 16);
   const int pairs = (c.heads - 1) / 2 + 1;  // of heads: a workgroup takes two at a time
   const int passes = (heads - 1) / per_pass + 1;
-  s.window = few ? 1 : kSlots8;
-  const int windows = (M - 1) / s.window + 1;
-  s.parts = few ? std::min(pairs, 65535) : std::min(pairs, std::max(1, 2048 / windows));
-  s.query_parts = few ? std::min(passes, 65535) : 1;
+  const int windows = (M - 1) / kSlots8 + 1;
+  const long long items = (long long)std::min(M, kSlots8) * pairs;  // of a window, at most
+  s.parts = std::max({1, std::min(pairs, 2048 / windows), (int)std::min<long long>(items, 512 / windows)});
+  s.query_parts = M < 768 ? std::min(passes, 65535) : 1;  // few tokens: as below
   const long long blocks = (long long)windows * s.parts;
   s.block_groups = (int)std::min<long long>(blocks, INT32_MAX);
   s.grid = blocks + (long long)M * s.query_parts;
@@ -510,7 +521,7 @@ hipError_t append(const RopeArgs& a, const KvView& c, hipStream_t stream) {
   if (c.format == kCacheFp8) {
     const Append8 s = append8_sizes(a.M, a.heads, c);
     rope_kv_append8_kernel<D><<<(unsigned)s.grid, kThreads, 0, stream>>>(
-        a, c, s.window, s.parts, s.block_groups, s.query_parts);
+        a, c, s.parts, s.block_groups, s.query_parts);
     return hipGetLastError();
   }
   const int passes = (a.heads + 2 * c.heads + per_pass - 1) / per_pass;

@@ -117,11 +117,12 @@ def test_append(D, heads, hk, page, R, inter):
         _check(cache, before, rows, (k, v))
 
 
-@pytest.mark.parametrize("M,B", [(768, 768), (900, 5), (1601, 97)])
-def test_append_many(M, B):
-    """From 768 tokens on, where workgroups look for runs in windows of 16 rows."""
+@pytest.mark.parametrize("M,B,hk", [(768, 768, 3), (900, 5, 3), (1601, 97, 3), (600, 600, 1),
+                                    (1100, 1100, 9), (1100, 300, 9), (2300, 900, 5)])
+def test_append_many(M, B, hk):
+    """Many windows of 16 rows, whose runs and heads are shared out among as many workgroups or fewer."""
     gen = torch.Generator().manual_seed(M)
-    D, hk, heads, page, cap = 64, 3, 4, 32, 416
+    D, heads, page, cap = 64, 2 * hk, 32, 416 if B < 900 else 64
     cache, _ = F.make_cache(gen, B, cap, hk, D, page)
     cuts = torch.randperm(M - 1, generator=gen)[:B - 1].sort()[0] + 1
     counts = torch.diff(torch.cat([torch.tensor([0]), cuts, torch.tensor([M])])).tolist()
