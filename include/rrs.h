@@ -712,10 +712,11 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
  * RRS_KV_INT4 rows stand for fp16(q s), as rrs_kv_read gives them (of a scale of 9360 for 9352 q). Logits,
  * softmax and sums in float32; for the product with V the weights are rounded to float16 in units of their own:
  * off by 2^-11 relative, or by 2^-37 of the row's largest one where that is more. Results repeat bit for bit
- * for the same arguments; they depend on other sequences through max_tokens and max_length only, which
- * decide where sums are cut. max_tokens * heads / kv_heads < 2^31 - 256; with r = sequences * kv_heads
- * and t = max_tokens * heads / kv_heads / 128 rounded up, r t (times the pieces that the slots are cut
- * into) < 2^24 workgroups.
+ * for the same arguments; they depend on other sequences through their lengths and rows, max_tokens and
+ * max_length only, which decide where sums are cut. max_tokens * heads / kv_heads < 2^31 - 256; with r =
+ * sequences * kv_heads and t = max_tokens * heads / kv_heads / 128 rounded up, r t (times the pieces that the
+ * slots are cut into) < 2^24 workgroups; with up to 128 max_tokens * heads / kv_heads, if sequences are cut,
+ * r * max_tokens * heads / kv_heads < 2^24.
  */
 size_t rrs_prompt_attention_workspace_bytes(const rrs_kv_cache* cache, int heads, int max_tokens,
                                             int max_length);

@@ -1,4 +1,4 @@
-// Attention of one new token per sequence over its paged cache. gfx950 only.
+// Attention of one new token per sequence over its paged cache, or of a few. gfx950 only.
 //
 // For a sequence and a KV head, up to 16 of the query heads that share it are the columns of the
 // matrix products. A wave takes tiles of slots (32 float16 or FP8, 64 INT4), with
@@ -40,6 +40,10 @@
 // us (latency); 179 x 64 heads of up to 5 slots 14 us. FP8: 64 sequences of 1 to 8192 slots, 8 KV heads of 128, 100 to
 // 105 us (5.0 to 5.2 TB/s: pieces of different sizes), one of 131071 with a mask 51 to 54 (5.0 to 5.2; a piece is 11
 // steps, of which the first waits for its loads), one of 213 with 32 heads 5.8.
+//
+// Of a few tokens (kTokens) every one has its columns, and a limit to the slots that it sees: that costs a comparison in
+// the last tiles only. 32 sequences of 4 tokens after up to 6000, 32 / 8 heads of 128, FP8, 48 us (3.7 TB/s with the
+// join), INT4 40, 9 of up to 7 after up to 1501, 20 / 5 heads of 64, float16, 13.7.
 #include <type_traits>
 
 #include "rrs_device.h"
@@ -87,6 +91,36 @@ struct Plan {
   bool adds_weights;  // the first launch adds the weights: whole sequences, one row block
 };
 
+// A few new tokens per sequence: the columns are theirs and the heads', token by token, each of which sees one
+// slot more than those of the token before. `heads` and Plan::group count the columns of all max_tokens; row_start
+// and M name the tokens' rows of Q.
+struct TokenArgs : AttentionArgs {
+  const int32_t* row_start;
+  int M, max_tokens;
+  int per_token;  // query heads per KV head
+  int of_model;   // query heads
+};
+template <bool kTokens>
+using Args = std::conditional_t<kTokens, TokenArgs, AttentionArgs>;
+
+// The rows of sequence b's tokens.
+__device__ __forceinline__ int2 tokens_of(const TokenArgs& a, int b) {
+  const int start = min(max(a.row_start[b], 0), a.M);
+  const int end = min(max(a.row_start[b + 1], start), a.M);
+  return make_int2(start, min(end - start, a.max_tokens));
+}
+// Its length; 0 where it has no tokens.
+__device__ __forceinline__ int length_of(const AttentionArgs& a, int b) {
+  return min(max(a.lengths[b], 0), a.max_length);
+}
+__device__ __forceinline__ int length_of(const TokenArgs& a, int b) {
+  return tokens_of(a, b).y > 0 ? min(max(a.lengths[b], 0), a.max_length) : 0;
+}
+// Column r of KV head hk as a row of Q; row0: the sequence's first.
+__device__ __forceinline__ size_t token_row(const TokenArgs& a, int row0, int hk, int r) {
+  return (size_t)(row0 + r / a.per_token) * a.of_model + hk * a.per_token + r % a.per_token;
+}
+
 // A piece of a sequence: slots [begin, end) of it, number `index` of all pieces, `count` of which
 // are the sequence's.
 struct Piece {
@@ -96,10 +130,11 @@ struct Piece {
 // Which piece `index` is; false past the last. Every wave of every workgroup works this out for
 // itself from the lengths, so that sequences of any lengths are cut into pieces of about the same
 // size without the host knowing them.
-__device__ __forceinline__ bool find_piece(const AttentionArgs& a, const KvView& c,
-                                           const Plan& plan, int index, Piece* out) {
+template <typename A>
+__device__ __forceinline__ bool find_piece(const A& a, const KvView& c, const Plan& plan,
+                                           int index, Piece* out) {
   const int lane = threadIdx.x & 63;
-  const auto length = [&](int b) { return min(max(a.lengths[b], 0), a.max_length); };
+  const auto length = [&](int b) { return length_of(a, b); };
   const auto all_steps = [&](int n) { return max(1, (n + plan.step - 1) / plan.step); };
   const auto steps_of = [&](int n) { return min(all_steps(n), 1 << 22); };  // sums fit an int
   int q = plan.steps, b = -1, first = 0;
@@ -236,6 +271,13 @@ __device__ __forceinline__ v8h eight_codes(uint32_t w) {
   const v2h c = two_codes<0>(w >> 8), d = two_codes<4>(w >> 8);
   return v8h{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// A scale of 9360, the largest there is, as the float16 below it: 7 times that is finite.
+__device__ __forceinline__ _Float16 below_9360(_Float16 s) {
+  return s == (_Float16)9360.0f ? (_Float16)9352.0f : s;
+}
+__device__ __forceinline__ _Float16 below_9360(uint32_t half) {
+  return below_9360(__builtin_bit_cast(_Float16, (uint16_t)half));
+}
 __device__ __forceinline__ int code_order(int e) { return (e >> 1) + 4 * (e & 1); }
 
 // Eight e4m3 codes as float16 in units of powers of two, one for each four: exact (rrs_kv.h).
@@ -266,6 +308,15 @@ __device__ __forceinline__ V mask_halves(V x, const bool* live) {
   for (int i = 0; i < kDwords; ++i)
     w[i] &= (live[2 * i] ? 0xFFFFu : 0u) | (live[2 * i + 1] ? 0xFFFF0000u : 0u);
   return __builtin_bit_cast(V, w);
+}
+
+// All ones in place of numbers that are not finite: halves, or e4m3 codes.
+template <bool kFp8>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  if constexpr (kFp8)
+    return (((w & 0x7F7F7F7Fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xFFu;
+  else
+    return (((w & 0x7C007C00u) + 0x04000400u) >> 15 & 0x00010001u) * 0xFFFFu;
 }
 
 // NaN if one of them is (the column's result is NaN then, whatever its maximum): two of these are one
@@ -358,11 +409,15 @@ __device__ __forceinline__ float2 weight_row(float top, float total) {
 // Grid: pieces x KV heads x row blocks. The row blocks of a piece and head read the same rows: they
 // are 8 apart, on one XCD, and share its L2.
 // kTeam: waves that share a piece; 1: every wave takes a whole sequence by itself.
-template <int D, int kFormat, bool kMask, int kTeam>
+// kTokens: columns of several tokens. The values of slots that not all of them see may be numbers that are not finite,
+// and 0 times those is NaN: they are 0 in LDS, and added at the end to the columns that do see them.
+template <int D, int kFormat, bool kMask, int kTeam, bool kTokens>
 __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd))
-    attention_kernel(AttentionArgs a, KvView c, Plan plan) {
+    attention_kernel(Args<kTokens> a, KvView c, Plan plan) {
   using S = Shape<D, kFormat, kTeam>;
   constexpr bool kInt4 = S::kInt4, kFp8 = S::kFp8;
+  // INT4: products that carry the values' scales, in units of their own; of tokens the operands are fp16(q s).
+  constexpr bool kUnits = kInt4 && !kTokens;
   constexpr int kLds = kTeam == 1 ? S::kValues : S::kLds;
   __shared__ __attribute__((aligned(16))) uint8_t lds[kWaves * kLds];
   __shared__ float2 wave_stats[kTeam][kRows], row_stats[kWaves / kTeam][kRows];
@@ -388,9 +443,22 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
     plan.of_seq[b] = make_int2(piece.first, piece.count);
 
   // Queries as the second operand: column col, channels as the keys' lanes hold them.
-  const int rows = min(plan.group - rb * kRows, kRows);
+  int rows = min(plan.group - rb * kRows, kRows);
   const int head0 = hk * plan.group + rb * kRows;
-  const uint16_t* qrow = a.Q + ((size_t)b * a.heads + head0 + min(col, rows - 1)) * D;
+  size_t qat = (size_t)b * a.heads + head0;
+  int row0 = 0, all_see = n, seen = n;  // slots that all columns see, and that this lane's does
+  if constexpr (kTokens) {
+    const int2 tokens = tokens_of(a, b);
+    rows = min(tokens.y * a.per_token - rb * kRows, kRows);
+    if (rows <= 0) return;
+    row0 = tokens.x;
+    all_see = n - tokens.y + 1 + rb * kRows / a.per_token;
+    seen = n - tokens.y + 1 + (rb * kRows + min(col, rows - 1)) / a.per_token;
+    qat = token_row(a, row0, hk, rb * kRows + min(col, rows - 1));
+  } else {
+    qat += min(col, rows - 1);
+  }
+  const uint16_t* qrow = a.Q + qat * D;
   v8h q[S::kSteps];
 #pragma unroll
   for (int i = 0; i < S::kSteps; ++i) {
@@ -466,7 +534,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
           key[u][i] = load_at<v4u>(p + i * (kInt4 ? 16 : 64), key_at);
       }
       if constexpr (kInt4) {  // four slots: 8 bytes, inside the page
-        ks[u] = load_at<v2u>(c.k_scale + row[u], 8 * quarter);
+        if constexpr (kUnits)
+          ks[u] = load_at<v2u>(c.k_scale + row[u], 8 * quarter);
+        else  // the lane's key's
+          ks[u][0] = load_at<uint16_t>(c.k_scale + row[u], 2 * col);
         vs[u] = load_at<v2u>(c.v_scale + row[u], 8 * quarter);
       }
       if constexpr (kFp8) {
@@ -496,6 +567,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
       }
   };
 
+  uint32_t found = 0;  // kTokens: values that are not finite
   int t0 = begin + (kTeam == 1 ? 0 : wave * S::kTile);
   if (t0 < end) {
     load_pages(t0 >> c.log_page);
@@ -517,8 +589,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
 #pragma unroll
       for (int i = 0; i < S::kSteps; ++i) {
         v8h k;
-        if constexpr (kInt4)
+        if constexpr (kUnits)
           k = eight_codes(key[u][i / 4][i % 4]);
+        else if constexpr (kInt4)
+          k = eight_codes(key[u][i / 4][i % 4]) * below_9360(ks[u][0]);
         else if constexpr (kFp8)
           k = eight_fp8(key[u][i / 2][2 * (i & 1)], key[u][i / 2][2 * (i & 1) + 1], key_unit[u],
                         key_unit[u]);
@@ -528,7 +602,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
       }
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        if constexpr (kInt4)
+        if constexpr (kUnits)
           l[u][r] = __builtin_fmaf(
               s[r], (float)__builtin_bit_cast(v2h, (uint32_t)ks[u][r / 2])[r & 1], 0.0f);
         else
@@ -541,23 +615,38 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
     }
     // Slots that take no part: a logit of -inf, a value scale of 0 (whatever was there).
     bool live[S::kBlocks * 4];
-    if (kMask || t0 + S::kTile > end) {
+    if (kMask || t0 + S::kTile > end || (kTokens && t0 + S::kTile > all_see)) {
       uint64_t in_tile = end - t0 >= 64 ? ~0ull : (1ull << (end - t0)) - 1;  // bit: slot t0 + it
       if constexpr (kMask) in_tile &= __ballot(mask != 0);
       const uint64_t mine = in_tile >> (4 * quarter);
+      const int upto = kTokens ? seen - t0 - 4 * quarter : 64;  // the column's slots of the tile
 #pragma unroll
       for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const bool in = mine >> (16 * u + r) & 1;
           live[4 * u + r] = in;
-          l[u][r] = in ? l[u][r] : -INFINITY;
+          l[u][r] = in && (!kTokens || 16 * u + r < upto) ? l[u][r] : -INFINITY;
         }
       if constexpr (kInt4) {
 #pragma unroll
         for (int u = 0; u < S::kBlocks / 2; ++u)
           vscale[u] = mask_halves(vscale[u], &live[8 * u]);
       }
+    }
+    if constexpr (kInt4 && kTokens) {
+#pragma unroll
+      for (int u = 0; u < S::kBlocks / 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (t0 + S::kTile > all_see) {
+            const uint32_t bad = not_finite<false>(vscale[u][e]);
+            vscale[u][e] &= ~bad;
+            found |= bad;
+          }
+          const v2h s = __builtin_bit_cast(v2h, (uint32_t)vscale[u][e]);
+          vscale[u][e] = __builtin_bit_cast(uint32_t, v2h{below_9360(s[0]), below_9360(s[1])});
+        }
     }
     if (logits) {
 #pragma unroll
@@ -574,10 +663,10 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
     for (int u = 0; u < S::kBlocks; ++u)
       top = larger(larger(larger(larger(top, l[u][0]), l[u][1]), l[u][2]), l[u][3]);
     bool fresh = false;  // INT4: m is to be set from the products
-    if (__any(top * scale > m + (kInt4 ? kFar : kRoom))) {
+    if (__any(top * scale > m + (kUnits ? kFar : kRoom))) {
       top = column_max(top) * scale;
       float up = fmaxf(m, top - kLift);
-      if constexpr (kInt4) {
+      if constexpr (kUnits) {
         fresh = top > m + kFar;
         up = fresh ? top : m;
       }
@@ -597,7 +686,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
       for (int r = 0; r < 4; ++r) {
         const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(l[u][r], scale, -base));
         sum += x;
-        if constexpr (kInt4) {  // as a mixed fma, which takes the float16 factor as it is
+        if constexpr (kUnits) {  // as a mixed fma, which takes the float16 factor as it is
           l[u][r] = __builtin_fmaf(
               x, (float)__builtin_bit_cast(v8h, vscale[u / 2])[4 * (u & 1) + r], 0.0f);
           most = larger(most, l[u][r]);
@@ -605,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
           p[4 * u + r] = (_Float16)x;
         }
       }
-    if constexpr (kInt4) {
+    if constexpr (kUnits) {
       if (__any(fresh || most > 0x1p15f)) {
         const float all = column_max(most);
         int e = 0;
@@ -627,7 +716,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
         for (int r = 0; r < 4; ++r) p[4 * u + r] = (_Float16)l[u][r];
     }
 
-    if constexpr (!kInt4) {
+    if constexpr (!kUnits) {
 #pragma unroll
       for (int i = 0; i < S::kBlocks * 2; ++i)
         rounded = __builtin_amdgcn_fdot2(v2h{p[2 * i], p[2 * i + 1]},
@@ -654,6 +743,19 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
         for (int i = 0; i < S::kPieces; ++i)
           if (t0 + 16 * u + i * kRowsPerLoad + lane / kPerRow >= end) val[u][i] = v4u{};
     }
+    if constexpr (kTokens && !kInt4)
+      if (t0 + S::kTile > all_see) {
+#pragma unroll
+        for (int u = 0; u < S::kBlocks; ++u)
+#pragma unroll
+          for (int i = 0; i < S::kPieces; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t bad = not_finite<kFp8>(val[u][i][e]);
+              val[u][i][e] &= ~bad;
+              found |= bad;
+            }
+      }
 #pragma unroll
     for (int u = 0; u < S::kBlocks; ++u)
 #pragma unroll
@@ -681,7 +783,8 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
           o[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(
-              eight_codes((uint32_t)w[h]),
+              kUnits ? eight_codes((uint32_t)w[h])
+                     : eight_codes((uint32_t)w[h]) * __builtin_bit_cast(v8h, vscale[h]),
               v8h{p[8 * h], p[8 * h + 1], p[8 * h + 2], p[8 * h + 3], p[8 * h + 4], p[8 * h + 5],
                   p[8 * h + 6], p[8 * h + 7]},
               o[j], 0, 0, 0);
@@ -723,13 +826,38 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
     __builtin_amdgcn_wave_barrier();
   }
 
+  if constexpr (kTokens)
+    if (__any(found != 0)) {
+      // The wave's tiles that not all columns see.
+      for (int s = begin + wave * S::kTile; s < end; s += kTeam * S::kTile)
+        for (int t = s; s + S::kTile > all_see && t < min(s + S::kTile, end); ++t) {
+          if (t >= seen || (kMask && !a.mask[(size_t)b * c.capacity() + t])) continue;
+          const size_t at = c.row_of(b, hk, t);
+          const uint8_t* value = c.v + at * S::kRow;
+          float all_of_row = 0.0f;  // INT4: a scale that is not finite
+          if constexpr (kInt4) all_of_row = half_to_float(c.v_scale[at]) * 0.0f;
+#pragma unroll
+          for (int j = 0; j < S::kOut; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int d = 16 * j + 4 * quarter + r;
+              float x = all_of_row;
+              if constexpr (kFp8)
+                x = (value[d] & 127) == 127 ? NAN : 0.0f;
+              else if constexpr (!kInt4)
+                x = half_to_float(reinterpret_cast<const uint16_t*>(value)[d]);
+              if (!(fabsf(x) < INFINITY)) o[j][r] += x;
+            }
+        }
+    }
+
   // The waves' sums meet in LDS. Float16 values: o is put in proportion to sum from the sum of the
   // rounded p, so that what rounding did to a weight it also did to the sum that divides it (one
   // weight that outgrows all others is then exact).
   sum += __shfl_xor(sum, 16);
   sum += __shfl_xor(sum, 32);
   float unit_o = 1.0f;
-  if constexpr (!kInt4) {
+  if constexpr (!kUnits) {
     rounded += __shfl_xor(rounded, 16);
     rounded += __shfl_xor(rounded, 32);
     unit_o = rounded != 0.0f ? sum / rounded : 0.0f;
@@ -778,8 +906,14 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
     *reinterpret_cast<v4f*>(mine + col * S::kLdO + 16 * j + 4 * quarter) = o[j] * unit_o;
   if (wave == 0 && quarter == 0)  // rows, for the weights
     row_stats[0][col] = weight_row(top, total);
+  const auto row_of = [&](int r) {  // of the output
+    if constexpr (kTokens)
+      return token_row(a, row0, hk, rb * kRows + r);
+    else
+      return (size_t)b * a.heads + head0 + r;
+  };
   if (threadIdx.x < rows) {
-    const size_t bh = (size_t)b * a.heads + head0 + threadIdx.x;
+    const size_t bh = row_of(threadIdx.x);
     if (whole && a.lse) a.lse[bh] = log_sum(top, total);
     if (plan.stats)
       plan.stats[(size_t)piece.index * a.heads + head0 + threadIdx.x] = make_float2(top, total);
@@ -792,7 +926,7 @@ __global__ void __launch_bounds__(kThreads, (Shape<D, kFormat, kTeam>::kPerSimd)
     for (int w = 0; w < kTeam; ++w)
       acc += *reinterpret_cast<const v4f*>(reinterpret_cast<const float*>(lds + w * kLds) +
                                            r * S::kLdO + d);
-    const size_t bh = (size_t)b * a.heads + head0 + r;
+    const size_t bh = row_of(r);
     if (whole)
       *reinterpret_cast<v4h*>(a.out + bh * D + d) =
           v4h{(_Float16)acc[0], (_Float16)acc[1], (_Float16)acc[2], (_Float16)acc[3]};
@@ -829,14 +963,20 @@ __device__ __forceinline__ float2 join_stats(const float2* stats, int count, int
 
 // The first `joins` workgroups join the pieces of one head each (of sequences of more than one
 // piece); the others turn the logits of 1024 slots of a (sequence, KV head) into weights.
-template <int D>
+template <int D, bool kTokens>
 __global__ void __launch_bounds__(kThreads)
-    attention_join_kernel(AttentionArgs a, KvView c, Plan plan, int joins, int weight_blocks) {
+    attention_join_kernel(Args<kTokens> a, KvView c, Plan plan, int joins, int weight_blocks) {
   constexpr int kParts = kThreads / (D / 4);  // pieces read at a time, 4 channels per thread
   __shared__ float4 acc_of[kThreads];
   __shared__ float2 of_row[kThreads];
   if ((int)blockIdx.x < joins) {
-    const int bh = blockIdx.x, b = bh / a.heads, h = bh % a.heads;
+    const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
+    size_t bh = blockIdx.x;  // row of the output
+    if constexpr (kTokens) {
+      const int2 tokens = tokens_of(a, b);
+      if (h % plan.group >= tokens.y * a.per_token) return;
+      bh = token_row(a, tokens.x, h / plan.group, h % plan.group);
+    }
     const int2 at = plan.of_seq[b];  // first piece, pieces
     if (at.y == 1) return;
     const float2* stats = plan.stats + (size_t)at.x * a.heads + h;
@@ -885,7 +1025,7 @@ __global__ void __launch_bounds__(kThreads)
     v4h y;
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = (_Float16)(some ? v[i] / all.y : 0.0f);
-    *reinterpret_cast<v4h*>(a.out + (size_t)bh * D + 4 * d4) = y;
+    *reinterpret_cast<v4h*>(a.out + bh * D + 4 * d4) = y;
     if (d4 == 0 && a.lse) a.lse[bh] = log_sum(all.x, all.y);
     return;
   }
@@ -1016,27 +1156,50 @@ Second second_grid(const Plan& p, const KvView& c, int heads, int max_length, bo
 template <int N>
 using Int = std::integral_constant<int, N>;
 
-template <int D>
-hipError_t launch(const AttentionArgs& a, const KvView& c, const Plan& p, hipStream_t stream) {
+template <int D, bool kTokens>
+hipError_t launch(const Args<kTokens>& a, const KvView& c, const Plan& p, hipStream_t stream) {
   const long long grid = first_grid(p, c, a.max_length);
   const auto run = [&](auto kernel) { kernel<<<(unsigned)grid, kThreads, 0, stream>>>(a, c, p); };
   const auto by_mask = [&](auto format, auto team) {
     constexpr int f = decltype(format)::value, n = decltype(team)::value;
-    a.mask ? run(attention_kernel<D, f, true, n>) : run(attention_kernel<D, f, false, n>);
+    a.mask ? run(attention_kernel<D, f, true, n, kTokens>)
+           : run(attention_kernel<D, f, false, n, kTokens>);
   };
   const auto by_team = [&](auto format) {
-    p.team == 1 ? by_mask(format, Int<1>()) : by_mask(format, Int<kWaves>());
+    if constexpr (!kTokens)
+      if (p.team == 1) return by_mask(format, Int<1>());
+    by_mask(format, Int<kWaves>());
   };
-  switch (c.format) {
-    case kCacheInt4: by_team(Int<kCacheInt4>()); break;
-    case kCacheFp8: by_team(Int<kCacheFp8>()); break;
-    default: by_team(Int<kCacheF16>());
+  if (c.format == kCacheFp8) {
+    by_team(Int<kCacheFp8>());
+  } else if (c.format == kCacheInt4) {
+    by_team(Int<kCacheInt4>());
+  } else {
+    by_team(Int<kCacheF16>());
   }
   if (hipError_t e = hipGetLastError()) return e;
   const Second s = second_grid(p, c, a.heads, a.max_length, a.weights != nullptr);
   if (s.grid > 0)
-    attention_join_kernel<D><<<(unsigned)s.grid, kThreads, 0, stream>>>(a, c, p, s.joins, s.blocks);
+    attention_join_kernel<D, kTokens>
+        <<<(unsigned)s.grid, kThreads, 0, stream>>>(a, c, p, s.joins, s.blocks);
   return hipGetLastError();
+}
+
+template <bool kTokens>
+hipError_t launch_dim(const Args<kTokens>& a, const KvView& c, const Plan& p, hipStream_t stream) {
+  switch (c.dim) {
+    case 64: return launch<64, kTokens>(a, c, p, stream);
+    case 128: return launch<128, kTokens>(a, c, p, stream);
+    default: return launch<256, kTokens>(a, c, p, stream);
+  }
+}
+
+// A few tokens: as many heads as columns.
+Plan make_tokens_plan(const KvView& c, int heads, int max_tokens, int max_length, void* workspace,
+                      size_t* bytes) {
+  Plan p = make_plan(c, heads * max_tokens, max_length, false, workspace, bytes);
+  p.team = kWaves;
+  return p;
 }
 
 }  // namespace
@@ -1057,11 +1220,57 @@ size_t attention_workspace_bytes(const KvView& c, int heads, int max_length, boo
 hipError_t launch_paged_attention(const AttentionArgs& a, const KvView& c, hipStream_t stream) {
   size_t bytes;
   const Plan p = make_plan(c, a.heads, a.max_length, a.weights != nullptr, a.workspace, &bytes);
-  switch (c.dim) {
-    case 64: return launch<64>(a, c, p, stream);
-    case 128: return launch<128>(a, c, p, stream);
-    default: return launch<256>(a, c, p, stream);
-  }
+  return launch_dim<false>(a, c, p, stream);
+}
+
+// Up to 16 columns are read as fast as one token's (32 sequences of 4 tokens after 6000, 32 / 8 heads of 128, FP8,
+// 85 -> 48 us, float16 106 -> 85; 16 of 16 after 3000, 32 / 32 heads, FP8, 79 -> 59). More are several row blocks, whose
+// rows are read by each: taken where the slots that they read are few (4 of 16 tokens after 300, 32 / 8 heads, float16, 14.2
+// -> 8.6 us, after 3000 25.2 -> 24.4; 8 of 16 28.0 and 31.8, one of 32 after 16000 37 and 49), and two blocks also where a
+// row is a short read or its tile for many rows a small one (32 of 8 after 6000, FP8 90 -> 81, INT4 91 -> 77; head dim 256, 8 of 16 after
+// 3000, 16 / 16 heads, 89 -> 65; but 32 of 32 alone, 16 / 16 heads, whose blocks are more than run at a time, 9.2 and 11.3).
+bool few_tokens(const KvView& c, int heads, int max_tokens, int max_length) {
+  const long long columns = (long long)max_tokens * (heads / c.heads);
+  if (columns > 128) return false;
+  const long long blocks = (columns - 1) / kRows + 1;
+  if (blocks == 1) return true;
+  const long long units = blocks * c.sequences * c.heads;
+  if (units > 768) return false;
+  return units * max_length <= 3 << 17 || (blocks == 2 && (c.format != kCacheF16 || c.dim == 256));
+}
+
+bool few_tokens_fits(const KvView& c, int heads, int max_tokens, int max_length) {
+  size_t bytes;
+  const Plan p = make_tokens_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
+  return fits_grid(first_grid(p, c, max_length), kThreads) &&
+         fits_grid(second_grid(p, c, heads * max_tokens, max_length, false).grid, kThreads);
+}
+
+size_t few_tokens_workspace_bytes(const KvView& c, int heads, int max_tokens, int max_length) {
+  size_t bytes;
+  make_tokens_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
+  return bytes;
+}
+
+hipError_t launch_few_tokens(const PromptArgs& a, const KvView& c, void* workspace,
+                             hipStream_t stream) {
+  size_t bytes;
+  const Plan p = make_tokens_plan(c, a.heads, a.max_tokens, a.max_length, workspace, &bytes);
+  TokenArgs x{};
+  x.Q = a.Q;
+  x.heads = a.heads * a.max_tokens;
+  x.lengths = a.lengths;
+  x.max_length = a.max_length;
+  x.scale = a.scale;
+  x.mask = a.mask;
+  x.out = a.out;
+  x.lse = a.lse;
+  x.row_start = a.row_start;
+  x.M = a.M;
+  x.max_tokens = a.max_tokens;
+  x.per_token = a.heads / c.heads;
+  x.of_model = a.heads;
+  return launch_dim<true>(x, c, p, stream);
 }
 
 }  // namespace rrs

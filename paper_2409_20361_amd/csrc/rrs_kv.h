@@ -118,6 +118,13 @@ size_t prompt_workspace_bytes(const KvView& c, int heads, int max_tokens, int ma
 hipError_t launch_prompt_attention(const PromptArgs& a, const KvView& c, void* workspace,
                                    hipStream_t stream);
 
+// The same for few tokens, by the attention of single ones.
+bool few_tokens(const KvView& c, int heads, int max_tokens, int max_length);
+bool few_tokens_fits(const KvView& c, int heads, int max_tokens, int max_length);
+size_t few_tokens_workspace_bytes(const KvView& c, int heads, int max_tokens, int max_length);
+hipError_t launch_few_tokens(const PromptArgs& a, const KvView& c, void* workspace,
+                             hipStream_t stream);
+
 struct EvictArgs {
   const int32_t* lengths;
   int max_length;

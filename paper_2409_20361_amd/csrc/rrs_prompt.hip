@@ -22,7 +22,9 @@
 // Measured: that batch 900 us (950 TFLOP/s; a float16 product of 8192^3 in the library reaches 1210; without the
 // exponentials, or without the way to LDS, 7 and 12 % less); as float16 945 us; two of 8192 with 16 / 8
 // heads of 256 880 (670); 1024 tokens after 12288 in INT4 265 us (810). Small calls are a chain of
-// launch, rows, pages and tiles and a second launch: nine sequences of up to 7 tokens after 1501 16 us.
+// launch, rows, pages and tiles and a second launch: eight of 16 tokens after 3000, 32 / 8 heads of 128, 28 us. A
+// few tokens over a long cache leave most of the matrix instructions' columns empty and are bound by HBM:
+// they go to the kernel of single tokens (few_tokens).
 //
 // Where the rows do not fill the card, the slots are cut into pieces, joined by a second kernel in order.
 //
@@ -700,7 +702,7 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
   p.pieces = (int)std::min(most, std::max(1ll, resident / units));
   // With a workgroup on every CU already, a second one and the join pay from some 20 steps on (32 / 8 heads:
-  // 1024 tokens 39 us in two pieces, 34 in one, 32 x 4 after up to 700 26 and 22, after up to 2000 38 and 48).
+  // 1024 tokens 39 us in two pieces, 34 in one, 32 x 30 after up to 700 34 and 28, after up to 2000 51 and 54).
   if (units >= 256 && max_length < 1280) p.pieces = 1;
   const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * p.rows : 0;
   const size_t stats = align256(rows * sizeof(float2));
@@ -747,12 +749,16 @@ hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream
 bool prompt_fits(const KvView& c, int heads, int max_tokens, int max_length) {
   // Rows of a sequence and KV head are numbered in 31 bits.
   if ((long long)max_tokens * (heads / c.heads) >= (1ll << 31) - 256) return false;
+  if (few_tokens(c, heads, max_tokens, max_length))
+    return few_tokens_fits(c, heads, max_tokens, max_length);
   size_t bytes;
   const Plan p = make_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
   return fits_grid(first_grid(p), 64 * p.waves) && fits_grid(second_grid(p, c.dim), kJoinThreads);
 }
 
 size_t prompt_workspace_bytes(const KvView& c, int heads, int max_tokens, int max_length) {
+  if (few_tokens(c, heads, max_tokens, max_length))
+    return few_tokens_workspace_bytes(c, heads, max_tokens, max_length);
   size_t bytes;
   make_plan(c, heads, max_tokens, max_length, nullptr, &bytes);
   return bytes;
@@ -760,6 +766,8 @@ size_t prompt_workspace_bytes(const KvView& c, int heads, int max_tokens, int ma
 
 hipError_t launch_prompt_attention(const PromptArgs& a, const KvView& c, void* workspace,
                                    hipStream_t stream) {
+  if (few_tokens(c, a.heads, a.max_tokens, a.max_length))
+    return launch_few_tokens(a, c, workspace, stream);
   size_t bytes;
   const Plan p = make_plan(c, a.heads, a.max_tokens, a.max_length, workspace, &bytes);
   switch (c.dim) {

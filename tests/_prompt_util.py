@@ -38,6 +38,11 @@ def attention(Q, plain, rows, lengths, scale, mask=None):
         if n == 0:
             res.append(None)
             continue
+        if L == 0:   # tokens that see nothing
+            o, l = torch.zeros((n, H, D)).double(), torch.full((n, H), -math.inf).double()
+            res.append({"o": o, "tol": o, "lse": l, "lse_tol": torch.zeros_like(l),
+                        "some": torch.zeros(n, dtype=torch.bool)})
+            continue
         k, v, _ = U.values(plain, b, L)
         hk = k.shape[0]
         q = Q[first:first + n].double().cpu().view(n, hk, H // hk, D).permute(1, 2, 0, 3)

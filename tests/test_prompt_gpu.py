@@ -88,6 +88,74 @@ def test_attention(D, heads, hk, page, seqs, mask, fmt):
     assert torch.equal(again[at], out[at])
 
 
+FEW = [
+    # D, heads, hk, page, [(new, length)], mask: up to 16 columns; more, whose blocks cut tokens in two; one
+    # sequence or more than 256; lengths of one tile, of several pieces, of one sequence only
+    (128, 32, 8, 64, [(4, 2000 + 37 * i) for i in range(8)], False),
+    (128, 8, 2, 16, [(i % 5, 30 + i) for i in range(300)], True),
+    (256, 8, 1, 32, [(4, 900), (0, 700), (2, 3), (1, 1)], True),
+    (64, 6, 2, 16, [(33, 1200), (1, 40), (7, 5), (33, 33)], False),
+    (128, 5, 5, 128, [(16, 5000)], True), (128, 40, 1, 64, [(3, 777), (2, 1)], False),
+    (64, 1, 1, 16, [(16, 16), (16, 0), (16, 17), (15, 4000)], False),
+    (128, 10, 10, 32, [(128, 900)], True), (256, 4, 4, 16, [(16, 16)] * 60, False),
+]
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4", "fp8"])
+@pytest.mark.parametrize("D,heads,hk,page,seqs,mask", FEW)
+def test_few_tokens(D, heads, hk, page, seqs, mask, fmt):
+    test_attention(D, heads, hk, page, seqs, mask, fmt)
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4", "fp8"])
+@pytest.mark.parametrize("mask", [False, True])
+@pytest.mark.parametrize("D,hk,group,n,L", [(128, 2, 4, 4, 70), (64, 1, 3, 5, 3000),
+                                            (256, 3, 2, 16, 129), (128, 1, 5, 11, 11)])
+def test_few_tokens_not_finite(D, hk, group, n, L, mask, fmt):
+    """Values that are not finite among the new tokens and before them, in slots that later tokens see, or nobody."""
+    gen = torch.Generator().manual_seed(D + L)
+    page = 16
+    cache, plain = R.make_cache(gen, 1, L, hk, D, page, fmt)
+    plain = rrs.KVCache(plain.k.clone(), plain.v.clone(), plain.table)
+    bad = [(L - 1, 2, math.nan), (L - n // 2, 40, math.inf), (L - n + 1, 5, -math.inf),
+           (max(L - n - 3, 0), 7, math.nan), (max(L - n - 2, 0), 60, math.inf)]
+    m = None
+    if mask:
+        m = (torch.rand((1, cache.capacity), generator=gen) < 0.7).cuda()
+        m[0, L - n + 1], m[0, L - 1] = False, True
+    for i, (t, d, what) in enumerate(bad):
+        p, at, h = int(cache.table[0, t // page]), t % page, i % hk
+        if fmt == "f16":
+            cache.v[p, h, at, d] = what
+            plain.v[p, h, at, d] = what
+        elif fmt == "int4":
+            cache.v_scale[p, h, at] = what
+            plain.v[p, h, at] = math.nan
+        else:
+            cache.v.view(torch.uint8)[p, h, at, d] = 127
+            plain.v[p, h, at, d] = math.nan
+    starts, rows = _starts([n])
+    Q = torch.randn((n, group * hk, D), generator=gen).half().cuda()
+    out, lse = rrs.prompt_attention(Q, cache, _int(starts), _int([L]), mask=m, return_lse=True)
+    R.check(out, lse, R.attention(Q, plain, rows, [L], D ** -0.5, m), rows)
+    # A key: NaN for the tokens that see it, for the others what was there.
+    t = L - 2
+    p, at = int(cache.table[0, t // page]), t % page
+    if m is not None:
+        m[0, t] = True
+        out, lse = rrs.prompt_attention(Q, cache, _int(starts), _int([L]), mask=m, return_lse=True)
+    if fmt == "f16":
+        cache.k[p, 0, at, 3] = math.nan
+    elif fmt == "int4":
+        cache.k_scale[p, 0, at] = math.nan
+    else:
+        cache.k.view(torch.uint8)[p, 0, at, 3] = 255
+    new, new_lse = rrs.prompt_attention(Q, cache, _int(starts), _int([L]), mask=m, return_lse=True)
+    assert bool(new[n - 2:, :group].isnan().all()) and bool(new_lse[n - 2:, :group].isnan().all())
+    R.check(new[:n - 2], new_lse[:n - 2],
+            R.attention(Q[:n - 2], plain, [(0, n - 2)], [L - 2], D ** -0.5, m), [(0, n - 2)])
+
+
 @pytest.mark.parametrize("fmt", ["f16", "int4", "fp8"])
 @pytest.mark.parametrize("scale", [-0.3, 0.0, 2.0])
 def test_scale(scale, fmt):
@@ -98,6 +166,10 @@ def test_scale(scale, fmt):
     out, lse = rrs.prompt_attention(Q, cache, _int(starts), _int([200, 77]), scale=scale,
                                     return_lse=True)
     R.check(out, lse, R.attention(Q, plain, rows, [200, 77], scale), rows)
+    starts, rows = _starts([5, 3])
+    out, lse = rrs.prompt_attention(Q[:8], cache, _int(starts), _int([200, 77]), max_tokens=5,
+                                    scale=scale, return_lse=True)
+    R.check(out, lse, R.attention(Q[:8], plain, rows, [200, 77], scale), rows)
 
 
 def test_growing_logits():
@@ -199,7 +271,8 @@ def test_many_tokens():
 
 
 @pytest.mark.parametrize("mask", [False, True])
-def test_graph(mask):
+@pytest.mark.parametrize("bound", [60, 4])
+def test_graph(mask, bound):
     """Captured once, replayed over other queries, starts and lengths."""
     gen = torch.Generator().manual_seed(9)
     cache, _ = R.make_cache(gen, 3, 700, 2, 128, 16, "fp8")
@@ -208,7 +281,7 @@ def test_graph(mask):
     m = torch.ones((3, cache.capacity), dtype=torch.bool, device="cuda") if mask else None
 
     def call():
-        return rrs.prompt_attention(Q, cache, starts, n, max_tokens=60, max_length=700, mask=m,
+        return rrs.prompt_attention(Q, cache, starts, n, max_tokens=bound, max_length=700, mask=m,
                                     return_lse=True)
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
@@ -219,13 +292,14 @@ def test_graph(mask):
         got = call()
     for s, l in (([0, 60, 60, 60], [700, 3, 9]), ([0, 1, 30, 60], [5, 640, 33]),
                  ([0, 20, 40, 60], [20, 20, 20])):
+        s = [x * bound // 60 for x in s]
         Q.copy_(torch.randn(Q.shape, generator=gen))
         starts.copy_(_int(s)), n.copy_(_int(l))
         if mask:
             m.copy_(torch.rand(m.shape, generator=gen) < 0.5)
         graph.replay()
         for x, y in zip(got, call()):
-            assert torch.equal(x, y)
+            assert torch.equal(x[:s[3]], y[:s[3]])
         torch.cuda.synchronize()
 
 
