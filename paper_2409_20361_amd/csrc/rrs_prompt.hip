@@ -63,8 +63,9 @@ struct Tile {
   static constexpr int kSteps = D / 16;   // mfma steps of a logit
   static constexpr int kOut = D / 32;     // blocks of output channels
   static constexpr int kBytes = kSlots * D * 2;
-  // Loads: kWidth bytes per thread (16, or what gives every wave something), kLanes threads to a row. The rows that a wave loads at a time, at most
-  // 16, lie in one block of 16 slots: their page and address are the wave's.
+  // Loads: kWidth bytes per thread (16, or what gives every wave something), kLanes threads to a row. The
+  // rows that a wave loads at a time, at most 16, lie in one block of 16 slots: their page and address are
+  // the wave's.
   static constexpr int kRow = kFormat == kCacheInt4 ? D / 2 : kFormat == kCacheFp8 ? D : 2 * D;
   static constexpr int kLanes = kRow / 16 > kThreads / kSlots ? kRow / 16 : kThreads / kSlots;
   static constexpr int kWidth = kRow / kLanes;
@@ -664,10 +665,10 @@ int join_rows(int dim, int pieces) {
 }
 
 // At head dim 128 workgroups of eight waves bring each tile to LDS for twice as many rows, but are half as many.
-// They are taken for 1024 rows or more of one sequence behind at least as many cached tokens (32 / 8 heads: 1024 after 8000, INT4,
-// 206 -> 187 us, 512 after 8000, FP8, 106 -> 97; 2000 after 2000, 32 / 32 heads, float16, 163 -> 144; but 300 after 300, 32 / 32 heads, 26 against 31) and from so
-// many rows of all sequences and KV heads times slots on (4096 tokens of one sequence 188 -> 170, 8192 of four 937
-// -> 891); not for less without a past (2048 of one 66 against 72, 512 of four after up to 4000 120 against 129).
+// They are taken for 1024 rows or more of one sequence behind at least as many cached tokens (32 / 8 heads:
+// 1024 after 8000, INT4, 206 -> 187 us, 512 after 8000, FP8, 106 -> 97; 2000 after 2000, 32 / 32 heads, float16,
+// 163 -> 144; but 300 after 300, 32 / 32 heads, 26 against 31) and from so many rows of all sequences and KV heads
+// times slots on (4096 tokens of one sequence 188 -> 170, 8192 of four 937 -> 891); not for less without a past (2048 of one 66 against 72, 512 of four after up to 4000 120 against 129).
 constexpr long long kWide = 5ll << 26;
 bool eight_waves(const KvView& c, int heads, int max_tokens, int max_length) {
   if (c.dim != 128) return false;
