@@ -224,14 +224,16 @@ def test_not_finite(D, hk, pieces, fmt):
     assert torch.equal(new_lse[n - 30:, 2:], lse[n - 30:, 2:])
 
 
-def test_bad_numbers():
-    """Rows, counts and lengths out of range are cut; the rest is as without them."""
+@pytest.mark.parametrize("bound", [8, 99])
+def test_bad_numbers(bound):
+    """Rows, counts and lengths out of range are cut; the rest is as without them. Few columns and many."""
     gen = torch.Generator().manual_seed(6)
     cache, plain = R.make_cache(gen, 3, 64, 2, 128, 16, "f16")
-    Q = torch.randn((20, 4, 128), generator=gen).half().cuda()
+    M = 12 + bound
+    Q = torch.randn((M, 4, 128), generator=gen).half().cuda()
     # More tokens than slots: the first ones see nothing. A length past the bound. Rows past M.
-    out, lse = rrs.prompt_attention(Q, cache, _int([0, 8, 12, 99]), _int([5, 1000, -4]),
-                                    max_tokens=8, max_length=64, return_lse=True)
+    out, lse = rrs.prompt_attention(Q, cache, _int([0, 8, 12, M + 79]), _int([5, 1000, -4]),
+                                    max_tokens=bound, max_length=64, return_lse=True)
     R.check(out, lse, R.attention(Q, plain, [(0, 8), (8, 4)], [5, 64], 128 ** -0.5),
             [(0, 8), (8, 4)])
     assert not out[12:].any()
@@ -241,7 +243,8 @@ def test_bad_numbers():
     zero = cache.table.clone()
     zero[0, 1] = 0
     starts, n = _int([0, 20, 20, 20]), _int([50, 1, 1])
-    got, want = (rrs.prompt_attention(Q, cache._replace(table=t), starts, n) for t in (table, zero))
+    got, want = (rrs.prompt_attention(Q, cache._replace(table=t), starts, n,
+                                      max_tokens=max(bound, 20))[:20] for t in (table, zero))
     assert torch.equal(got, want)
 
 
