@@ -10,7 +10,8 @@
 //   O^T += V^T P^T values from LDS, transposed (ds_read_b64_tr), in the order of slots that the lane's p
 //                  have, so that P goes from one product's result into the other's operand.
 // p is rounded to float16 in units that leave a row's largest at 2^12 or more, as in the attention
-// of single tokens; sums are float32.
+// of single tokens, and divided by the sum of what it was rounded to, so that the weights of a row add up to 1
+// (of slots with equal values the output is that value); sums are float32.
 //
 // The matrix instructions bound it (4 D flops per row and slot), if the vector instructions (an exponential, a
 // product, a sum and a maximum per row and slot, and a part of each tile's way to LDS) run beside them.
@@ -97,7 +98,8 @@ struct Plan {
   int pairs;   // sequences x KV heads
   bool by_xcd;
   float* part;    // pairs x tiles x pieces x rows x D: sums relative to m; nullptr: one piece
-  float2* stats;  // the same without D: m (base 2) and the sum of p
+  float2* stats;  // the same without D: m (base 2) and the sum of p as float16
+  float* sums;    // the sum of p as float32: for lse
 };
 
 __device__ __forceinline__ float larger(float a, float b) {
@@ -182,7 +184,9 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, const KvView& c, 
   return (long long)w->tile * plan.rows < (long long)w->count * plan.group;
 }
 
-template <int D, int kFormat, bool kMask, int kWaves>
+// kLse: the logarithm of the sum is asked for, which takes the weights before they are rounded: a second sum (four
+// prompts of 8192 tokens, 32 / 8 heads of 128, FP8: 892 us without, 925 with it).
+template <int D, int kFormat, bool kMask, bool kLse, int kWaves>
 __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
                                   (Tile<D, kFormat, kWaves>::kPerSimd))
     prompt_kernel(PromptArgs a, KvView c, Plan plan) {
@@ -232,7 +236,9 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
   }
 
   v16f o[T::kOut] = {};
-  float m = -INFINITY, sum = 0.0f;
+  float m = -INFINITY;
+  float sum = 0.0f;    // of p as it goes into the product with V
+  float before = 0.0f;  // of p before it is rounded
 
   // A wave's part of a tile: in pass p rows kWaveRows (4 p + wave) ... of it, kLanes threads to each.
   const int my_row_of = lane / T::kLanes, my_lane = lane % T::kLanes;
@@ -423,6 +429,7 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
       const float shrink = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - up);
       m = up;
       sum *= shrink;
+      if constexpr (kLse) before *= shrink;
 #pragma unroll
       for (int j = 0; j < T::kOut; ++j) o[j] *= shrink;
     }
@@ -437,10 +444,14 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
     for (int i = 0; i < kAhead; ++i) ks[i] = key_of(buf, u, i);
     next = v16f{};
     const auto add = [&](int r) {  // of a pair
-      sum += x[r];
-      sum += x[r + 1];
-      p[r / 8][r % 8] = (_Float16)x[r];
-      p[r / 8][r % 8 + 1] = (_Float16)x[r + 1];
+      if constexpr (kLse) {
+        before += x[r];
+        before += x[r + 1];
+      }
+      const v2h two = {(_Float16)x[r], (_Float16)x[r + 1]};
+      p[r / 8][r % 8] = two[0];
+      p[r / 8][r % 8 + 1] = two[1];
+      sum = __builtin_amdgcn_fdot2(two, v2h{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
     };
 #pragma unroll
     for (int i = 0; i < T::kSteps; ++i) {
@@ -561,17 +572,20 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
         }
     }
 
-  {
-    const uint32_t u = __builtin_bit_cast(uint32_t, sum);
-    const auto x = __builtin_amdgcn_permlane32_swap(u, u, false, false);
-    sum = __builtin_bit_cast(float, (uint32_t)x[0]) + __builtin_bit_cast(float, (uint32_t)x[1]);
-  }
+  const auto both_lanes = [](float x) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const auto y = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    return __builtin_bit_cast(float, (uint32_t)y[0]) + __builtin_bit_cast(float, (uint32_t)y[1]);
+  };
+  sum = both_lanes(sum);
+  if constexpr (kLse) before = both_lanes(before);
   if (row0 + 32 * wave + col >= rows) return;
   if (plan.part) {
     const size_t unit =
         (((size_t)(at.b * c.heads + at.hk) * plan.tiles + at.tile) * plan.pieces + at.piece) *
             T::kRows + 32 * wave + col;
     if (half == 0) plan.stats[unit] = make_float2(m, sum);
+    if (kLse && half == 0) plan.sums[unit] = before;
     float* out = plan.part + unit * D;
 #pragma unroll
     for (int j = 0; j < T::kOut; ++j)
@@ -591,7 +605,7 @@ __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
       *reinterpret_cast<v4h*>(out + 32 * j + 2 * r + 4 * half) =
           v4h{(_Float16)(o[j][r] * inv), (_Float16)(o[j][r + 1] * inv),
               (_Float16)(o[j][r + 2] * inv), (_Float16)(o[j][r + 3] * inv)};
-  if (half == 0 && a.lse) a.lse[row] = log_sum(m, sum);
+  if (kLse && half == 0) a.lse[row] = log_sum(m, before);
 }
 
 // Pieces of a row joined: D / 4 threads to a row, or several groups of so many, which take the row's pieces in
@@ -602,6 +616,7 @@ __global__ void __launch_bounds__(kJoinThreads)
   constexpr int kLanes = D / 4, kGroups = kJoinThreads / (kLanes * kRowsAtOnce);
   __shared__ v4f sums[kGroups > 1 ? kJoinThreads : 1];
   __shared__ float2 stats[kGroups > 1 ? kGroups : 1][kRowsAtOnce];
+  __shared__ float befores[kGroups > 1 ? kGroups : 1][kRowsAtOnce];
   const int blocks = plan.rows / kRowsAtOnce, unit = blockIdx.x / blocks;
   const int pair = unit / plan.tiles, tile = unit % plan.tiles;
   const int b = pair / c.heads, hk = pair % c.heads;
@@ -613,7 +628,7 @@ __global__ void __launch_bounds__(kJoinThreads)
   const long long my_row = (long long)tile * plan.rows + r;
   const bool there = my_row < (long long)min(end - start, a.max_tokens) * plan.group;
   const size_t first = (size_t)unit * plan.pieces * plan.rows + r;
-  float top = -INFINITY, total = 0.0f;
+  float top = -INFINITY, total = 0.0f, before = 0.0f;
   v4f acc = {};
   if (there) {
 #pragma unroll 4
@@ -626,23 +641,28 @@ __global__ void __launch_bounds__(kJoinThreads)
       const float2 st = plan.stats[at];
       const float f = __builtin_amdgcn_exp2f(st.x - base);
       total += st.y * f;
+      if (a.lse) before += plan.sums[at] * f;
       acc += *reinterpret_cast<const v4f*>(plan.part + at * D + d) * f;
     }
   }
   if constexpr (kGroups > 1) {
     sums[threadIdx.x] = acc;
-    if (d == 0) stats[group][mine] = make_float2(top, total);
+    if (d == 0) {
+      stats[group][mine] = make_float2(top, total);
+      befores[group][mine] = before;
+    }
     __syncthreads();
     if (group > 0) return;
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) top = fmaxf(top, stats[g][mine].x);
     const float base = top == -INFINITY ? 0.0f : top;
-    total = 0.0f;
+    total = before = 0.0f;
     acc = v4f{};
 #pragma unroll
     for (int g = 0; g < kGroups; ++g) {
       const float f = __builtin_amdgcn_exp2f(stats[g][mine].x - base);
       total += stats[g][mine].y * f;
+      before += befores[g][mine] * f;
       acc += sums[g * kLanes * kRowsAtOnce + threadIdx.x] * f;
     }
   }
@@ -653,7 +673,7 @@ __global__ void __launch_bounds__(kJoinThreads)
   *reinterpret_cast<v4h*>(a.out + row * D + d) =
       v4h{(_Float16)(acc[0] * inv), (_Float16)(acc[1] * inv), (_Float16)(acc[2] * inv),
           (_Float16)(acc[3] * inv)};
-  if (d == 0 && a.lse) a.lse[row] = log_sum(top, total);
+  if (d == 0 && a.lse) a.lse[row] = log_sum(top, before);
 }
 
 // Rows of a workgroup of the join: up to eight pieces one after the other; more by eight groups of threads (head
@@ -706,11 +726,13 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   // 1024 tokens 39 us in two pieces, 34 in one, 32 x 30 after up to 700 34 and 28, after up to 2000 51 and 54).
   if (units >= 256 && max_length < 1280) p.pieces = 1;
   const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * p.rows : 0;
-  const size_t stats = align256(rows * sizeof(float2));
-  *bytes = stats + rows * c.dim * 4;
+  const size_t stats = align256(rows * sizeof(float2)), sums = align256(rows * sizeof(float));
+  *bytes = stats + sums + rows * c.dim * 4;
   if (workspace && rows) {
-    p.stats = static_cast<float2*>(workspace);
-    p.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + stats);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    p.stats = reinterpret_cast<float2*>(ws);
+    p.sums = reinterpret_cast<float*>(ws + stats);
+    p.part = reinterpret_cast<float*>(ws + stats + sums);
   }
   return p;
 }
@@ -721,12 +743,15 @@ hipError_t launch(const PromptArgs& a, const KvView& c, const Plan& p, hipStream
   const auto run = [&](auto format) {
     constexpr int f = decltype(format)::value;
     const auto go = [&](auto kernel) { kernel<<<grid, 64 * p.waves, 0, stream>>>(a, c, p); };
+    const auto by_mask = [&](auto lse, auto waves) {
+      constexpr bool kLse = decltype(lse)::value != 0;
+      constexpr int kWaves = decltype(waves)::value;
+      a.mask ? go(prompt_kernel<D, f, true, kLse, kWaves>)
+             : go(prompt_kernel<D, f, false, kLse, kWaves>);
+    };
     if constexpr (D == 128)
-      if (p.waves == 8) {
-        a.mask ? go(prompt_kernel<D, f, true, 8>) : go(prompt_kernel<D, f, false, 8>);
-        return;
-      }
-    a.mask ? go(prompt_kernel<D, f, true, 4>) : go(prompt_kernel<D, f, false, 4>);
+      if (p.waves == 8) return a.lse ? by_mask(Int<1>(), Int<8>()) : by_mask(Int<0>(), Int<8>());
+    a.lse ? by_mask(Int<1>(), Int<4>()) : by_mask(Int<0>(), Int<4>());
   };
   switch (c.format) {
     case kCacheInt4: run(Int<kCacheInt4>()); break;

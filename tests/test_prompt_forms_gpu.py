@@ -15,15 +15,15 @@ def _int(x):
 
 
 def _pieces(cache, heads, tokens, top, rows):
-    """Pieces that the slots are cut into: the workspace holds D sums and two numbers for each and every row of the
-    tiles of `rows` rows. Fails where the tiles are of another size, or the tokens few enough for another kernel."""
+    """Pieces that the slots are cut into: the workspace holds D sums and three numbers for each and every row of
+    the tiles of `rows` rows. Fails where the tiles are of another size, or the tokens few enough for another kernel."""
     B, hk, D = cache.table.shape[0], cache.k.shape[1], cache.k.shape[3]
     if cache.k.dtype == torch.uint8:
         D *= 2
     assert tokens * heads // hk > 128
     tiles = -(-tokens * heads // hk // rows)
     need = rrs.prompt_attention_workspace_bytes(cache, heads, tokens, top)
-    unit = B * hk * tiles * rows * (4 * D + 8)
+    unit = B * hk * tiles * rows * (4 * D + 12)
     assert need % unit == 0, (need, unit)
     return need // unit
 
@@ -100,3 +100,48 @@ def test_eight_waves_in_pieces(L, mask, fmt):
     assert torch.equal(out[:, 4:].view(torch.int16), before[:, 4:].view(torch.int16))
     assert torch.equal(lse[:, 4:], before_lse[:, 4:])
     assert bool(lse[:n - 30].isfinite().all())
+
+
+@pytest.mark.parametrize("fmt", ["f16", "int4", "fp8"])
+@pytest.mark.parametrize("D,n,group,L", [(64, 70, 2, 300), (128, 70, 2, 300), (128, 260, 4, 700), (256, 70, 2, 200),
+                                         (128, 7, 2, 300)])
+def test_equal_values(D, n, group, L, fmt):
+    """Slots that all hold the same value: the output is that value, whatever the weights and their rounding.
+
+    With float16 weights p the output is sum p v / sum p. Both sums are float32 over no more than L products that are
+    exact (11 bits each): with their rescaling each is off by at most 2 L 2^-24 relative, the quotient by
+    less than 2^-12 for L <= 700, which rounds to the float16 number v. Two slots count, the second with 4 to 8 times
+    the first's weight, in a later block: no weight but the first's is a power of two."""
+    page, slot = 64, 100
+    pages = -(-L // page)
+    table = torch.arange(pages, dtype=torch.int32, device="cuda").view(1, -1)
+    kind = {"f16": rrs.KV_F16, "int4": rrs.KV_INT4, "fp8": rrs.KV_FP8}[fmt]
+    cache = rrs.kv_cache(pages, 1, page, D, table, kind)
+    # Values of 2047 / 1024 (FP8: 15 / 8), whose half step is 2^-12 of them; keys of 0, but 1 at the slot.
+    for pool in (cache.k, cache.v):
+        pool.view(torch.uint8).zero_()
+    if fmt == "f16":
+        cache.v.fill_(2047 / 1024)
+        cache.k[slot // page, 0, slot % page, 0] = 1.0
+        v = 2047 / 1024
+    elif fmt == "int4":
+        cache.k_scale.fill_(1.0), cache.v_scale.fill_(2047 / 1024)
+        cache.v.fill_(0x11)
+        cache.k[slot // page, 0, slot % page, 0] = 1
+        v = 2047 / 1024
+    else:
+        cache.k_scale.fill_(1.0), cache.v_scale.fill_(1.0)
+        cache.v.view(torch.uint8).fill_(0x3F)
+        cache.k.view(torch.uint8)[slot // page, 0, slot % page, 0] = 0x38
+        v = 15 / 8
+    mask = torch.zeros((1, cache.capacity), dtype=torch.bool, device="cuda")
+    mask[0, 0] = mask[0, slot] = True
+    scale = 0.125
+    Q = torch.zeros((n, group, D), dtype=torch.float16, device="cuda")
+    Q[:, :, 0] = torch.linspace(2.0, 2.98, n * group).view(n, group).cuda() * math.log(2) / scale
+    for m in (mask, None):
+        out, lse = rrs.prompt_attention(Q, cache, _int([0, n]), _int([L]), max_length=L, scale=scale,
+                                        mask=m, return_lse=True)
+        assert bool((out == v).all()), (out.float() - v).abs().max().item()
+    out = rrs.prompt_attention(Q, cache, _int([0, n]), _int([L]), scale=scale, mask=mask)
+    assert bool((out == v).all())
