@@ -712,10 +712,12 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   Plan p{};
   p.group = heads / c.heads;
   p.pairs = c.sequences * c.heads;
-  p.by_xcd = p.pairs % 8 == 0 || p.pairs >= 64;
-  p.waves = eight_waves(c, heads, max_tokens, max_length) ? 8 : 4;
-  p.rows = 32 * p.waves;
-  p.tiles = (int)(((long long)max_tokens * p.group - 1) / p.rows + 1);
+  // Grids past what a launch may hold do without eight waves, and without the rounding that by_xcd brings.
+  for (p.waves = eight_waves(c, heads, max_tokens, max_length) ? 8 : 4;; p.waves = 4) {
+    p.rows = 32 * p.waves;
+    p.tiles = (int)(((long long)max_tokens * p.group - 1) / p.rows + 1);
+    if (p.waves == 4 || fits_grid((long long)p.pairs * p.tiles, 64 * p.waves)) break;
+  }
   // Pieces, of four steps at least, where the tiles alone do not fill the card.
   const int slots = c.dim == 256 ? 32 : 64;
   const long long resident = c.dim == 256 || p.waves == 8 ? 256 : c.dim == 64 ? 768 : 512;
@@ -725,6 +727,8 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   // With a workgroup on every CU already, a second one and the join pay from some 20 steps on (32 / 8 heads:
   // 1024 tokens 39 us in two pieces, 34 in one, 32 x 30 after up to 700 34 and 28, after up to 2000 51 and 54).
   if (units >= 256 && max_length < 1280) p.pieces = 1;
+  p.by_xcd = p.pairs % 8 == 0 || p.pairs >= 64;
+  p.by_xcd = p.by_xcd && fits_grid(first_grid(p), 64 * p.waves);
   const size_t rows = p.pieces > 1 ? (size_t)units_of(p) * p.rows : 0;
   const size_t stats = align256(rows * sizeof(float2)), sums = align256(rows * sizeof(float));
   *bytes = stats + sums + rows * c.dim * 4;
