@@ -575,7 +575,8 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *    is stated at rrs_rope_kv_append. rrs_kv_evict moves single rows and refuses this format.
  *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
  *    read. A page that a call writes into belongs to one row of the table: that of a token that is
- *    appended, and every page of a cache that rrs_kv_evict takes. Others may be shared.
+ *    appended, and every page of a cache that rrs_kv_evict takes, which has it once. Others may be shared.
+ *    (RRS_DEBUG: else RRS_ERR_PRECONDITION; an append knows of a row as far as the page of its last token.)
  * Limits: head_dim 64, 128 or 256; page_size 16, 32, 64, 128 or 256; kv_heads,
  * sequences, max_pages, pages >= 1; sequences * kv_heads < 2^23; max_pages * page_size
  * <= 2^30. The struct is read on the host during the call only. A launch holds fewer than 2^32

@@ -129,7 +129,14 @@ rrs_status debug_check_lengths(const rrs_kv_cache& c, const int32_t* lengths, in
   return RRS_OK;
 }
 
-// The pages that M tokens are written to are pages of the cache.
+rrs_status shared_page(int page, int row, int other) {
+  std::fprintf(stderr, "[rrs] RRS_DEBUG: page %d, which the call writes into, is in rows %d and %d\n",
+               page, row, other);
+  return RRS_ERR_PRECONDITION;
+}
+
+// The pages that M tokens are written to are pages of the cache, each of one row: of rows that have a token here, as
+// far as their last one's page (entries behind a row's length may hold anything, and the lengths are not known).
 rrs_status debug_check_places(const rrs_kv_cache& c, const int32_t* seq, const int32_t* slot,
                               int M, void* stream) {
   std::unique_ptr<int32_t[]> b, s, t;
@@ -138,6 +145,10 @@ rrs_status debug_check_places(const rrs_kv_cache& c, const int32_t* seq, const i
   if (rrs_status e =
           debug_fetch_new(&t, c.table, (size_t)c.sequences * (size_t)c.max_pages, stream))
     return e;
+  std::unique_ptr<int64_t[]> written(new (std::nothrow) int64_t[(size_t)M]);  // page, row
+  std::unique_ptr<int32_t[]> entries(new (std::nothrow) int32_t[(size_t)c.sequences]());
+  if (!written || !entries) return RRS_ERR_HIP;
+  size_t count = 0;
   for (int m = 0; m < M; ++m) {
     const int32_t bm = b[(size_t)m], sm = s[(size_t)m];
     if (bm < 0 || bm >= c.sequences || sm < 0 || sm >= capacity(c)) continue;  // not stored
@@ -148,7 +159,43 @@ rrs_status debug_check_places(const rrs_kv_cache& c, const int32_t* seq, const i
                    (int)p, (int)c.pages);
       return RRS_ERR_PRECONDITION;
     }
+    written[count++] = (int64_t)p << 32 | bm;
+    entries[(size_t)bm] = std::max(entries[(size_t)bm], i + 1);
   }
+  int64_t* end = written.get() + count;
+  std::sort(written.get(), end);
+  for (size_t j = 1; j < count; ++j)
+    if (written[j] != written[j - 1] && written[j] >> 32 == written[j - 1] >> 32)
+      return shared_page((int)(written[j] >> 32), (int)(written[j - 1] & INT32_MAX),
+                         (int)(written[j] & INT32_MAX));
+  for (int r = 0; r < c.sequences; ++r)
+    for (int i = 0; i < entries[(size_t)r]; ++i) {
+      const int32_t p = t[(size_t)r * (size_t)c.max_pages + (size_t)i];
+      if (p < 0) continue;
+      const int64_t* at = std::lower_bound(written.get(), end, (int64_t)p << 32);
+      if (at != end && *at >> 32 == p && (*at & INT32_MAX) != r)
+        return shared_page(p, r, (int)(*at & INT32_MAX));
+    }
+  return RRS_OK;
+}
+
+// No page below the lengths is there twice. After debug_check_lengths.
+rrs_status debug_check_unshared(const rrs_kv_cache& c, const int32_t* lengths, void* stream) {
+  const size_t all = (size_t)c.sequences * (size_t)c.max_pages;
+  std::unique_ptr<int32_t[]> n, t;
+  if (rrs_status e = debug_fetch_new(&n, lengths, (size_t)c.sequences, stream)) return e;
+  if (rrs_status e = debug_fetch_new(&t, c.table, all, stream)) return e;
+  std::unique_ptr<int64_t[]> pages(new (std::nothrow) int64_t[all]);  // page, row
+  if (!pages) return RRS_ERR_HIP;
+  size_t count = 0;
+  for (int b = 0; b < c.sequences; ++b)
+    for (int i = 0; (int64_t)i * c.page_size < n[(size_t)b]; ++i)
+      pages[count++] = (int64_t)t[(size_t)b * (size_t)c.max_pages + (size_t)i] << 32 | b;
+  std::sort(pages.get(), pages.get() + count);
+  for (size_t j = 1; j < count; ++j)
+    if (pages[j] >> 32 == pages[j - 1] >> 32)
+      return shared_page((int)(pages[j] >> 32), (int)(pages[j - 1] & INT32_MAX),
+                         (int)(pages[j] & INT32_MAX));
   return RRS_OK;
 }
 
@@ -428,8 +475,10 @@ rrs_status rrs_kv_evict(const rrs_kv_cache* cache, const int32_t* lengths, int m
     return RRS_ERR_ALIGN;
   if (workspace_bytes < need) return RRS_ERR_WORKSPACE;
   if (rrs_status s = check_device()) return s;
-  if (debug)
+  if (debug) {
     if (rrs_status s = debug_check_lengths(c, lengths, max_length, stream)) return s;
+    if (rrs_status s = debug_check_unshared(c, lengths, stream)) return s;
+  }
   const rrs::EvictArgs a{lengths, max_length, weights,     slot_pos,    keep_from,
                          budget,  kept,       new_lengths, weights_out, pos_out};
   return from_hip(rrs::launch_kv_evict(a, view(c), workspace, static_cast<hipStream_t>(stream)));
