@@ -434,8 +434,13 @@ rrs_status rrs_prompt_attention(const void* Q, int M, int heads, const rrs_kv_ca
   if (rrs_status s = check_device()) return s;
   if (debug) {
     if (rrs_status s = debug_check_starts(row_start, c.sequences, M, max_tokens, stream)) return s;
-    if (rrs_status s = debug_check_finite_f16(
-            Q, (size_t)M * (size_t)heads * (size_t)c.head_dim, "Q", stream))
+    int32_t begin = 0, end = 0;  // rows of no sequence may hold anything
+    if (rrs_status s = debug_fetch(&begin, row_start, sizeof(begin), stream)) return s;
+    if (rrs_status s = debug_fetch(&end, row_start + c.sequences, sizeof(end), stream)) return s;
+    const size_t row = (size_t)heads * (size_t)c.head_dim;
+    if (rrs_status s =
+            debug_check_finite_f16(static_cast<const uint16_t*>(Q) + (size_t)begin * row,
+                                   (size_t)(end - begin) * row, "Q", stream))
       return s;
     if (rrs_status s = debug_check_lengths(c, lengths, max_length, stream)) return s;
   }
