@@ -95,7 +95,8 @@ enum {
   RRS_ERR_FLAGS = -9,      /* unknown or unsupported flag bits (_ex functions) */
   RRS_ERR_PRECONDITION = -10, /* RRS_DEBUG only: an input is not finite, perm /
                                  block_order is not a permutation, or an index of the
-                                 key/value cache's calls is out of range */
+                                 key/value cache's calls is out of range, or a place
+                                 or page that the call writes is not its own */
   RRS_ERR_TIMEOUT = -11       /* RRS_DEBUG only: a bounded wait between workgroups ran
                                  out (the affected outputs were written as NaN) */
 };
@@ -572,7 +573,8 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *    7, no infinities, 0x7F and 0xFF are NaN, largest 448). k_scale, v_scale: pages x kv_heads x
  *    page_size / 16 float16, one for each block of 16 slots of a page and head: a power of two s
  *    in [2^-15, 2^8] (0 counts as 2^-15). A row stands for q s, which is a float16 number exactly. What an append makes of it
- *    is stated at rrs_rope_kv_append. rrs_kv_evict moves single rows and refuses this format.
+ *    is stated at rrs_rope_kv_append. rrs_kv_evict moves single rows and refuses this format (weights and slot_pos
+ *    are kept for it all the same, for a mask, say).
  *  - table: sequences x max_pages int32. Entries past a sequence's last page are not
  *    read. A page that a call writes into belongs to one row of the table: that of a token that is
  *    appended, and every page of a cache that rrs_kv_evict takes, which has it once. Others may be shared.
@@ -585,7 +587,7 @@ rrs_status rrs_linear_reorder_scratch(const void* X, const void* Wq, const float
  *  - rrs_rope_kv_append: M >= 2^24; into RRS_KV_FP8 M + M / 16 >= 2^24 or, for M < 768,
  *    2048 + M min(heads * head_dim / 4096, 65535) >= 2^24;
  *  - rrs_paged_attention with weights, where they take a second launch (more than 16 query
- *    heads per KV head, or sequences that are cut): r * max_length / 1024, and sequences * heads
+ *    heads per KV head, or sequences that are cut): r * max_length / 1024, with sequences * heads added
  *    if they are cut, >= 2^24;
  *  - rrs_kv_evict: r >= 2^22 up to 16384 slots, r * max_length / 8192 >= 2^22 above; or 2^24 or more
  *    workgroups of 4096 bytes of k for rows that may move;
@@ -651,7 +653,9 @@ enum { RRS_ROPE_INTERLEAVED = 1 };
  * +-240 where s = 2^8, so that q s <= 61440), NaN where x is not finite. Where the scale grows, the block's
  * other rows get the codes of their q s in the new scale: the same numbers, but for those below 2^-6 s,
  * which are rounded to multiples of 2^-9 s. A value is off by at most 2^-4 of itself or half of 2^-9 s,
- * and by that half once more, in smaller scales, for every time that its scale has grown.
+ * and by that half once more, in smaller scales, for every time that its scale has grown. A scale does not become smaller
+ * until the block's first slot is written: tokens that are taken back (a row cut to fewer slots: rejected proposals,
+ * say) leave the block the scale that they brought, and its older rows their rounding.
  */
 rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int heads,
                               const int32_t* positions, int axes, const int32_t* sections,
@@ -664,7 +668,7 @@ rrs_status rrs_rope_kv_append(const void* qkv, int64_t row_stride, int M, int he
  * appended before):
  *   out[b, h] = sum_t p_t v_t,  p = softmax over t < lengths[b] of scale q_bh . k_t.
  *   Q        in : sequences x heads x head_dim float16; heads a multiple of kv_heads, query
- *                 head h reads KV head h / (heads / kv_heads).
+ *                 head h reads KV head h / (heads / kv_heads). sequences * heads < 2^23.
  *   lengths  in : sequences int32; max_length >= every length, 1 <= max_length <=
  *                 max_pages * page_size. The launches and the workspace follow from it, not from
  *                 the lengths: short sequences under a large bound are not taken in the forms
@@ -712,7 +716,8 @@ rrs_status rrs_paged_attention(const void* Q, int heads, const rrs_kv_cache* cac
  *                  contents ignored.
  * RRS_KV_INT4 rows stand for fp16(q s), as rrs_kv_read gives them (of a scale of 9360 for 9352 q). Logits,
  * softmax and sums in float32; for the product with V the weights are rounded to float16 in units of their own:
- * off by 2^-11 relative, or by 2^-37 of the row's largest one where that is more. Results repeat bit for bit
+ * off by 2^-11 relative, or by 2^-37 of the row's largest one where that is more, and divided by the sum of what they
+ * were rounded to (slots of equal values give that value). Results repeat bit for bit
  * for the same arguments; they depend on other sequences through their lengths and rows, max_tokens and
  * max_length only, which decide where sums are cut. max_tokens * heads / kv_heads < 2^31 - 256; with r =
  * sequences * kv_heads and t = max_tokens * heads / kv_heads / 128 rounded up, r t (times the pieces that the

@@ -240,7 +240,7 @@ const char* rrs_status_string(rrs_status s) {
              "affected outputs are NaN";
     case RRS_ERR_PRECONDITION:
       return "RRS_ERR_PRECONDITION: (RRS_DEBUG) an input is not finite, a permutation is not "
-             "one, or an index is out of range";
+             "one, an index is out of range, or a page to be written is not one row's";
     default: return "RRS_ERR_UNKNOWN";
   }
 }

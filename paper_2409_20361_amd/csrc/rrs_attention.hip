@@ -42,7 +42,7 @@
 // steps, of which the first waits for its loads), one of 213 with 32 heads 5.8.
 //
 // Of a few tokens (kTokens) every one has its columns, and a limit to the slots that it sees: that costs a comparison in
-// the last tiles only. 32 sequences of 4 tokens after up to 6000, 32 / 8 heads of 128, FP8, 48 us (3.7 TB/s with the
+// the last tiles only. 32 sequences of up to 4 tokens after up to 6000, 32 / 8 heads of 128, FP8, 48 us (3.7 TB/s with the
 // join), INT4 40, 9 of up to 7 after up to 1501, 20 / 5 heads of 64, float16, 13.7.
 #include <type_traits>
 
@@ -1223,13 +1223,14 @@ hipError_t launch_paged_attention(const AttentionArgs& a, const KvView& c, hipSt
   return launch_dim<false>(a, c, p, stream);
 }
 
-// Up to 16 columns are read as fast as one token's (32 sequences of 4 tokens after 6000, 32 / 8 heads of
-// 128: FP8 85 -> 48 us, INT4 80 -> 40, float16 106 -> 85; 16 of 16 after 3000, 32 / 32 heads, FP8, 79 -> 59). More are
-// several row blocks, each of which reads the rows: taken where the slots that they read are few (4 of 16 tokens
-// after 300, 32 / 8 heads, float16, 14.2 -> 8.6 us, after 3000 25.2 -> 24.4; 8 of 16 28.0 and 31.8, one of 32 after
-// 16000 37 and 49), and two blocks also where a row is a short read or the other kernel's tile is a small one (32 of 8
-// after 6000, FP8 90 -> 81, INT4 91 -> 77; head dim 256, 8 of 16 after 3000, 16 / 16 heads, 89 -> 65; float16 at 128
-// 119 and 136), while the blocks run at the same time (32 of 32 alone, 16 / 16 heads, 1024 blocks: 9.2 and 11.3).
+// Measured on batches n x t after s: n sequences, the first of t new tokens behind s cached ones, the others of 1 to t
+// behind 0 to s. Up to 16 columns are read as fast as one token's (32 x 4 after 6000, 32 / 8 heads of 128: FP8 85 -> 48
+// us, INT4 80 -> 40, float16 106 -> 85; 16 x 16 after 3000, 32 / 32 heads, FP8, 79 -> 59). More are
+// several row blocks, each of which reads the rows: taken where the slots that they read are few (4 x 16
+// after 300, 32 / 8 heads, float16, 14.2 -> 8.6 us, after 3000 25.2 -> 24.4; 8 x 16 28.0 and 31.8, 1 x 32 after
+// 16000 37 and 49), and two blocks also where a row is a short read or the other kernel's tile is a small one (32 x 8
+// after 6000, FP8 90 -> 81, INT4 91 -> 77; head dim 256, 8 x 16 after 3000, 16 / 16 heads, 89 -> 65; float16 at 128
+// 119 and 136), while the blocks run at the same time (32 x 32 after 0, 16 / 16 heads, 1024 blocks: 9.2 and 11.3).
 bool few_tokens(const KvView& c, int heads, int max_tokens, int max_length) {
   const long long columns = (long long)max_tokens * (heads / c.heads);
   if (columns > 128) return false;

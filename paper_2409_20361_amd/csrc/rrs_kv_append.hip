@@ -491,10 +491,10 @@ __global__ void __launch_bounds__(kThreads)
 
 // Workgroups of an append into FP8. A window of 16 rows has work for one workgroup per pair of heads if its
 // tokens are a prompt's, and for 16 if each is of another sequence, which the host does not know. Workgroups
-// without work delay the others, so there are more than the pairs only up to two per CU (into 8 heads of 128: 500
-// tokens of a prompt 11.6 us, with four per CU 14.7, 2000 17.8 and 21.6; one per sequence, 1000 131 us, with
-// none added 147, 800 into one head of 64 16, 14.7 with four, 42 with none), and fewer where windows alone
-// are many (6113 tokens into 32 heads: 2048 in all 99 us, 1024 109, 4096 108).
+// without work delay the others, so there are more than the pairs only up to two per CU (the append alone, from 32
+// heads into 8 of 128: 500 tokens of a prompt 7.7 us, with four per CU 10.5, with none added 8.4, 2000 11.5, 15.4, 11.6; a
+// token of each of 64 sequences 5.1, 5.8, 36.4, of 1000 23.6, 23.3, 36.5; of 800 into one head of 64 7.0, 6.4, 32), and
+// fewer where windows alone are many (6113 tokens into 32 heads: 2048 in all 57 us, 1024 64, 4096 65).
 struct Append8 {
   int parts, query_parts;
   int block_groups;

@@ -17,14 +17,16 @@
 // product, a sum and a maximum per row and slot, and a part of each tile's way to LDS) run beside them.
 // The next block's S^T is computed beside this block's exponentials, and every product's operands are
 // read three products ahead, in an issue order that is written out: left to itself the compiler reads an
-// operand and waits for it (prompts of 8192 tokens, four, 32 / 8 heads of 128, FP8: 1147 -> 915 us).
+// operand and waits for it (four prompts of up to 8192 tokens, 32 / 8 heads of 128, FP8: 1147 -> 915 us).
 // Addresses of a wave's rows are scalar (its rows lie in one block of 16 slots, one page), and what is rare is
 // kept out of the loop, where its constants cost the scalar registers of all (1147 -> 983 us).
-// Measured: that batch 900 us (950 TFLOP/s; a float16 product of 8192^3 in the library reaches 1210; without the
-// exponentials, or without the way to LDS, 7 and 12 % less); as float16 945 us; two of 8192 with 16 / 8
-// heads of 256 880 (670); 1024 tokens after 12288 in INT4 265 us (810). Small calls are a chain of
-// launch, rows, pages and tiles and a second launch: eight of 16 tokens after 3000, 32 / 8 heads of 128, 28 us. A
-// few tokens over a long cache leave most of the matrix instructions' columns empty and are bound by HBM:
+// Measured: that batch 905 us (950 TFLOP/s; a float16 product of 8192^3 in the library reaches 1210; without the
+// exponentials, or without the way to LDS, 7 and 12 % less), 890 to 960 from card to card; as float16 955 us (900),
+// with 32 heads of 64 538 (800), two of up to 8192 with 16 / 8 heads of 256 813 (720: one workgroup per CU, and a
+// barrier for every 32 slots); 1024 tokens after 12288 in INT4 with lse 271 us (790). One prompt, 32 / 8 heads of
+// 128: 1024 tokens 33 us (260), 2048 64 (540): tiles that see most end long after the others. Small calls are a chain of launch,
+// rows, pages and tiles and a second launch: eight of up to 16 tokens after up to 3000, 27 us. A few tokens over a
+// long cache leave most of the matrix instructions' columns empty and are bound by HBM:
 // they go to the kernel of single tokens (few_tokens).
 //
 // Where the rows do not fill the card, the slots are cut into pieces, joined by a second kernel in order.
@@ -159,8 +161,8 @@ struct Where {
 };
 __device__ __forceinline__ bool find_tile(const PromptArgs& a, const KvView& c, const Plan& plan,
                                           Where* w) {
-  // Tiles that see most come first. Those of a pair are on one XCD and share its L2, where that
-  // leaves no XCD without work.
+  // A pair's tiles that see most come first; pairs come in their order, whatever they see. A pair's tiles are on one
+  // XCD and share its L2, where that leaves no XCD without work.
   const int per = plan.tiles * plan.pieces;
   int pair, k;
   if (plan.by_xcd) {
@@ -185,7 +187,8 @@ __device__ __forceinline__ bool find_tile(const PromptArgs& a, const KvView& c, 
 }
 
 // kLse: the logarithm of the sum is asked for, which takes the weights before they are rounded: a second sum (four
-// prompts of 8192 tokens, 32 / 8 heads of 128, FP8: 892 us without, 925 with it).
+// prompts of up to 8192 tokens, 32 / 8 heads of 128, FP8: 905 us without, 939 with it; with the float32 sum alone, by
+// which a row of equal values is off by a float16 step, 893).
 template <int D, int kFormat, bool kMask, bool kLse, int kWaves>
 __global__ void __launch_bounds__((Tile<D, kFormat, kWaves>::kThreads),
                                   (Tile<D, kFormat, kWaves>::kPerSimd))
@@ -688,7 +691,8 @@ int join_rows(int dim, int pieces) {
 // They are taken for 1024 rows or more of one sequence behind at least as many cached tokens (32 / 8 heads:
 // 1024 after 8000, INT4, 206 -> 187 us, 512 after 8000, FP8, 106 -> 97; 2000 after 2000, 32 / 32 heads, float16,
 // 163 -> 144; but 300 after 300, 32 / 32 heads, 26 against 31) and from so many rows of all sequences and KV heads
-// times slots on (4096 tokens of one sequence 188 -> 170, 8192 of four 937 -> 891); not for less without a past (2048 of one 66 against 72, 512 of four after up to 4000 120 against 129).
+// times slots on (4096 tokens of one sequence 188 -> 170, up to 8192 of four 937 -> 891); not for less without a past
+// (2048 of one 66 against 72, up to 512 of four after up to 4000 120 against 129).
 constexpr long long kWide = 5ll << 26;
 bool eight_waves(const KvView& c, int heads, int max_tokens, int max_length) {
   if (c.dim != 128) return false;
@@ -725,7 +729,7 @@ Plan make_plan(const KvView& c, int heads, int max_tokens, int max_length, void*
   const long long most = std::max(1, ((max_length - 1) / slots + 1) / 4);
   p.pieces = (int)std::min(most, std::max(1ll, resident / units));
   // With a workgroup on every CU already, a second one and the join pay from some 20 steps on (32 / 8 heads:
-  // 1024 tokens 39 us in two pieces, 34 in one, 32 x 30 after up to 700 34 and 28, after up to 2000 51 and 54).
+  // 1024 tokens 39 us in two pieces, 34 in one, 32 x up to 30 after up to 700 34 and 28, after up to 2000 51 and 54).
   if (units >= 256 && max_length < 1280) p.pieces = 1;
   p.by_xcd = p.pairs % 8 == 0 || p.pairs >= 64;
   p.by_xcd = p.by_xcd && fits_grid(first_grid(p), 64 * p.waves);
